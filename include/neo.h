@@ -662,6 +662,142 @@ int neo_layout_search(const neo_node* nodes, int n_nodes, int N, int C, int H, i
 /* Message of the last failing call on this thread ("" if none). */
 const char* neo_last_error(void);
 
+/* ======================================================================================
+ * Token operators: the integer path of a transformer layer (integer inference
+ * is the paper's future work, Sections 1 and 5; the scheme is the one of the
+ * dense layer above with one scale per token instead of one per tensor).
+ *
+ * Quantization of a row of values v: s = max|v| / 127 in float32 (1 for a row
+ * of zeros; at least the smallest normal float), q = clamp(round_half_even(v /
+ * s), -127, 127), the division in float32.  A row with an infinity or a NaN
+ * gets s = NaN and q = 0, so whatever is computed from it is NaN.
+ * int8 rows are padded with zero bytes to INp = ceil(cols / 16) * 16, their
+ * pointers 16-byte aligned and their strides multiples of 16 (NEO_ERR_ALIGN).
+ * Pointers to float data (float32, float16, bfloat16: enum neo_dtype) need
+ * their element's alignment only.  Strides are in elements, in 64 bits, and
+ * at least the row's length; offsets are computed in 64 bits, so tensors may
+ * exceed 2^31 - 1 elements.  A call with no tokens (rows, M or tokens 0)
+ * succeeds and does nothing.  Sums, norms and softmax statistics are float32
+ * (int32 for integer products, exact).  Results do not depend on other work
+ * on the device: the same call gives the same bits.
+ * ====================================================================================== */
+enum neo_dtype { NEO_F32 = 0, NEO_F16 = 1, NEO_BF16 = 2 };
+
+/*
+ * Residual addition, root-mean-square norm, quantization:
+ *   h = x + residual,  y = h / sqrt(mean(h^2) + eps) * gamma,  (yq, y_scale) = quantized y
+ * evaluated in float32 from the unrounded h; h and y rounded once.
+ *   x         device [rows][cols] of `dtype`
+ *   residual  device, the same shape and type, or NULL (h = x)
+ *   gamma     device float32 [cols], or NULL (ones)
+ *   h         device, `dtype`, or NULL: the residual stream.  May be x or
+ *             residual itself (same pointer and stride)
+ *   y         device, `dtype`, or NULL: the norm unquantized
+ *   yq        device int8 [rows][INp], with y_scale device float32 [rows]; both or neither
+ * cols at most 65,536 (NEO_ERR_UNSUPPORTED).  eps >= 0 and finite.
+ */
+int neo_rmsnorm_int8(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                     const float* gamma, float eps, int rows, int cols, int dtype, void* h,
+                     int64_t h_stride, void* y, int64_t y_stride, int8_t* yq, int64_t yq_stride,
+                     float* y_scale, neo_stream_t stream);
+
+/*
+ * Rows quantized with a scale of their own: v = x, or with `gate` (non-NULL)
+ * v = x * gate / (1 + exp(-gate)), the gated unit between a transformer's two
+ * MLP products, in float32.  x and gate device [rows][cols] of `dtype` (they
+ * may be the halves of one buffer), xq device int8 [rows][INp], x_scale device
+ * float32 [rows].  cols at most 65,536.
+ * neo_dequantize_tokens_int8: y[i][j] = xq[i][j] * x_scale[i], rounded once to `dtype`.
+ */
+int neo_quantize_tokens_int8(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
+                             int rows, int cols, int dtype, int8_t* xq, int64_t xq_stride,
+                             float* x_scale, neo_stream_t stream);
+int neo_dequantize_tokens_int8(const int8_t* xq, int64_t xq_stride, const float* x_scale, int rows,
+                               int cols, int dtype, void* y, int64_t y_stride, neo_stream_t stream);
+
+/*
+ * Product of int8 rows and int8 weight rows with scales per token and channel:
+ *   y[m][n] = act( (float32(sum_k xq[m][k] * w_rows[n][k]) * x_scale[m]) * w_scale[n] + bias[n] )
+ * the sum exact in int32, then one float32 rounding per operation and one to `dtype`.
+ *   xq      device int8 [M][INp] (row stride xq_stride), x_scale device float32 [M]
+ *   w_rows  device int8 [out_features][INp], w_scale device float32
+ *           [out_features], as neo_pack_dense_int8 writes them
+ *   bias    device float32 [out_features], or NULL;  act enum neo_act
+ *   y       device [M][out_features] of `dtype`, row stride y_stride
+ * in_features at most 133,144 (the int32 sum's bound).  A product split over
+ * in_features keeps its partial sums in the workspace of the stream, grown as
+ * neo_conv2d_nchwxc's (NEO_ERR_STATE if it would have to grow during capture).
+ */
+int neo_matmul_int8(const int8_t* xq, int64_t xq_stride, const float* x_scale, int M, int in_features,
+                    const int8_t* w_rows, const float* w_scale, int out_features, const float* bias,
+                    int act, int dtype, void* y, int64_t y_stride, neo_stream_t stream);
+
+/*
+ * Paged key/value cache in int8: token entry o of page p, head h holds
+ * head_dim keys k[((p * kv_heads + h) * page_size + o) * head_dim ...] and the
+ * scale k_scale[(p * kv_heads + h) * page_size + o]; values likewise.  All
+ * device memory, k and v 16-byte aligned; offsets are 64-bit.  head_dim is a
+ * multiple of 16 up to 256; page_size any.
+ */
+typedef struct neo_kv_cache {
+    int8_t* k;
+    int8_t* v;
+    float* k_scale;
+    float* v_scale;
+    int pages, kv_heads, page_size, head_dim;
+} neo_kv_cache;
+
+/*
+ * neo_kv_write_int8: token t's keys and values, device [tokens][kv_heads][head_dim]
+ *   of `dtype` (strides per token and per head), quantized per token and head
+ *   into the entry slots[t] (device int64: page * page_size + entry).  Tokens
+ *   whose slot lies outside the cache (-1, say) are skipped.  Slots must differ.
+ * neo_kv_read_int8: out[t][h] = the entry slots[t] times its scale, rounded
+ *   once to `dtype`, [tokens][kv_heads][head_dim] contiguous; zeros for a slot
+ *   outside the cache.  k_out or v_out may be NULL.
+ */
+int neo_kv_write_int8(const neo_kv_cache* cache, const void* k, int64_t k_token_stride,
+                      int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                      int64_t v_head_stride, int tokens, int dtype, const int64_t* slots,
+                      neo_stream_t stream);
+int neo_kv_read_int8(const neo_kv_cache* cache, const int64_t* slots, int tokens, int dtype,
+                     void* k_out, void* v_out, neo_stream_t stream);
+
+/*
+ * Causal attention of each sequence's newest tokens over its paged cache (the
+ * newest tokens' own keys and values are in the cache already).  Sequence b
+ * has context_lens[b] cached tokens, of which the last n_b = q_starts[b + 1] -
+ * q_starts[b] are its queries: rows q_starts[b] .. q_starts[b + 1] - 1 of q.
+ * Query i of them stands at position p = context_lens[b] - n_b + i and sees
+ * the tokens 0 .. p (with window > 0 only the last `window` of those):
+ *   out[i][hq] = sum_j softmax_j(scale * q[i][hq] . k_j) v_j,  k_j, v_j of the
+ *   kv head hq / (q_heads / kv_heads), dequantized.
+ * A query that sees nothing (p < 0) gets zeros.  What the cache holds in
+ * entries that a query does not see never reaches its output.
+ *   q, out        device [tokens][q_heads][head_dim] of `dtype`, strides per
+ *                 token and head; q_heads a multiple of kv_heads
+ *   page_table    device int32 [seqs][table_stride]: token j of sequence b
+ *                 lies in page page_table[b][j / page_size].  An entry outside
+ *                 [0, pages) hides its tokens from every query
+ *   context_lens, q_starts  device int32 [seqs], [seqs + 1]; q_starts[0] = 0,
+ *                 ascending, q_starts[seqs] = tokens
+ *   max_chunk, max_context  host: bounds of n_b and of context_lens (at most
+ *                 table_stride * page_size); tokens past them are not computed
+ *                 and not read
+ * Products run on fp16 MFMA with float32 sums: int8 values are exact there,
+ * float16 and bfloat16 queries too (scaled by a power of two per row); the
+ * softmax weights are rounded to 11 bits, and float32 queries and their
+ * weights are taken as two fp16 terms (22 bits).  A call split over the
+ * context keeps its parts in the workspace of the stream (as neo_matmul_int8).
+ */
+int neo_attention_paged_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride,
+                             int64_t q_head_stride, int tokens, int q_heads, int dtype,
+                             const int32_t* page_table, int64_t table_stride,
+                             const int32_t* context_lens, const int32_t* q_starts, int seqs,
+                             int max_chunk, int max_context, float scale, int window, void* out,
+                             int64_t out_token_stride, int64_t out_head_stride,
+                             neo_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -115,6 +115,57 @@ void from_kernel_order(const float* in, const ConvShape& s, float* packed) {
                     }
 }
 
+namespace {
+
+// Split-reduction workspace of the standalone calls, one per
+// (device, stream) so that calls on different streams never share it; calls
+// on one stream are ordered by the stream.  Grows on demand (hipFree of the
+// old buffer, hipMalloc of the new one); a call that would grow it while the
+// stream is being captured into a graph fails with NEO_ERR_STATE and launches
+// nothing (allocation is not capturable), so the first call of a given size
+// must be made outside capture.
+struct StreamWs {
+    float* ws = nullptr;
+    size_t bytes = 0;
+};
+std::mutex g_ws_mu;
+std::map<std::pair<int, hipStream_t>, StreamWs> g_ws;
+
+}  // namespace
+
+int stream_workspace(const char* fn, hipStream_t st, size_t bytes, float** ws) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return hip_fail(e, (std::string(fn) + ": hipGetDevice").c_str());
+    std::lock_guard<std::mutex> lk(g_ws_mu);
+    StreamWs& w = g_ws[{dev, st}];
+    if (w.bytes < bytes) {
+        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+        e = hipStreamIsCapturing(st, &cap);
+        if (e != hipSuccess) return hip_fail(e, (std::string(fn) + ": hipStreamIsCapturing").c_str());
+        if (cap != hipStreamCaptureStatusNone)
+            return fail(NEO_ERR_STATE, std::string(fn) + ": the split-reduction workspace must "
+                                       "grow to " + std::to_string(bytes) + " bytes, which "
+                                       "cannot happen during stream capture; make one call of "
+                                       "this size outside capture first");
+        if (w.ws) {
+            e = hipFree(w.ws);
+            w.ws = nullptr;
+            w.bytes = 0;
+            if (e != hipSuccess) return hip_fail(e, (std::string(fn) + ": hipFree of the workspace").c_str());
+        }
+        e = hipMalloc(&w.ws, bytes);
+        if (e != hipSuccess) {
+            w.ws = nullptr;
+            return fail(NEO_ERR_OOM, std::string(fn) + ": workspace allocation of " +
+                                         std::to_string(bytes) + " bytes: " + hipGetErrorString(e));
+        }
+        w.bytes = bytes;
+    }
+    *ws = w.ws;
+    return NEO_OK;
+}
+
 }  // namespace neo
 
 using namespace neo;
@@ -152,53 +203,6 @@ long blocked_elems(long N, long C, long H, long W, int blk) {
     } while (0)
 
 int out_dim(int n, int k, int s, int p) { return (n + 2 * p - k) / s + 1; }
-
-// Split-reduction workspace of the standalone convolution call, one per
-// (device, stream) so that calls on different streams never share it; calls
-// on one stream are ordered by the stream.  Grows on demand (hipFree of the
-// old buffer, hipMalloc of the new one); a call that would grow it while the
-// stream is being captured into a graph fails with NEO_ERR_STATE and launches
-// nothing (allocation is not capturable), so the first call of a given size
-// must be made outside capture.
-struct StreamWs {
-    float* ws = nullptr;
-    size_t bytes = 0;
-};
-std::mutex g_ws_mu;
-std::map<std::pair<int, hipStream_t>, StreamWs> g_ws;
-
-int stream_workspace(hipStream_t st, size_t bytes, float** ws) {
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return hip_fail(e, "neo_conv2d_blocked: hipGetDevice");
-    std::lock_guard<std::mutex> lk(g_ws_mu);
-    StreamWs& w = g_ws[{dev, st}];
-    if (w.bytes < bytes) {
-        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-        e = hipStreamIsCapturing(st, &cap);
-        if (e != hipSuccess) return hip_fail(e, "neo_conv2d_blocked: hipStreamIsCapturing");
-        if (cap != hipStreamCaptureStatusNone)
-            return fail(NEO_ERR_STATE, "neo_conv2d_blocked: the split-reduction workspace must "
-                                       "grow to " + std::to_string(bytes) + " bytes, which "
-                                       "cannot happen during stream capture; make one call of "
-                                       "this size outside capture first");
-        if (w.ws) {
-            e = hipFree(w.ws);
-            w.ws = nullptr;
-            w.bytes = 0;
-            if (e != hipSuccess) return hip_fail(e, "neo_conv2d_blocked: hipFree of the workspace");
-        }
-        e = hipMalloc(&w.ws, bytes);
-        if (e != hipSuccess) {
-            w.ws = nullptr;
-            return fail(NEO_ERR_OOM, std::string("neo_conv2d_blocked: workspace allocation of ") +
-                                         std::to_string(bytes) + " bytes: " + hipGetErrorString(e));
-        }
-        w.bytes = bytes;
-    }
-    *ws = w.ws;
-    return NEO_OK;
-}
 
 // Optional override of the launch configuration, "fk,fp,split[,waves]", for
 // tuning sweeps of the standalone call.
@@ -370,7 +374,7 @@ int neo_conv2d_nchwxc(const float* x, int x_block, int N, int C, int H, int W,
     if (rc != NEO_OK) return rc;
     float* ws = nullptr;
     if (cfg.split > 1) {
-        rc = stream_workspace((hipStream_t)stream, conv_workspace_bytes(s, cfg), &ws);
+        rc = stream_workspace("neo_conv2d_blocked", (hipStream_t)stream, conv_workspace_bytes(s, cfg), &ws);
         if (rc != NEO_OK) return rc;
     }
     hipError_t e = launch_conv2d(s, cfg, x, w_packed, false, bias, res, y, ws,
@@ -444,7 +448,7 @@ int neo_conv2d_winograd(const float* x, int N, int C, int H, int W, const float*
     env_wino_config(s, &cfg);
     float* ws = nullptr;
     if (cfg.split > 1) {
-        rc = stream_workspace((hipStream_t)stream, conv_workspace_bytes(s, cfg), &ws);
+        rc = stream_workspace("neo_conv2d_blocked", (hipStream_t)stream, conv_workspace_bytes(s, cfg), &ws);
         if (rc != NEO_OK) return rc;
     }
     hipError_t e = launch_wino(s, cfg, x, u, bias, res, y, ws, (hipStream_t)stream);

@@ -1,0 +1,451 @@
+// Causal attention of the newest tokens of each sequence over its paged int8
+// cache:
+//
+//   out[i] = sum_j w_ij v_j / sum_j p_ij,   p_ij = exp(scale q_i.k_j - m_i)
+//   k_j = ks_j K_j,  v_j = vs_j V_j  (K, V int8),  w_ij = p_ij vs_j
+//
+// in one pass over the cache with the running maximum m_i and sum of each row.
+//
+// The rows of a unit (a sequence and a key/value head) are its new tokens times
+// the query heads that share the head: row = token * G + head.  Products run on
+// fp16 MFMA with float32 sums.  int8 values are exact in fp16.  A query row is
+// scaled by a power of two that puts its largest value in [2^14, 2^15), so
+// float16 and bfloat16 queries are exact too (values 2^-28 of the largest and
+// less lose bits); a float32 query is the sum of two fp16 terms.  The weights
+// w_ij are scaled by 2^(14 - E), E the exponent of the largest vs that the row
+// has seen so far, and rounded to fp16 (float32: two terms; Levels below).
+//
+// S^T = K Q^T and O^T = V^T P^T: the accumulator's layout of S^T (a lane holds
+// four neighbouring keys of one row) is the layout of the second product's
+// operand, so weights go from one product to the other in registers.
+#include "token_types.h"
+
+namespace neo {
+namespace {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLift = 14.f;  // weights are at most 2^15: the top of fp16's range
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kMinusInf = -__builtin_inff();
+
+// ---- int8 to fp16 ------------------------------------------------------------------------
+// A byte v + 128 (the sign bit flipped) under a zero byte is the fp16 number
+// (v + 128) 2^-24; times 2^15, minus 2^-2, it is v 2^-9, exactly.
+constexpr float kInt8Unit = 1.f / 512;
+__device__ inline uint32_t biased(uint32_t w) { return w ^ 0x80808080u; }
+__device__ inline h2 from_biased(uint32_t halves) {
+    const h2 up = {(_Float16)32768.f, (_Float16)32768.f}, bias = {(_Float16)-0.25f, (_Float16)-0.25f};
+    return __builtin_elementwise_fma(__builtin_bit_cast(h2, halves), up, bias);
+}
+// Four neighbouring bytes of one dword; one byte of each of two dwords.
+__device__ inline void unpack4(uint32_t w, h2& lo, h2& hi) {
+    lo = from_biased(__builtin_amdgcn_perm(0, w, 0x0c010c00u));
+    hi = from_biased(__builtin_amdgcn_perm(0, w, 0x0c030c02u));
+}
+__device__ inline h2 pair(uint32_t a, uint32_t b, int t) {
+    return from_biased(__builtin_amdgcn_perm(b, a, 0x0c000c00u | (uint32_t)(4 + t) << 16 | (uint32_t)t));
+}
+__device__ inline h8 join(h2 a, h2 b, h2 c, h2 d) {
+    return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ inline int exponent(uint32_t bits) { return (int)(bits >> 23) - 127; }
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Weights in fp16.  A term holds 11 bits from fp16's least normal number 2^-14
+// up, two terms hold 22 from 2^-3 up; smaller weights (of keys whose scores lie
+// far below the row's largest) are taken in further passes, scaled up by `step`
+// each, so that every weight keeps its bits: a position at which the largest
+// keys' values are 0 is the sum of the small ones.
+template <int TERMS>
+struct Levels {
+    static constexpr float least = TERMS == 1 ? 0x1p-14f : 0x1p-3f, step = TERMS == 1 ? 0x1p28f : 0x1p17f;
+    __device__ static void terms(const f32x8& v, h8 (&w)[TERMS]) {
+        w[0] = __builtin_convertvector(v, h8);
+        if constexpr (TERMS == 2) w[1] = __builtin_convertvector(v - __builtin_convertvector(w[0], f32x8), h8);
+    }
+    // The terms of the weights from `least` up; the others scaled for the next
+    // pass.  Returns whether any is left.
+    __device__ static bool take(f32x8& v, h8 (&w)[TERMS]) {
+        f32x8 now;
+        bool left = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool later = v[i] < least;  // (a NaN goes now)
+            now[i] = later ? 0.f : v[i];
+            v[i] = later ? v[i] * step : 0.f;
+            left |= v[i] != 0.f;
+        }
+        terms(now, w);
+        return left;
+    }
+};
+
+// ---- a unit's tokens -----------------------------------------------------------------
+struct Unit {
+    int first, n, all, ctx, end;  // first row of q; new tokens computed, all of them; cached tokens, those read
+};
+__device__ inline Unit unit_of(const AttnArgs& a, int b) {
+    Unit u;
+    u.first = min(max(a.starts[b], 0), a.tokens);
+    u.all = min(max(a.starts[b + 1], u.first), a.tokens) - u.first;
+    u.n = min(u.all, a.max_chunk);
+    u.ctx = max(a.contexts[b], 0);
+    u.end = min(u.ctx, a.max_context);
+    return u;
+}
+// The keys [lo, hi) that the chunk's tokens t0 .. t1 see.
+__device__ inline void key_range(const AttnArgs& a, const Unit& u, int t0, int t1, int& lo, int& hi) {
+    hi = min(u.end, u.ctx - u.all + t1 + 1);
+    lo = a.window ? max(0, u.ctx - u.all + t0 + 1 - a.window) : 0;
+    hi = max(hi, lo);
+}
+
+// Splits of the keys: `keys` (a multiple of 128) each, counted from the range's
+// start rounded down to a multiple of 32.
+struct Split {
+    int count, keys;
+};
+__device__ inline int splits_of(const Split& sp, int lo, int hi) {
+    return min(sp.count, max(1, (hi - (lo & ~31) + sp.keys - 1) / sp.keys));
+}
+
+// A row's parts in the workspace: o[unit][row][split][head_dim] in true units
+// relative to the part's maximum, ml[unit][row][split] (maximum, sum).
+struct Parts {
+    float* o;
+    float2* ml;
+    int rows;  // rows a unit can have
+};
+
+template <typename T>
+__device__ inline void store_row(const AttnArgs& a, const Unit& u, int h, int G, int row, int d, float v) {
+    const int t = row / G, hq = h * G + row - t * G;
+    static_cast<T*>(a.out)[(int64_t)(u.first + t) * a.ots + (int64_t)hq * a.ohs + d] = (T)v;
+}
+
+// ---- 16 rows a workgroup ------------------------------------------------------------
+// Four waves take turns at blocks of 32 keys; the key and value bytes go from
+// memory straight into registers (every byte is used once) and the waves'
+// results are joined in LDS.
+constexpr int kRowsWaves = 4;
+
+template <typename T, int DP, int TERMS>
+__global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Split sp, Parts ws) {
+    constexpr int KB = DP / 4, STEPS = DP / 32, VB = DP / 16;  // bytes of a key a lane holds, products, of a value
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim, ps = a.c.page_size;
+    const int split = blockIdx.x % sp.count, at = blockIdx.x / sp.count;
+    const int units = a.seqs * H, tile = at / units, unit = at - tile * units, b = unit / H, h = unit - b * H;
+    const Unit u = unit_of(a, b);
+    const int rows = u.n * G, row0 = tile * 16;
+    if (row0 >= rows) return;
+    int lo, hi;
+    key_range(a, u, row0 / G, (min(row0 + 16, rows) - 1) / G, lo, hi);
+    const int first = (lo & ~31) + split * sp.keys, last = min(hi, first + sp.keys);
+    if (split >= splits_of(sp, lo, hi)) return;
+
+    // this lane's row of queries: values d = g * KB + ...
+    const int row = row0 + li;
+    const bool live = row < rows;
+    const int tok = (live ? row : row0) / G, pos = u.ctx - u.all + tok;
+    h8 q[TERMS][STEPS];
+    float fq;  // what a score is multiplied with
+    {
+        const int hq = h * G + (live ? row : row0) - tok * G;
+        const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)hq * a.qhs + g * KB;
+        f32x8 v[STEPS];
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            v[s] = g * KB + s * 8 < D ? load8(src + s * 8) : f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[s][i]));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+        const int e = top >= kInfBits ? 0 : min(14 - exponent(top), 126);
+        const float up = ldexpf(1.f, e);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            v[s] *= up;
+            q[0][s] = __builtin_convertvector(v[s], h8);
+            if constexpr (TERMS == 2) q[1][s] = __builtin_convertvector(v[s] - __builtin_convertvector(q[0][s], f32x8), h8);
+        }
+        fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
+        // (no score of a query with an infinity is finite: its softmax is undefined)
+        if (top >= kInfBits) fq = __uint_as_float(0x7fc00000u);
+    }
+
+    v4f o[VB];
+#pragma unroll
+    for (int t = 0; t < VB; ++t) o[t] = v4f{0, 0, 0, 0};
+    float m = kMinusInf, l = 0.f;
+    int E = -127;  // exponent of the largest value scale seen so far
+
+    for (int kb = first + wave * 32; kb < last; kb += kRowsWaves * 32) {
+        // K: this lane's keys are kb + li and kb + 16 + li
+        u4 kw[2][KB / 16];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int key = min(kb + 16 * t + li, hi - 1), pg = key / ps;
+            int page = a.table[b * a.table_stride + pg];
+            if ((uint32_t)page >= (uint32_t)a.c.pages) page = 0;
+            const int8_t* p = a.c.k + (((int64_t)page * H + h) * ps + (key - pg * ps)) * D + g * KB;
+#pragma unroll
+            for (int c = 0; c < KB / 16; ++c)
+                kw[t][c] = g * KB + c * 16 < D ? *reinterpret_cast<const u4*>(p + c * 16) : u4{0, 0, 0, 0};
+        }
+        // V and both scales: keys kb + 16 t + 4 g + r
+        uint32_t vw[2][4][VB / 4];
+        float ks[2][4], vs[2][4];
+        uint32_t seen = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int j = kb + 16 * t + 4 * g + r, key = min(j, hi - 1), pg = key / ps;
+                int page = a.table[b * a.table_stride + pg];
+                const bool there = (uint32_t)page < (uint32_t)a.c.pages;
+                if (!there) page = 0;
+                const int64_t e = ((int64_t)page * H + h) * ps + (key - pg * ps);
+                ks[t][r] = a.c.k_scale[e];
+                vs[t][r] = a.c.v_scale[e];
+                const int8_t* p = a.c.v + e * D + li * VB;
+                const bool in = li * VB < D;
+#pragma unroll
+                for (int c = 0; c < VB / 4; ++c) vw[t][r][c] = in ? reinterpret_cast<const uint32_t*>(p)[c] : 0;
+                const bool see = there && j < last && j <= pos && (!a.window || j > pos - a.window) && live;
+                seen |= (uint32_t)see << (4 * t + r);
+            }
+
+        v4f s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = v4f{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < STEPS; ++c) {
+                h2 x[4];
+                unpack4(biased(kw[t][c / 2][c % 2 * 2]), x[0], x[1]);
+                unpack4(biased(kw[t][c / 2][c % 2 * 2 + 1]), x[2], x[3]);
+                const h8 k = join(x[0], x[1], x[2], x[3]);
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i][c], s[t], 0, 0, 0);
+            }
+        }
+
+        float top = kMinusInf;
+        uint32_t vtop = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool see = seen >> (4 * t + r) & 1;
+                s[t][r] = see ? s[t][r] * ks[t][r] * fq : kMinusInf;
+                vs[t][r] = see ? vs[t][r] : 0.f;
+                top = fmaxf(top, s[t][r]);
+                vtop = max(vtop, magnitude(vs[t][r]));
+            }
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 16, 64));
+        vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 32, 64));
+        const float mn = fmaxf(m, top), m0 = mn == kMinusInf ? 0.f : mn;
+        const float lift = m0 - kLift;  // weights (and l) are 2^14 times p
+        const int En = max(E, min(exponent(vtop), 126));
+        if (__any(mn > m || En > E)) {
+            const float f = exp2_fast(m - m0), fo = ldexpf(f, E - En);
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < VB; ++t) o[t] *= fo;
+            m = mn;
+            E = En;
+        }
+        f32x8 pv;
+        bool small = false;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float p = exp2_fast(s[t][r] - lift);
+                l += p;
+                pv[4 * t + r] = p * ldexpf(vs[t][r], -E);
+                small |= pv[4 * t + r] != 0.f && pv[4 * t + r] < Levels<TERMS>::least;
+            }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < VB / 4; ++c) vw[t][r][c] = biased(vw[t][r][c]);
+        auto values = [&](int t) {
+            const int c = t / 4, y = t % 4;
+            return join(pair(vw[0][0][c], vw[0][1][c], y), pair(vw[0][2][c], vw[0][3][c], y),
+                        pair(vw[1][0][c], vw[1][1][c], y), pair(vw[1][2][c], vw[1][3][c], y));
+        };
+        h8 w[TERMS];
+        if (!__any(small)) {
+            Levels<TERMS>::terms(pv, w);
+#pragma unroll
+            for (int t = 0; t < VB; ++t) {
+                const h8 v = values(t);
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], o[t], 0, 0, 0);
+            }
+        } else {
+            float down = 1.f;
+            do {
+                small = Levels<TERMS>::take(pv, w);
+#pragma unroll
+                for (int t = 0; t < VB; ++t) {
+                    const h8 v = values(t);
+                    v4f z = {0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < TERMS; ++i) z = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], z, 0, 0, 0);
+                    o[t] += z * down;
+                }
+                down *= 1.f / Levels<TERMS>::step;
+            } while (__any(small));
+        }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    l *= 0x1p-14f;
+
+    // the waves' parts: o[t][r] is value d = (4 g + r) * VB + t of row li
+    __shared__ float red_m[kRowsWaves][16], red_l[kRowsWaves][16], red_o[16][DP + 4];
+    if (g == 0) {
+        red_m[wave][li] = m;
+        red_l[wave][li] = l;
+    }
+    __syncthreads();
+    {
+        float M = kMinusInf;
+#pragma unroll
+        for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][li]);
+        const float f = m == kMinusInf ? 0.f : ldexpf(exp2_fast(m - M), E - 14 + 9);
+#pragma unroll
+        for (int w = 0; w < kRowsWaves; ++w) {
+            if (wave == w) {
+#pragma unroll
+                for (int t = 0; t < VB; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float& to = red_o[li][(4 * g + r) * VB + t];
+                        to = w ? to + o[t][r] * f : o[t][r] * f;
+                    }
+            }
+            __syncthreads();
+        }
+    }
+    for (int t = threadIdx.x; t < 16 * DP; t += kRowsWaves * 64) {
+        const int rr = t / DP, d = t - rr * DP, rw = row0 + rr;
+        if (rw >= rows || d >= D) continue;
+        float M = kMinusInf, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][rr]);
+#pragma unroll
+        for (int w = 0; w < kRowsWaves; ++w) L += red_m[w][rr] == kMinusInf ? red_l[w][rr] : red_l[w][rr] * exp2_fast(red_m[w][rr] - M);
+        const float v = red_o[rr][d];
+        if (sp.count == 1) {
+            store_row<T>(a, u, h, G, rw, d, L == 0.f ? 0.f : v / L);
+        } else {
+            const int64_t part = ((int64_t)unit * ws.rows + rw) * sp.count + split;
+            ws.o[part * D + d] = v;
+            if (d == 0) ws.ml[part] = make_float2(M, L);
+        }
+    }
+}
+
+// The parts of a row, joined: one wave a row.
+template <typename T, int TILE>
+__global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Parts ws) {
+    const int lane = threadIdx.x & 63;
+    const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int unit = (int)(at / ws.rows), row = (int)(at - (int64_t)unit * ws.rows);
+    if (unit >= a.seqs * H) return;
+    const int b = unit / H, h = unit - b * H;
+    const Unit u = unit_of(a, b);
+    const int rows = u.n * G;
+    if (row >= rows) return;
+    const int row0 = row / TILE * TILE;
+    int lo, hi;
+    key_range(a, u, row0 / G, (min(row0 + TILE, rows) - 1) / G, lo, hi);
+    const int count = splits_of(sp, lo, hi);
+    const float2* ml = ws.ml + at * sp.count;
+    const float* o = ws.o + at * sp.count * D;
+    float M = kMinusInf;
+    for (int s = 0; s < count; ++s) M = fmaxf(M, ml[s].x);
+    float L = 0.f, v[4] = {0, 0, 0, 0};
+    for (int s = 0; s < count; ++s) {
+        const float f = ml[s].x == kMinusInf ? 1.f : exp2_fast(ml[s].x - M);
+        L += ml[s].y * f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (lane + 64 * i < D) v[i] += o[(int64_t)s * D + lane + 64 * i] * f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (lane + 64 * i < D) store_row<T>(a, u, h, G, row, lane + 64 * i, L == 0.f ? 0.f : v[i] / L);
+}
+
+// Enough workgroups for the chip from splits of at least 256 keys.
+Split choose_split(const AttnArgs& a, int tile) {
+    const int G = a.q_heads / a.c.kv_heads;
+    const int64_t tiles = ((int64_t)a.max_chunk * G + tile - 1) / tile;
+    const int64_t groups = tiles * a.seqs * a.c.kv_heads;
+    int64_t range = a.max_context;
+    if (a.window) range = std::min<int64_t>(range, (int64_t)a.window + (tile + G - 1) / G + 33);
+    const int64_t want = std::max<int64_t>(1, 4096 / groups);
+    const int64_t keys = std::max<int64_t>(256, (range / want + 127) / 128 * 128);
+    return Split{(int)((range + 31 + keys - 1) / keys), (int)keys};
+}
+
+size_t parts_floats(const AttnArgs& a, const Split& sp, int64_t* o_floats) {
+    const int64_t rows = (int64_t)a.seqs * a.c.kv_heads * a.max_chunk * (a.q_heads / a.c.kv_heads);
+    *o_floats = rows * sp.count * a.c.head_dim;
+    return (size_t)(*o_floats + 4 + rows * sp.count * 2);
+}
+
+template <typename T, int DP, int TERMS>
+hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
+    const Split sp = choose_split(a, 16);
+    const int G = a.q_heads / a.c.kv_heads;
+    int64_t of;
+    parts_floats(a, sp, &of);
+    const Parts p{ws, reinterpret_cast<float2*>(ws + (of + 3) / 4 * 4), a.max_chunk * G};
+    const int64_t blocks = (((int64_t)a.max_chunk * G + 15) / 16) * a.seqs * a.c.kv_heads * sp.count;
+    hipLaunchKernelGGL((attention_rows<T, DP, TERMS>), dim3((unsigned)blocks), dim3(kRowsWaves * 64), 0, st, a, sp, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || sp.count == 1) return e;
+    const int64_t rows = (int64_t)a.seqs * a.c.kv_heads * p.rows;
+    hipLaunchKernelGGL((attention_join<T, 16>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, sp, p);
+    return hipGetLastError();
+}
+
+template <typename T, int TERMS>
+hipError_t by_dim(const AttnArgs& a, float* ws, hipStream_t st) {
+    if (a.c.head_dim <= 64) return launch_d<T, 64, TERMS>(a, ws, st);
+    if (a.c.head_dim <= 128) return launch_d<T, 128, TERMS>(a, ws, st);
+    return launch_d<T, 256, TERMS>(a, ws, st);
+}
+
+}  // namespace
+
+size_t attention_workspace(int, const AttnArgs& a) {
+    const Split sp = choose_split(a, 16);
+    int64_t of;
+    return sp.count == 1 ? 0 : parts_floats(a, sp, &of) * sizeof(float);
+}
+
+hipError_t launch_attention(int dtype, const AttnArgs& a, float* ws, hipStream_t st) {
+    if (dtype == NEO_F32) return by_dim<float, 2>(a, ws, st);
+    if (dtype == NEO_F16) return by_dim<_Float16, 1>(a, ws, st);
+    return by_dim<__bf16, 1>(a, ws, st);
+}
+
+}  // namespace neo

@@ -10,6 +10,7 @@ import ctypes
 import json
 import os
 import re
+from typing import NamedTuple
 
 import numpy as np
 
@@ -62,6 +63,12 @@ class Node(ctypes.Structure):
                 ("bn_eps", ctypes.c_float), ("ic_bn", ctypes.c_int), ("oc_bn", ctypes.c_int)]
 
 
+class KvCacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
 _lib = None
 _RAW_STREAM = False  # set by lib(): torch hands out the current stream's raw handle
 
@@ -81,6 +88,7 @@ def lib():
     import torch  # noqa: F401
     L = ctypes.CDLL(LIB_PATH)
     P, I, F, S = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+    L64, KV = ctypes.c_int64, ctypes.POINTER(KvCacheStruct)
     sig = {
         "neo_conv2d_blocked": [P, I, I, I, I, P, I, I, I, P, I, I, I, I,
                                ctypes.POINTER(Epilogue), P, I, I, P],
@@ -120,6 +128,14 @@ def lib():
         "neo_run_graph": [P, P, P, P],
         "neo_run_step": [P, I, P, P, P],
         "neo_plan_calibrate_int8": [P, P, P, P],
+        "neo_rmsnorm_int8": [P, L64, P, L64, P, F, I, I, I, P, L64, P, L64, P, L64, P, P],
+        "neo_quantize_tokens_int8": [P, L64, P, L64, I, I, I, P, L64, P, P],
+        "neo_dequantize_tokens_int8": [P, L64, P, I, I, I, P, L64, P],
+        "neo_matmul_int8": [P, L64, P, I, I, P, P, I, P, I, I, P, L64, P],
+        "neo_kv_write_int8": [KV, P, L64, L64, P, L64, L64, I, I, P, P],
+        "neo_kv_read_int8": [KV, P, I, I, P, P, P],
+        "neo_attention_paged_int8": [KV, P, L64, L64, I, I, I, P, L64, P, P, I, I, I, F, I, P, L64,
+                                     L64, P],
         "neo_tune_db_save": [ctypes.c_char_p],
         "neo_tune_db_load": [ctypes.c_char_p],
         "neo_tune_db_clear": [],
@@ -457,6 +473,238 @@ def dense_int8(xq, IN, w_rows, w_scale, OUT, x_scale, bias=None, act="none", out
                                 float(x_scale), _dptr(bias, "bias"), ACT[act] if isinstance(act, str) else int(act),
                                 yp, float(y_scale or 0.0), qp, _stream(stream)))
     return (None if out is False else out), out_q
+
+
+# --------------------------------------------------------------------------------------
+# Token operators: the integer path of a transformer layer
+# --------------------------------------------------------------------------------------
+class KVCache(NamedTuple):
+    """A paged int8 cache: k and v int8 [pages][kv_heads][page_size][head_dim],
+    their scales float32 [pages][kv_heads][page_size].  Any tuple of the four
+    tensors in this order serves as well."""
+    k: "torch.Tensor"
+    v: "torch.Tensor"
+    k_scale: "torch.Tensor"
+    v_scale: "torch.Tensor"
+
+
+def kv_cache(pages, kv_heads, page_size, head_dim, device="cuda"):
+    """A new, zeroed cache."""
+    import torch
+    q = [torch.zeros((pages, kv_heads, page_size, head_dim), device=device, dtype=torch.int8) for _ in range(2)]
+    s = [torch.zeros((pages, kv_heads, page_size), device=device, dtype=torch.float32) for _ in range(2)]
+    return KVCache(*q, *s)
+
+
+_DTYPES = {}   # torch dtype -> enum neo_dtype; filled on first use
+
+
+def _dtype(t):
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    code = _DTYPES.get(t)
+    if code is None:
+        raise TypeError(f"{t} is not float32, float16 or bfloat16")
+    return code
+
+
+def _rows(t, name, like=None):
+    """A device tensor [rows][cols] of neighbouring elements: (pointer, row stride)."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device (cuda) tensor")
+    if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
+        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, not {tuple(like.shape)} of {like.dtype}")
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be two-dimensional with neighbouring elements in its rows")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+
+
+def _rows8(t, rows, cols, name):
+    """int8 rows [rows][dense_row_bytes(cols)]: (pointer, row stride)."""
+    import torch
+    if t.dtype != torch.int8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < dense_row_bytes(cols):
+        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, not int8 rows {(rows, dense_row_bytes(cols))}")
+    return _rows(t, name)
+
+
+def _vec(t, n, dtype, name):
+    """A device vector of at least n elements."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{name} must be a device (cuda) tensor of {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() < n:
+        raise ValueError(f"{name} holds {t.numel()} elements, the call needs {n}")
+    return t.data_ptr()
+
+
+def rmsnorm_int8(x, gamma, eps=1e-5, residual=None, h=None, y=None, out=None, scale=None, quantize=True, stream=None):
+    """Residual addition, root-mean-square norm, quantization: (int8 rows
+    [rows][dense_row_bytes(cols)], scales [rows], h).  x [rows][cols] float32,
+    float16 or bfloat16; h = x + residual (allocated when residual is given and
+    h is None; h=residual or h=x works in place; h=False leaves it out).  y,
+    when given, receives the norm unquantized; quantize=False leaves the int8
+    rows out."""
+    import torch
+    rows, cols = x.shape
+    xp, xs = _rows(x, "x")
+    rp, rs = (None, 0) if residual is None else _rows(residual, "residual", x)
+    if h is None and residual is not None:
+        h = torch.empty((rows, cols), device=x.device, dtype=x.dtype)
+    hp, hs = (None, 0) if h is None or h is False else _rows(h, "h", x)
+    yp, ys = (None, 0) if y is None else _rows(y, "y", x)
+    qp, qs, sp = None, 0, None
+    if quantize:
+        if out is None:
+            out = torch.empty((rows, dense_row_bytes(cols)), device=x.device, dtype=torch.int8)
+        if scale is None:
+            scale = torch.empty(rows, device=x.device, dtype=torch.float32)
+        qp, qs = _rows8(out, rows, cols, "out")
+        sp = _vec(scale, rows, torch.float32, "scale")
+    _check(lib().neo_rmsnorm_int8(xp, xs, rp, rs, _vec(gamma, cols, torch.float32, "gamma"), eps, rows, cols,
+                                  _dtype(x.dtype), hp, hs, yp, ys, qp, qs, sp, _stream(stream)))
+    return out, scale, (None if h is False else h)
+
+
+def quantize_tokens_int8(x, gate=None, out=None, scale=None, stream=None):
+    """Rows x [rows][cols], or x * silu(gate), in int8 with a scale each:
+    (int8 rows [rows][dense_row_bytes(cols)], scales [rows])."""
+    import torch
+    rows, cols = x.shape
+    xp, xs = _rows(x, "x")
+    gp, gs = (None, 0) if gate is None else _rows(gate, "gate", x)
+    if out is None:
+        out = torch.empty((rows, dense_row_bytes(cols)), device=x.device, dtype=torch.int8)
+    if scale is None:
+        scale = torch.empty(rows, device=x.device, dtype=torch.float32)
+    qp, qs = _rows8(out, rows, cols, "out")
+    _check(lib().neo_quantize_tokens_int8(xp, xs, gp, gs, rows, cols, _dtype(x.dtype), qp, qs,
+                                          _vec(scale, rows, torch.float32, "scale"), _stream(stream)))
+    return out, scale
+
+
+def dequantize_tokens_int8(xq, x_scale, cols, dtype, out=None, stream=None):
+    """The values [rows][cols] that int8 rows and their scales stand for."""
+    import torch
+    rows = xq.shape[0]
+    qp, qs = _rows8(xq, rows, cols, "xq")
+    if out is None:
+        out = torch.empty((rows, cols), device=xq.device, dtype=dtype)
+    elif out.dtype != dtype or tuple(out.shape) != (rows, cols):
+        raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {(rows, cols)} of {dtype}")
+    yp, ys = _rows(out, "out")
+    _check(lib().neo_dequantize_tokens_int8(qp, qs, _vec(x_scale, rows, torch.float32, "x_scale"), rows, cols,
+                                            _dtype(dtype), yp, ys, _stream(stream)))
+    return out
+
+
+def matmul_int8(xq, x_scale, IN, w_rows, w_scale, OUT, bias=None, act="none", dtype=None, out=None, stream=None):
+    """int8 rows xq [M][dense_row_bytes(IN)] with scales [M] (rmsnorm_int8,
+    quantize_tokens_int8) times int8 weight rows with scales [OUT]
+    (pack_dense_int8): [M][OUT] of dtype (bfloat16 unless said or out given)."""
+    import torch
+    M = xq.shape[0]
+    qp, qs = _rows8(xq, M, IN, "xq")
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else out.dtype
+    if out is None:
+        out = torch.empty((M, OUT), device=xq.device, dtype=dtype)
+    elif out.dtype != dtype or tuple(out.shape) != (M, OUT):
+        raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {(M, OUT)} of {dtype}")
+    yp, ys = _rows(out, "out")
+    f32 = torch.float32
+    _check(lib().neo_matmul_int8(qp, qs, _vec(x_scale, M, f32, "x_scale"), M, IN,
+                                 _vec(w_rows, OUT * dense_row_bytes(IN), torch.int8, "w_rows"),
+                                 _vec(w_scale, OUT, f32, "w_scale"), OUT, _vec(bias, OUT, f32, "bias"),
+                                 ACT[act] if isinstance(act, str) else int(act), _dtype(dtype), yp, ys, _stream(stream)))
+    return out
+
+
+def _cache(cache):
+    """A KVCache (or a tuple of its four tensors) as the C struct."""
+    import torch
+    k, v, ks, vs = cache
+    if k.dim() != 4 or v.shape != k.shape or ks.shape != k.shape[:3] or vs.shape != ks.shape:
+        raise ValueError("a cache is k and v [pages][kv_heads][page_size][head_dim] and their scales [pages][kv_heads][page_size]")
+    P, H, page, D = k.shape
+    return KvCacheStruct(_vec(k, 0, torch.int8, "k"), _vec(v, 0, torch.int8, "v"), _vec(ks, 0, torch.float32, "k_scale"),
+                         _vec(vs, 0, torch.float32, "v_scale"), P, H, page, D)
+
+
+def _heads(t, heads, dim, name):
+    """A device tensor [tokens][heads][dim] of neighbouring dim: (pointer, strides)."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device (cuda) tensor")
+    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not [tokens][{heads or 'q_heads'}][{dim}]")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name} must have neighbouring elements in its heads")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def kv_write_int8(cache, k, v, slots, stream=None):
+    """Quantizes k and v [tokens][kv_heads][head_dim] into the cache entries
+    slots [tokens] (int64: page * page_size + entry; a slot outside the cache,
+    -1 say, skips its token)."""
+    import torch
+    c = _cache(cache)
+    if k.dtype != v.dtype or k.shape != v.shape:
+        raise ValueError("k and v differ in shape or type")
+    T = k.shape[0]
+    _check(lib().neo_kv_write_int8(ctypes.byref(c), *_heads(k, c.kv_heads, c.head_dim, "k"),
+                                   *_heads(v, c.kv_heads, c.head_dim, "v"), T, _dtype(k.dtype),
+                                   _vec(slots, T, torch.int64, "slots"), _stream(stream)))
+
+
+def kv_read_int8(cache, slots, dtype, k_out=None, v_out=None, stream=None):
+    """Keys and values [tokens][kv_heads][head_dim] of the entries slots."""
+    import torch
+    c = _cache(cache)
+    T = slots.numel()
+    shape = (T, c.kv_heads, c.head_dim)
+    outs = []
+    for o in (k_out, v_out):
+        if o is None:
+            o = torch.empty(shape, device=slots.device, dtype=dtype)
+        elif o.dtype != dtype or tuple(o.shape) != shape:
+            raise ValueError(f"an output is {tuple(o.shape)} of {o.dtype}, not {shape} of {dtype}")
+        outs.append(o)
+    _check(lib().neo_kv_read_int8(ctypes.byref(c), _vec(slots, T, torch.int64, "slots"), T, _dtype(dtype),
+                                  _vec(outs[0], 0, dtype, "k_out"), _vec(outs[1], 0, dtype, "v_out"), _stream(stream)))
+    return tuple(outs)
+
+
+def attention_paged_int8(cache, q, page_table, context_lens, q_starts, max_chunk, max_context, scale=None, window=0,
+                         out=None, stream=None):
+    """Causal attention of each sequence's newest tokens over its paged cache:
+    q [tokens][q_heads][head_dim], page_table int32 [seqs][pages of a sequence],
+    context_lens int32 [seqs], q_starts int32 [seqs + 1]; max_chunk and
+    max_context bound the sequences' new and cached tokens.  scale:
+    1 / sqrt(head_dim) unless given; window > 0: each token sees that many."""
+    import torch
+    c = _cache(cache)
+    qp, qt, qh = _heads(q, None, c.head_dim, "q")
+    T, Hq, D = q.shape
+    if page_table.dim() != 2 or page_table.dtype != torch.int32 or not page_table.is_cuda or \
+            (page_table.stride(1) != 1 and page_table.shape[1] > 1):
+        raise ValueError("page_table must be a device int32 [seqs][pages]")
+    B, most = page_table.shape
+    if max_context > most * c.page_size:
+        raise ValueError(f"max_context {max_context} exceeds the {most} pages a sequence has")
+    if out is None:
+        out = torch.empty((T, Hq, D), device=q.device, dtype=q.dtype)
+    elif out.dtype != q.dtype or out.shape != q.shape:
+        raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {tuple(q.shape)} of {q.dtype}")
+    op, ot, oh = _heads(out, Hq, D, "out")
+    i32 = torch.int32
+    _check(lib().neo_attention_paged_int8(ctypes.byref(c), qp, qt, qh, T, Hq, _dtype(q.dtype), page_table.data_ptr(),
+                                          page_table.stride(0) if B > 1 else most, _vec(context_lens, B, i32, "context_lens"),
+                                          _vec(q_starts, B + 1, i32, "q_starts"), B, max_chunk, max_context,
+                                          D ** -0.5 if scale is None else scale, window, op, ot, oh, _stream(stream)))
+    return out
 
 
 def _int8_args(xq, C, w_packed, K, R, S, stride, pad):

@@ -1,0 +1,661 @@
+"""The token operators (neo_rmsnorm_int8, neo_quantize_tokens_int8,
+neo_dequantize_tokens_int8, neo_matmul_int8, neo_kv_write_int8,
+neo_kv_read_int8, neo_attention_paged_int8): refusals on the host; on the GPU
+against plain implementations in 64 bits.
+
+Tolerances, all derived from the formats (u = 2^-24 for float32, 2^-11 for
+float16, 2^-8 for bfloat16, half a unit in the last place relative):
+
+* quantization and dequantization: the interface fixes every rounding, so rows
+  of float32, float16 and bfloat16 are bit-exact against the same float32
+  operations in numpy; so is the product's float32 output;
+* the norm: a lane adds at most cols / 64 squares before six or ten tree
+  additions, so the sum of squares is within (cols / 64 + 16) u, the norm
+  within half of that plus four roundings; an int8 value times its scale lies
+  within half a step of the norm, and a step's worth of those errors;
+* attention: with A = sum_j p_ij |v_j| / sum_j p_ij and B = max_j scale sum_d
+  |q_id k_jd|, the scores are within (head_dim + 8) u B (float32 sums of
+  head_dim products in any order, two float32 terms of the query dropped below
+  2^-22), so the weights within twice that plus their rounding (2^-11; two
+  terms 2^-21) and that of the exponential and of the sums (64 u and u per
+  key of the longest chain, keys / 32), all relative to A; plus the output's rounding.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from paper_1809_02697_amd import neo
+
+from gpu_util import torch_cuda
+
+FAKE = ctypes.c_void_p(1 << 20)   # aligned, never dereferenced: validation fails first
+ODD = ctypes.c_void_p((1 << 20) + 1)
+MIS = ctypes.c_void_p((1 << 20) + 8)
+F32, F16, BF16 = 0, 1, 2
+U = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
+TINY = {"float32": 2.0 ** -149, "float16": 2.0 ** -25, "bfloat16": 2.0 ** -134}
+
+
+# ---- refusals (host) -------------------------------------------------------------------
+
+def _norm(x=FAKE, xs=64, r=None, rs=0, gamma=FAKE, eps=1e-5, rows=2, cols=64, dtype=BF16, h=None, hs=0, y=None, ys=0,
+          q=FAKE, qs=64, s=FAKE):
+    return neo.lib().neo_rmsnorm_int8(x, xs, r, rs, gamma, eps, rows, cols, dtype, h, hs, y, ys, q, qs, s, None)
+
+
+def test_norm_refusals():
+    assert _norm(x=None) == -1 and "neo_rmsnorm_int8: x" in neo.last_error()
+    assert _norm(rows=-1) == -1 and _norm(cols=0) == -1 and _norm(dtype=3) == -1 and _norm(dtype=-1) == -1
+    assert _norm(x=ODD) == -3 and _norm(r=ODD, rs=64) == -3 and _norm(h=ODD, hs=64) == -3 and _norm(y=ODD, ys=64) == -3
+    assert _norm(xs=63) == -2 and _norm(r=FAKE, rs=63) == -2 and _norm(h=FAKE, hs=63) == -2 and _norm(y=FAKE, ys=0) == -2
+    assert _norm(q=MIS) == -3 and _norm(qs=72) == -3 and _norm(qs=48) == -2
+    assert _norm(s=None) == -1 and _norm(q=None) == -1
+    assert _norm(q=None, s=None) == -1 and "none of" in neo.last_error()
+    for eps in (-1e-5, float("nan"), float("inf")):
+        assert _norm(eps=eps) == -1
+    assert _norm(cols=65537, xs=65537, qs=65552) == -4
+    assert _norm(h=FAKE, hs=80) == -2 and "stride" in neo.last_error()   # in place of x with another stride
+    assert _norm(rows=0, x=None, q=None, s=None) == 0                    # no tokens: nothing to do
+
+
+def test_quantize_refusals():
+    def call(x=FAKE, xs=64, g=None, gs=0, rows=2, cols=64, dtype=F32, q=FAKE, qs=64, s=FAKE):
+        return neo.lib().neo_quantize_tokens_int8(x, xs, g, gs, rows, cols, dtype, q, qs, s, None)
+    assert call(x=None) == -1 and "neo_quantize_tokens_int8" in neo.last_error()
+    assert call(q=None) == -1 and call(s=None) == -1 and call(cols=0) == -1 and call(rows=-1) == -1 and call(dtype=7) == -1
+    assert call(x=ODD) == -3 and call(g=ODD, gs=64) == -3 and call(q=MIS) == -3 and call(s=ODD) == -3 and call(qs=65) == -3
+    assert call(xs=10) == -2 and call(g=FAKE, gs=10) == -2 and call(cols=65, xs=65, qs=64) == -2
+    assert call(cols=70000, xs=70000, qs=70000) == -4
+    assert call(rows=0, x=None) == 0
+
+    def back(q=FAKE, qs=64, s=FAKE, rows=2, cols=64, dtype=F32, y=FAKE, ys=64):
+        return neo.lib().neo_dequantize_tokens_int8(q, qs, s, rows, cols, dtype, y, ys, None)
+    assert back(q=None) == -1 and back(s=None) == -1 and back(y=None) == -1 and back(dtype=3) == -1
+    assert back(q=MIS) == -3 and back(y=ODD) == -3 and back(qs=40) == -2 and back(ys=63) == -2
+    assert back(rows=0, q=None) == 0
+
+
+def test_matmul_refusals():
+    def call(x=FAKE, xs=64, xsc=FAKE, M=2, K=64, w=FAKE, ws=FAKE, N=32, b=None, act=0, dtype=BF16, y=FAKE, ys=32):
+        return neo.lib().neo_matmul_int8(x, xs, xsc, M, K, w, ws, N, b, act, dtype, y, ys, None)
+    for name in ("x", "xsc", "w", "ws", "y"):
+        assert call(**{name: None}) == -1 and "neo_matmul_int8" in neo.last_error()
+    assert call(M=-1) == -1 and call(K=0) == -1 and call(N=0) == -1 and call(act=5) == -1 and call(dtype=9) == -1
+    assert call(x=MIS) == -3 and call(w=MIS) == -3 and call(y=ODD) == -3 and call(b=ODD) == -3 and call(xs=72) == -3
+    assert call(xs=48) == -2 and call(ys=31) == -2
+    assert call(K=133145, xs=133152) == -4 and "133,144" in neo.last_error()
+    assert call(M=0, x=None) == 0
+
+
+def _struct(**over):
+    f = dict(k=1 << 20, v=1 << 20, k_scale=1 << 20, v_scale=1 << 20, pages=4, kv_heads=2, page_size=16, head_dim=64)
+    f.update(over)
+    return ctypes.byref(neo.KvCacheStruct(**f))
+
+
+BAD_CACHES = [(dict(k=None), -1), (dict(v_scale=None), -1), (dict(pages=0), -1), (dict(kv_heads=0), -1), (dict(page_size=0), -1),
+              (dict(head_dim=0), -1), (dict(head_dim=72), -4), (dict(head_dim=272), -4), (dict(k=(1 << 20) + 8), -3),
+              (dict(v=(1 << 20) + 8), -3), (dict(k_scale=(1 << 20) + 2), -3)]
+
+
+def test_cache_refusals():
+    def write(c=None, k=FAKE, v=FAKE, st=64, T=3, dtype=F16, slots=FAKE):
+        return neo.lib().neo_kv_write_int8(_struct() if c is None else c, k, st, 64, v, st, 64, T, dtype, slots, None)
+
+    def read(c=None, slots=FAKE, T=3, dtype=F16, k=FAKE, v=FAKE):
+        return neo.lib().neo_kv_read_int8(_struct() if c is None else c, slots, T, dtype, k, v, None)
+    for over, code in BAD_CACHES:
+        assert write(_struct(**over)) == code and "neo_kv_write_int8: cache" in neo.last_error(), over
+        assert read(_struct(**over)) == code and "neo_kv_read_int8: cache" in neo.last_error(), over
+    assert neo.lib().neo_kv_read_int8(None, FAKE, 3, F16, FAKE, FAKE, None) == -1
+    assert write(k=None) == -1 and write(v=None) == -1 and write(slots=None) == -1 and write(T=-1) == -1 and write(st=-64) == -1
+    assert write(k=ODD) == -3 and write(slots=ctypes.c_void_p((1 << 20) + 4)) == -3 and write(dtype=4) == -1
+    assert read(slots=None) == -1 and read(k=None, v=None) == -1 and read(k=ODD) == -3 and read(dtype=-2) == -1
+    assert write(T=0, k=None) == 0 and read(T=0, slots=None) == 0
+
+
+def test_attention_refusals():
+    def call(c=None, q=FAKE, qt=256, qh=64, T=3, Hq=4, dtype=F16, table=FAKE, ts=8, ctx=FAKE, st=FAKE, B=2, n=2, most=100,
+             scale=0.125, window=0, out=FAKE, ot=256, oh=64):
+        return neo.lib().neo_attention_paged_int8(_struct() if c is None else c, q, qt, qh, T, Hq, dtype, table, ts, ctx, st, B,
+                                                  n, most, scale, window, out, ot, oh, None)
+    for over, code in BAD_CACHES:
+        assert call(_struct(**over)) == code and "neo_attention_paged_int8: cache" in neo.last_error(), over
+    for name in ("q", "table", "ctx", "st", "out"):
+        assert call(**{name: None}) == -1, name
+    for name in ("q", "out", "table", "ctx", "st"):
+        assert call(**{name: ODD}) == -3, name
+    assert call(T=-1) == -1 and call(Hq=0) == -1 and call(B=-1) == -1 and call(n=-1) == -1 and call(most=-1) == -1 and call(window=-1) == -1
+    assert call(Hq=3) == -2 and call(qt=-1) == -1 and call(oh=63) == -2 and call(ot=1) == -2
+    assert call(most=129) == -2 and "table_stride" in neo.last_error()      # 8 pages of 16 tokens
+    for s in (0.0, -1.0, float("nan"), float("inf")):
+        assert call(scale=s) == -1
+    assert call(T=1 << 29, n=1 << 29) == -4
+    assert call(T=0, q=None) == 0 and call(B=0, q=None) == 0 and call(n=0, q=None) == 0
+
+
+# ---- GPU ---------------------------------------------------------------------------------
+
+gpu = pytest.mark.gpu
+TYPES = ["float32", "float16", "bfloat16"]
+
+
+@pytest.fixture(scope="module")
+def torch():
+    t = torch_cuda()
+    neo.lib()
+    return t
+
+
+def _np(t, kind=np.float64):
+    import torch
+    torch.cuda.synchronize()
+    return t.detach().cpu().to(torch.float64 if kind == np.float64 else torch.float32).numpy()
+
+
+def _rand(torch, shape, dtype, seed, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * spread).to(getattr(torch, dtype))
+
+
+def _quantized(x):
+    """Rows of float32 values: int8 values and scales, as the interface fixes them."""
+    x = x.astype(np.float32)
+    top = np.abs(x).max(-1)
+    s = np.where(top == 0, np.float32(1), np.maximum(top / np.float32(127), np.float32(2.0 ** -126)))
+    return np.clip(np.rint(x / s[..., None]), -127, 127).astype(np.int8), s
+
+
+def _step_check(q, s, y, slack):
+    """int8 rows and scales against 64-bit values: the scale is that of the
+    largest, each value within half a step."""
+    top = np.abs(y).max(-1)
+    s = s.astype(np.float64)
+    assert (np.abs(s - np.where(top == 0, 1, top / 127)) <= (slack + 2 * U["float32"]) * np.where(top == 0, 1, top / 127)).all()
+    assert (np.abs(q * s[:, None] - y) <= s[:, None] * 0.5 * (1 + 2e-6) + (slack + 4 * U["float32"]) * (np.abs(y) + top[:, None])).all()
+
+
+NORMS = [(1, 1), (3, 7), (2, 16), (5, 64), (1, 513), (130, 511), (9, 2048), (3, 2049), (2, 4096), (1, 4097), (4, 8191),
+         (2, 16384), (1, 16385), (2, 40000), (1, 65536)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", NORMS)
+def test_norm(torch, rows, cols, dtype):
+    x, r = _rand(torch, (rows, cols), dtype, 1), _rand(torch, (rows, cols), dtype, 2, 3.0)
+    gamma = torch.rand(cols, generator=torch.Generator().manual_seed(3)) + 0.5
+    h64 = (x.float() + r.float()).numpy().astype(np.float64)   # the float32 sum is part of the definition
+    y64 = h64 / np.sqrt((h64 ** 2).mean(1, keepdims=True) + 1e-5) * gamma.numpy().astype(np.float64)
+    slack = (cols / 64 + 16) * U["float32"] / 2 + 4 * U["float32"]
+    y = torch.full((rows, cols), float("nan"), dtype=x.dtype, device="cuda")
+    q, s, h = neo.rmsnorm_int8(x.cuda(), gamma.cuda(), 1e-5, residual=r.cuda(), y=y)
+    assert torch.equal(h.cpu(), (x.float() + r.float()).to(x.dtype))
+    assert (np.abs(_np(y) - y64) <= (slack + U[dtype] * (1 + slack)) * np.abs(y64) + TINY[dtype]).all()
+    q, s = q.cpu().numpy().astype(np.float64), _np(s)
+    assert q.shape[1] == -(-cols // 16) * 16 and not q[:, cols:].any()
+    _step_check(q[:, :cols], s, y64, slack)
+    # without a residual, gamma or int8 output
+    out = neo.rmsnorm_int8(x.cuda(), None, 1e-5, y=y, quantize=False)
+    assert out == (None, None, None)
+    x64 = x.double().numpy()
+    ref = x64 / np.sqrt((x64 ** 2).mean(1, keepdims=True) + 1e-5)
+    assert (np.abs(_np(y) - ref) <= (slack + U[dtype] * (1 + slack)) * np.abs(ref) + TINY[dtype]).all()
+
+
+@gpu
+@pytest.mark.parametrize("place", ["residual", "x"])
+def test_norm_in_place_and_strides(torch, place):
+    """Rows that are slices of wider buffers, h in place of an input, guarded borders."""
+    rows, cols = 5, 301
+    wide = [torch.full((rows, cols + 9), 77.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    x, r = (w[:, 3:3 + cols] for w in wide)
+    x.copy_(_rand(torch, (rows, cols), "bfloat16", 5)); r.copy_(_rand(torch, (rows, cols), "bfloat16", 6))
+    gamma = torch.ones(cols, device="cuda")
+    q0, s0, h0 = neo.rmsnorm_int8(x, gamma, residual=r)
+    out = torch.full((rows, 400), 99, dtype=torch.int8, device="cuda")
+    kept = [w.clone() for w in wide]
+    q1, s1, h1 = neo.rmsnorm_int8(x, gamma, residual=r, h=r if place == "residual" else x, out=out)
+    assert torch.equal(q0, q1[:, :304]) and torch.equal(s0, s1) and torch.equal(h0, h1)
+    assert (out[:, 304:] == 99).all()
+    for w, k, name in zip(wide, kept, ("x", "residual")):
+        k[:, 3:3 + cols] = h0 if name == place else k[:, 3:3 + cols]
+        assert torch.equal(w, k)
+
+
+@gpu
+def test_norm_extremes(torch):
+    """Squares past float32's range, tiny rows, zero rows, eps 0, infinities and NaN."""
+    x = torch.ones(6, 40)
+    x[0] *= 3e30
+    x[1] = 0
+    x[2, 7] = float("inf")
+    x[3, 9] = float("nan")
+    x[4] *= 1e-30
+    y = torch.empty(6, 40, device="cuda")
+    q, s, _ = neo.rmsnorm_int8(x.cuda(), None, 1e-5, y=y)
+    q, s, y = q.cpu().numpy()[:, :40], s.cpu().numpy(), y.cpu().numpy()
+    assert np.allclose(y[0], 1, rtol=1e-6) and (q[0] == 127).all() and np.isclose(s[0], 1 / 127)
+    assert (y[1] == 0).all() and (q[1] == 0).all() and s[1] == 1
+    for i in (2, 3):
+        assert np.isnan(s[i]) and (q[i] == 0).all()
+    assert np.allclose(y[4], 1e-30 / math.sqrt(1e-5), rtol=1e-6)
+    assert np.allclose(y[5], 1 / math.sqrt(1 + 1e-5), rtol=1e-6)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (4, 15), (7, 16), (3, 100), (2, 2049), (600, 33), (2, 11000), (1, 65535)])
+def test_quantize_tokens(torch, rows, cols, dtype):
+    x = _rand(torch, (rows, cols), dtype, 11, 2.0)
+    x[0, 0] = 0
+    if rows > 2:
+        x[1] = 0
+    q, s = neo.quantize_tokens_int8(x.cuda())
+    qr, sr = _quantized(x.float().numpy())
+    assert np.array_equal(s.cpu().numpy(), sr)
+    got = q.cpu().numpy()
+    assert np.array_equal(got[:, :cols], qr) and not got[:, cols:].any()
+    back = neo.dequantize_tokens_int8(q, s, cols, x.dtype)
+    assert torch.equal(back.cpu(), torch.from_numpy(qr.astype(np.float32) * sr[:, None]).to(x.dtype))
+    # gated: the halves of one buffer
+    both = torch.cat([_rand(torch, (rows, cols), dtype, 12, 3.0), x], 1).cuda()
+    q, s = neo.quantize_tokens_int8(both[:, cols:], gate=both[:, :cols])
+    g64 = both[:, :cols].cpu().double().numpy()
+    y64 = x.double().numpy() * g64 / (1 + np.exp(-g64))
+    # expf 2 u, the sum, the division and the product one each
+    _step_check(q.cpu().numpy()[:, :cols].astype(np.float64), _np(s), y64, 6 * U["float32"])
+
+
+@gpu
+def test_quantize_extremes(torch):
+    x = torch.zeros(6, 20)
+    x[0, 3] = float("inf"); x[0, 4] = 1
+    x[1, 5] = float("nan")
+    x[2] = 1e-42
+    x[3] = 3.4e38
+    x[4, 0], x[4, 1] = -5.0, 2.5      # an exact tie: 63.5 rounds to 64
+    q, s = neo.quantize_tokens_int8(x.cuda())
+    q, s = q.cpu().numpy(), s.cpu().numpy()
+    assert np.isnan(s[:2]).all() and (q[:2] == 0).all()
+    qr, sr = _quantized(x[2:].numpy())
+    assert np.array_equal(s[2:], sr) and np.array_equal(q[2:, :20], qr)
+    assert q[4, 0] == -127 and q[4, 1] == 64
+    # a gate of minus a large number closes: silu(-200) is -0
+    q, s = neo.quantize_tokens_int8(torch.ones(1, 20, device="cuda"), gate=torch.full((1, 20), -200.0, device="cuda"))
+    assert (q == 0).all() and s.item() == 1
+    # a row with an infinity is NaN where it is read
+    q, s = neo.quantize_tokens_int8(x.cuda())
+    assert torch.isnan(neo.dequantize_tokens_int8(q, s, 20, torch.float16)[:2]).all()
+
+
+def _product(xq, xs, wq, ws, bias, relu):
+    acc = xq.astype(np.int64) @ wq.astype(np.int64).T
+    v = acc.astype(np.float32) * xs[:, None] * ws[None]
+    v = v.astype(np.float32)
+    if bias is not None:
+        v = v + bias
+    return np.maximum(v, np.float32(0)) if relu else v
+
+
+MATMULS = [(1, 1, 1), (1, 64, 16), (1, 4096, 100), (2, 130, 17), (15, 512, 33), (16, 1000, 64), (17, 96, 80), (33, 257, 129),
+           (64, 128, 64), (65, 640, 200), (100, 2049, 65), (127, 48, 256), (129, 1024, 129), (200, 144, 520), (257, 384, 300),
+           (512, 272, 511), (1030, 160, 260), (7, 16384, 40), (300, 9000, 70)]
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N", MATMULS)
+def test_matmul(torch, M, K, N):
+    rng = np.random.default_rng([M, K, N])
+    Kp = -(-K // 16) * 16
+    xq, wq = np.zeros((M, Kp), np.int8), np.zeros((N, Kp), np.int8)
+    xq[:, :K], wq[:, :K] = rng.integers(-127, 128, (M, K)), rng.integers(-127, 128, (N, K))
+    xq[0, :K], wq[0, :K] = 127, -127        # the largest sums
+    xs, ws = rng.uniform(0.01, 0.1, M).astype(np.float32), rng.uniform(0.001, 0.1, N).astype(np.float32)
+    b = rng.normal(size=N).astype(np.float32)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    for bias, act in ((None, "none"), (b, "relu")):
+        ref = _product(xq, xs, wq, ws, bias, act == "relu")
+        for dtype in (torch.float32, torch.float16, torch.bfloat16):
+            y = neo.matmul_int8(c(xq), c(xs), K, c(wq), c(ws), N, bias=None if bias is None else c(bias), act=act, dtype=dtype)
+            assert torch.equal(y.cpu(), torch.from_numpy(ref).to(dtype)), (act, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N", [(3, 100, 50), (150, 300, 270)])
+def test_matmul_strides(torch, M, K, N):
+    """Rows of a wider buffer in, a column slice of a wider buffer out; what lies beside it stays."""
+    rng = np.random.default_rng(3)
+    Kp = -(-K // 16) * 16
+    xq, wq = np.zeros((M, Kp), np.int8), np.zeros((N, Kp), np.int8)
+    xq[:, :K], wq[:, :K] = rng.integers(-127, 128, (M, K)), rng.integers(-127, 128, (N, K))
+    xs, ws = rng.uniform(0.01, 0.1, M).astype(np.float32), rng.uniform(0.001, 0.1, N).astype(np.float32)
+    wide = torch.full((M, Kp + 48), 55, dtype=torch.int8, device="cuda")
+    wide[:, 16:16 + Kp] = torch.from_numpy(xq).cuda()
+    out = torch.full((M, N + 7), 9.0, dtype=torch.float16, device="cuda")
+    y = neo.matmul_int8(wide[:, 16:16 + Kp], torch.from_numpy(xs).cuda(), K, torch.from_numpy(wq).cuda(), torch.from_numpy(ws).cuda(), N,
+                        out=out[:, 3:3 + N])
+    assert torch.equal(y.cpu(), torch.from_numpy(_product(xq, xs, wq, ws, None, False)).half())
+    assert (out[:, :3] == 9).all() and (out[:, 3 + N:] == 9).all()
+
+
+@gpu
+def test_matmul_of_a_bad_row(torch):
+    """A token with a NaN scale is NaN, its neighbours are not."""
+    q, s = neo.quantize_tokens_int8(torch.tensor([[1.0, 2.0], [float("inf"), 1.0], [3.0, 4.0]], device="cuda"))
+    w, ws = neo.pack_dense_int8(torch.eye(2, device="cuda"))
+    y = neo.matmul_int8(q, s, 2, w, ws, 2, dtype=torch.float32)
+    assert torch.isnan(y[1]).all() and torch.isfinite(y[[0, 2]]).all()
+
+
+CACHES = [(1, 16, 1, 1), (2, 64, 16, 5), (3, 80, 10, 40), (8, 128, 64, 33), (4, 256, 7, 100), (1, 240, 128, 300)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,D,page,tokens", CACHES)
+def test_cache_write_and_read(torch, H, D, page, tokens, dtype):
+    pages = -(-tokens // page) + 3
+    cache = neo.kv_cache(pages, H, page, D)
+    for t in cache:
+        t.fill_(3)
+    before = [t.clone() for t in cache]
+    qkv = _rand(torch, (tokens, 3 * H * D), dtype, 21).cuda()
+    k, v = qkv[:, :H * D].view(tokens, H, D), qkv[:, 2 * H * D:].view(tokens, H, D)
+    slots = torch.randperm(pages * page, generator=torch.Generator().manual_seed(1))[:tokens]
+    if tokens > 2:
+        slots[1], slots[2] = -1, pages * page      # skipped
+    neo.kv_write_int8(cache, k, v, slots.cuda())
+    good = [i for i in range(tokens) if 0 <= slots[i] < pages * page]
+    p, o = slots[good] // page, slots[good] % page
+    for c, s, c0, s0, x in ((cache.k, cache.k_scale, before[0], before[2], k), (cache.v, cache.v_scale, before[1], before[3], v)):
+        qr, sr = _quantized(x.float().cpu().numpy())
+        c0, s0 = c0.cpu(), s0.cpu()
+        c0[p, :, o], s0[p, :, o] = torch.from_numpy(qr[good]), torch.from_numpy(sr[good])
+        assert torch.equal(c.cpu(), c0) and torch.equal(s.cpu(), s0)
+    ko, vo = neo.kv_read_int8(cache, slots.cuda(), k.dtype)
+    for out, x in ((ko, k), (vo, v)):
+        qr, sr = _quantized(x.float().cpu().numpy())
+        ref = torch.from_numpy(qr.astype(np.float32) * sr[..., None]).to(k.dtype)
+        bad = [i for i in range(tokens) if i not in good]
+        ref[bad] = 0
+        assert torch.equal(out.cpu(), ref)
+
+
+@gpu
+def test_cache_bad_values(torch):
+    cache = neo.kv_cache(2, 2, 4, 16)
+    k = torch.ones(1, 2, 16, device="cuda")
+    v = k.clone()
+    k[0, 0, 3], v[0, 1, 5] = float("nan"), float("-inf")
+    neo.kv_write_int8(cache, k, v, torch.tensor([5], device="cuda"))
+    assert torch.isnan(cache.k_scale[1, 0, 1]) and torch.isnan(cache.v_scale[1, 1, 1])
+    assert torch.isfinite(cache.k_scale[1, 1, 1]) and torch.isfinite(cache.v_scale[1, 0, 1])
+    ko, vo = neo.kv_read_int8(cache, torch.tensor([5, 4], device="cuda"), torch.float32)
+    assert torch.isnan(ko[0, 0]).all() and (ko[0, 1] == 1).all() and torch.isnan(vo[0, 1]).all() and (ko[1] == 0).all()
+
+
+# ---- attention -----------------------------------------------------------------------------
+
+def _paged(torch, contexts, H, D, page, seed, spare=2):
+    """A cache whose unused entries hold NaN scales and extreme bytes, and a page table
+    whose unused entries lie outside the cache."""
+    rng = np.random.default_rng(seed)
+    need = [-(-c // page) for c in contexts]
+    P = sum(need) + spare
+    order = rng.permutation(P)
+    table = np.full((len(contexts), max(need) + 1), 1 << 30, np.int32)
+    k, v = (rng.normal(size=(P, H, page, D)) * 40 for _ in "kv")
+    k, v = (np.clip(np.rint(x), -127, 127).astype(np.int8) for x in (k, v))
+    ks, vs = (rng.uniform(0.005, 0.05, (P, H, page)).astype(np.float32) for _ in "kv")
+    used = np.zeros((P, page), bool)
+    at = 0
+    for b, (n, c) in enumerate(zip(need, contexts)):
+        table[b, :n] = order[at:at + n]
+        for j in range(n):
+            used[order[at + j], :min(page, c - j * page)] = True
+        at += n
+    for s, x in ((ks, k), (vs, v)):
+        s.transpose(0, 2, 1)[~used] = np.nan
+        x.transpose(0, 2, 1, 3)[~used] = -128
+    return k, v, ks, vs, table
+
+
+def _attention64(q, k, v, ks, vs, table, contexts, starts, scale, window):
+    """Outputs and the two magnitudes A and B of the tolerance."""
+    T, Hq, D = q.shape
+    H, page = k.shape[1], k.shape[2]
+    G = Hq // H
+    out, A, B = np.zeros((T, Hq, D)), np.zeros((T, Hq, D)), np.zeros((T, Hq, 1))
+    for b, c in enumerate(contexts):
+        n = starts[b + 1] - starts[b]
+        j = np.arange(c)
+        pages = table[b, j // page]
+        for h in range(Hq):
+            with np.errstate(over="ignore"):
+                kk = k[pages, h // G, j % page].astype(np.float64) * ks[pages, h // G, j % page][:, None]
+                vv = v[pages, h // G, j % page].astype(np.float64) * vs[pages, h // G, j % page][:, None]
+            for i in range(n):
+                p = c - n + i
+                lo = max(0, p + 1 - window) if window else 0
+                if p < 0:
+                    continue
+                row = q[starts[b] + i, h].astype(np.float64)
+                s = kk[lo:p + 1] @ row * scale
+                w = np.exp(s - s.max())
+                out[starts[b] + i, h] = w @ vv[lo:p + 1] / w.sum()
+                A[starts[b] + i, h] = w @ np.abs(vv[lo:p + 1]) / w.sum()
+                B[starts[b] + i, h] = (np.abs(kk[lo:p + 1]) @ np.abs(row)).max() * scale
+    return out, A, B
+
+
+def _attention_bound(out, A, B, D, longest, dtype):
+    u = U["float32"]
+    weights = (2.0 ** -21 if dtype == "float32" else 2.0 ** -11) + 2 * (D + 8) * u * B + (64 + longest / 32) * u
+    return U[dtype] * np.abs(out) + weights * A * (1 + U[dtype]) + TINY[dtype]
+
+
+def _attend(torch, dtype, chunks, contexts, Hq, H, D, page, window=0, seed=0, scale=None, spread=1.0):
+    k, v, ks, vs, table = _paged(torch, contexts, H, D, page, seed)
+    starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+    q = _rand(torch, (int(starts[-1]), Hq, D), dtype, seed + 1, spread)
+    scale = D ** -0.5 if scale is None else scale
+    ref, A, B = _attention64(q.double().numpy(), k, v, ks, vs, table, contexts, starts, scale, window)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    got = neo.attention_paged_int8((c(k), c(v), c(ks), c(vs)), q.cuda(), c(table), c(np.array(contexts, np.int32)), c(starts),
+                                   max(chunks), max(contexts), scale=scale, window=window)
+    err, bound = np.abs(_np(got) - ref), _attention_bound(ref, A, B, D, max(contexts), dtype)
+    assert np.isfinite(_np(got)).all()
+    assert (err <= bound).all(), f"{(err > bound).sum()} of {err.size} beyond the bound, worst {(err / bound).max():.2f} times"
+    return got
+
+
+ATTN = [  # chunks, contexts, q heads, kv heads, head dim, page size, window
+    ([1], [1], 1, 1, 16, 1, 0),
+    ([1], [33], 4, 1, 64, 16, 0),
+    ([1, 1, 1], [700, 5, 64], 8, 2, 128, 64, 0),
+    ([1], [1500], 16, 1, 80, 10, 0),
+    ([1, 1], [300, 1111], 24, 1, 256, 16, 0),
+    ([1], [3000], 32, 4, 128, 128, 500),
+    ([3, 0, 7], [3, 0, 130], 6, 2, 64, 7, 0),
+    ([5, 2], [40, 2], 3, 3, 96, 10, 3),
+    ([17], [17], 5, 1, 128, 16, 0),
+    ([40, 1, 9], [90, 400, 9], 8, 2, 128, 32, 0),
+    ([64], [640], 4, 4, 64, 64, 100),
+    ([130], [130], 2, 1, 240, 48, 0),
+    ([200, 70], [333, 70], 4, 2, 128, 16, 65),
+    ([300], [2100], 2, 2, 64, 128, 0),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(ATTN)))
+def test_attention(torch, case, dtype):
+    chunks, contexts, Hq, H, D, page, window = ATTN[case]
+    _attend(torch, dtype, chunks, contexts, Hq, H, D, page, window, seed=case)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("spread", [1e-4, 30.0])
+def test_attention_flat_and_sharp(torch, dtype, spread):
+    """Nearly uniform weights, and rows that one key dominates."""
+    _attend(torch, dtype, [1, 33], [2000, 500], 4, 2, 64, 16, seed=50, spread=spread)
+
+
+@gpu
+@pytest.mark.parametrize("chunk", [5, 40])
+def test_attention_rows_that_see_nothing(torch, chunk):
+    """More new tokens than cached ones (the first see nothing), no context at all, pages outside the cache."""
+    H, D, page = 2, 64, 16
+    k, v, ks, vs, table = _paged(torch, [20, 0, 64], H, D, page, 7)
+    table[2, :] = -1                        # a sequence whose pages do not exist
+    starts = np.array([0, chunk, 2 * chunk, 3 * chunk], np.int32)
+    contexts = [3, 0, 64]
+    q = _rand(torch, (3 * chunk, 4, D), "float16", 8)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    got = _np(neo.attention_paged_int8((c(k), c(v), c(ks), c(vs)), q.cuda(), c(table), c(np.array(contexts, np.int32)), c(starts),
+                                       chunk, 64, scale=0.125))
+    ref, A, B = _attention64(q[:chunk].double().numpy(), k, v, ks, vs, table, [3], starts, 0.125, 0)
+    assert (got[:chunk - 3] == 0).all() and (got[chunk:] == 0).all()
+    assert (np.abs(got[:chunk] - ref) <= _attention_bound(ref, A, B, D, 64, "float16")).all()
+
+
+@gpu
+@pytest.mark.parametrize("chunk", [2, 33])
+def test_attention_bad_entries_reach_only_who_sees_them(torch, chunk):
+    """A NaN key, an infinite and a huge value scale at the last token: earlier
+    queries of the chunk keep their bits."""
+    H, D, page, ctx = 1, 64, 16, 70
+    k, v, ks, vs, table = _paged(torch, [ctx], H, D, page, 9)
+    starts = np.array([0, chunk], np.int32)
+    q = _rand(torch, (chunk, 2, D), "bfloat16", 10).cuda()
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    run = lambda: neo.attention_paged_int8((c(k), c(v), c(ks), c(vs)), q, c(table), c(np.array([ctx], np.int32)), c(starts), chunk, ctx)  # noqa: E731
+    good = run()
+    at = table[0, (ctx - 1) // page], 0, (ctx - 1) % page
+    for s, bad in ((ks, np.nan), (vs, np.nan), (vs, np.inf), (vs, np.float32(1e30))):
+        was = s[at]
+        s[at] = bad
+        got = run()
+        s[at] = was
+        assert torch.equal(got[:-1], good[:-1])
+        if not np.isfinite(bad):
+            assert torch.isnan(got[-1]).any() or torch.isinf(got[-1]).any()
+
+
+@gpu
+def test_attention_bad_query(torch):
+    """An infinity or a NaN in a query makes that head's row NaN and no other."""
+    k, v, ks, vs, table = _paged(torch, [50], 1, 64, 16, 12)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    for chunk in (3, 40):
+        q = _rand(torch, (chunk, 2, 64), "float32", 13)
+        q[1, 0, 5], q[2, 1, 60] = float("inf"), float("nan")
+        got = neo.attention_paged_int8((c(k), c(v), c(ks), c(vs)), q.cuda(), c(table), c(np.array([50], np.int32)),
+                                       c(np.array([0, chunk], np.int32)), chunk, 50).cpu()
+        bad = torch.zeros(chunk, 2, dtype=torch.bool)
+        bad[1, 0] = bad[2, 1] = True
+        assert torch.isnan(got[bad]).all() and torch.isfinite(got[~bad]).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_scales_of_any_magnitude(torch, dtype):
+    """Value scales from 1e-30 to 1e30 and queries near the format's ends: the
+    result follows the scales (float32 range permitting)."""
+    big = {"float32": 1e20, "float16": 1e4, "bfloat16": 1e20}[dtype]
+    for chunk in (1, 40):
+        for vscale, qscale in ((1e-30, 1.0), (1e30 if dtype != "float16" else 100.0, 1.0), (1.0, big), (1.0, 1 / big)):
+            k, v, ks, vs, table = _paged(torch, [100], 1, 64, 16, 14)
+            vs *= np.float32(vscale)
+            q = (_rand(torch, (chunk, 2, 64), "float32", 15) * qscale).to(getattr(torch, dtype))
+            starts = np.array([0, chunk], np.int32)
+            scale = 0.125 / qscale
+            ref, A, B = _attention64(q.double().numpy(), k, v, ks, vs, table, [100], starts, scale, 0)
+            c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+            got = _np(neo.attention_paged_int8((c(k), c(v), c(ks), c(vs)), q.cuda(), c(table), c(np.array([100], np.int32)), c(starts),
+                                               chunk, 100, scale=scale))
+            assert (np.abs(got - ref) <= _attention_bound(ref, A, B, 64, 100, dtype)).all(), (chunk, vscale, qscale)
+
+
+@gpu
+@pytest.mark.parametrize("chunk", [1, 50])
+def test_attention_strides_and_repeat(torch, chunk):
+    """q and out as slices of wider buffers, a table with a wider stride: the
+    same bits as contiguous ones, on another stream too."""
+    H, D, page, ctx = 2, 64, 16, 1000
+    k, v, ks, vs, table = _paged(torch, [ctx], H, D, page, 16)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    cache, ctxs, starts = (c(k), c(v), c(ks), c(vs)), c(np.array([ctx], np.int32)), c(np.array([0, chunk], np.int32))
+    q = _rand(torch, (chunk, 4, D), "bfloat16", 17).cuda()
+    plain = neo.attention_paged_int8(cache, q, c(table), ctxs, starts, chunk, ctx)
+    wide = torch.full((chunk, 7, D + 16), 5.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, 1:5, 8:8 + D] = q
+    out = torch.full((chunk, 6, D + 3), 5.0, dtype=torch.bfloat16, device="cuda")
+    tab = torch.full((1, table.shape[1] + 5), -7, dtype=torch.int32, device="cuda")
+    tab[:, :table.shape[1]] = c(table)
+    neo.attention_paged_int8(cache, wide[:, 1:5, 8:8 + D], tab[:, :table.shape[1]], ctxs, starts, chunk, ctx, out=out[:, 1:5, 3:])
+    assert torch.equal(out[:, 1:5, 3:], plain)
+    out[:, 1:5, 3:] = 5
+    assert (out == 5).all()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = neo.attention_paged_int8(cache, q, c(table), ctxs, starts, chunk, ctx)
+    torch.cuda.synchronize()
+    assert torch.equal(again, plain)
+
+
+@gpu
+def test_attention_beyond_the_bounds(torch):
+    """Contexts and chunks past max_context, max_chunk and the table are not read."""
+    k, v, ks, vs, table = _paged(torch, [64], 1, 64, 16, 18)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    q = _rand(torch, (4, 2, 64), "float16", 19).cuda()
+    cache = (c(k), c(v), c(ks), c(vs))
+    for contexts, starts in (([1 << 30], [0, 4]), ([-5], [0, 4]), ([64], [0, 1 << 30]), ([64], [-9, 3]), ([64], [3, 1])):
+        neo.attention_paged_int8(cache, q, c(table), c(np.array(contexts, np.int32)), c(np.array(starts, np.int32)), 4, 64)
+    torch.cuda.synchronize()
+
+
+@gpu
+def test_no_tokens(torch):
+    e = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    q, s, h = neo.rmsnorm_int8(e(0, 64), None, residual=e(0, 64))
+    assert q.shape == (0, 64) and h.shape == (0, 64)
+    q, s = neo.quantize_tokens_int8(e(0, 40))
+    w, ws = neo.pack_dense_int8(torch.ones(8, 40, device="cuda"))
+    assert neo.matmul_int8(q, s, 40, w, ws, 8).shape == (0, 8)
+    cache = neo.kv_cache(2, 1, 4, 16)
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    neo.kv_write_int8(cache, e(0, 1, 16), e(0, 1, 16), none)
+    assert neo.kv_read_int8(cache, none, torch.float16)[0].shape == (0, 1, 16)
+    z = torch.zeros(2, dtype=torch.int32, device="cuda")
+    assert neo.attention_paged_int8(cache, e(0, 1, 16), z[:1].view(1, 1), z[:1], z, 0, 0).shape == (0, 1, 16)
+
+
+@gpu
+def test_wrong_tensors_are_refused(torch):
+    x = torch.ones(4, 32, device="cuda")
+    q, s = neo.quantize_tokens_int8(x)
+    w, ws = neo.pack_dense_int8(torch.ones(8, 32, device="cuda"))
+    cache = neo.kv_cache(2, 1, 4, 16)
+    z = torch.zeros(2, dtype=torch.int32, device="cuda")
+    k = torch.ones(1, 1, 16, device="cuda")
+    slots = torch.zeros(1, dtype=torch.int64, device="cuda")
+    for bad in (lambda: neo.quantize_tokens_int8(x.cpu()), lambda: neo.quantize_tokens_int8(x.double()),
+                lambda: neo.quantize_tokens_int8(x.t()), lambda: neo.quantize_tokens_int8(x, gate=x[:, :16]),
+                lambda: neo.rmsnorm_int8(x, torch.ones(31, device="cuda")), lambda: neo.rmsnorm_int8(x, None, residual=x.half()),
+                lambda: neo.matmul_int8(q, s[:3], 32, w, ws, 8), lambda: neo.matmul_int8(q, s, 33, w, ws, 8),
+                lambda: neo.matmul_int8(q, s, 32, w, ws, 9), lambda: neo.matmul_int8(x, s, 32, w, ws, 8),
+                lambda: neo.kv_write_int8(cache, k, k, slots.int()), lambda: neo.kv_write_int8(cache, k, k[:, :, :8], slots),
+                lambda: neo.kv_write_int8(cache, k, k.half(), slots), lambda: neo.kv_write_int8(cache[:3] + (cache[3][:1],), k, k, slots),
+                lambda: neo.attention_paged_int8(cache, k, z.view(2, 1), z, z, 1, 4),
+                lambda: neo.attention_paged_int8(cache, k, z[:1].view(1, 1), z[:1], z, 1, 5),
+                lambda: neo.attention_paged_int8(cache, torch.ones(1, 1, 32, device="cuda"), z[:1].view(1, 1), z[:1], z, 1, 4)):
+        with pytest.raises((TypeError, ValueError)):
+            bad()
