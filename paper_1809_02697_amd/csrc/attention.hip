@@ -18,6 +18,9 @@
 // S^T = K Q^T and O^T = V^T P^T: the accumulator's layout of S^T (a lane holds
 // four neighbouring keys of one row) is the layout of the second product's
 // operand, so weights go from one product to the other in registers.
+#include <atomic>
+#include <type_traits>
+
 #include "token_types.h"
 
 namespace neo {
@@ -25,11 +28,29 @@ namespace {
 
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLift = 14.f;  // weights are at most 2^15: the top of fp16's range
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMinusInf = -__builtin_inff();
+
+constexpr int kLowestE = -64;
+
+// Four rows' values of this lane's column: in each 16 lanes, lane i points at
+// four neighbouring columns of row i / 4, and gets the four rows of column i.
+__device__ inline h4 read_transposed(const _Float16* p) {
+    return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p));
+}
+
+template <typename T>
+__device__ inline void store4(T* p, v4f v) {
+    typedef T raw __attribute__((ext_vector_type(4)));
+    typedef T loose __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    *reinterpret_cast<loose*>(p) = __builtin_convertvector(v, raw);
+}
 
 // ---- int8 to fp16 ------------------------------------------------------------------------
 // A byte v + 128 (the sign bit flipped) under a zero byte is the fp16 number
@@ -108,6 +129,10 @@ __device__ inline void key_range(const AttnArgs& a, const Unit& u, int t0, int t
 // start rounded down to a multiple of 32.
 struct Split {
     int count, keys;
+    // key / page_size = key * page_mul >> page_shift for keys below 2^31
+    uint32_t page_mul;
+    int page_shift;
+    __device__ int page(int key) const { return (int)((uint64_t)(uint32_t)key * page_mul >> page_shift); }
 };
 __device__ inline int splits_of(const Split& sp, int lo, int hi) {
     return min(sp.count, max(1, (hi - (lo & ~31) + sp.keys - 1) / sp.keys));
@@ -191,7 +216,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
         u4 kw[2][KB / 16];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int key = min(kb + 16 * t + li, hi - 1), pg = key / ps;
+            const int key = min(kb + 16 * t + li, hi - 1), pg = sp.page(key);
             int page = a.table[b * a.table_stride + pg];
             if ((uint32_t)page >= (uint32_t)a.c.pages) page = 0;
             const int8_t* p = a.c.k + (((int64_t)page * H + h) * ps + (key - pg * ps)) * D + g * KB;
@@ -207,7 +232,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int j = kb + 16 * t + 4 * g + r, key = min(j, hi - 1), pg = key / ps;
+                const int j = kb + 16 * t + 4 * g + r, key = min(j, hi - 1), pg = sp.page(key);
                 int page = a.table[b * a.table_stride + pg];
                 const bool there = (uint32_t)page < (uint32_t)a.c.pages;
                 if (!there) page = 0;
@@ -360,9 +385,334 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
     }
 }
 
-// The parts of a row, joined: one wave a row.
-template <typename T, int TILE>
-__global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Parts ws) {
+// ---- 32 rows a wave -------------------------------------------------------------------
+// NW waves share tiles of KT keys: keys and values are converted to fp16 once
+// per workgroup on their way into LDS (the next tile's bytes travel meanwhile),
+// and each wave multiplies its 32 rows with them on 32x32x16 products.  Values
+// lie in LDS as they came and are read transposed.
+template <typename T, int DP, int TERMS, int NW>
+struct TileShape {
+    static constexpr int KT = DP == 256 ? 32 : 64, THREADS = NW * 64, ROWS = NW * 32;
+    static constexpr int CH = DP / 16, CHUNKS = KT * CH, LOADS = (CHUNKS + THREADS - 1) / THREADS;
+    static constexpr int KSTRIDE = DP, VSTRIDE = DP + 32;  // halves; the value rows' 64 spare bytes spread their banks
+    struct alignas(512) Buffer {  // (a key row's pieces are exchanged within 256 bytes by xor)
+        _Float16 k[KT * KSTRIDE], v[KT * VSTRIDE];
+        float ks[KT], vs[KT];
+        unsigned long long hidden;  // tokens in pages outside the cache
+        int top;                    // exponent of the largest value scale
+    };
+    static constexpr int BYTES = 2 * sizeof(Buffer);
+    static constexpr int MASK = CH * 2 < 16 ? CH * 2 - 1 : 15;
+};
+
+template <typename T, int DP, int TERMS, int NW>
+__global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, Parts ws) {
+    typedef TileShape<T, DP, TERMS, NW> C;
+    constexpr int KT = C::KT, SUB = KT / 32, STEPS = DP / 16, DT = DP / 32;
+    typedef typename C::Buffer Buffer;
+    extern __shared__ __align__(512) char lds[];
+    Buffer* buf = reinterpret_cast<Buffer*>(lds);
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, half = lane >> 5;
+    const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim, ps = a.c.page_size;
+    const int split = blockIdx.x % sp.count, at = blockIdx.x / sp.count;
+    const int units = a.seqs * H, tiles = gridDim.x / sp.count / units;
+    const int tile = tiles - 1 - at / units, unit = at % units, b = unit / H, h = unit - b * H;
+    const Unit u = unit_of(a, b);
+    const int rows = u.n * G, row0 = tile * C::ROWS;
+    if (row0 >= rows) return;
+    int lo, hi;
+    key_range(a, u, row0 / G, (min(row0 + C::ROWS, rows) - 1) / G, lo, hi);
+    if (split >= splits_of(sp, lo, hi)) return;
+    const int first = (lo & ~31) + split * sp.keys, last = min(hi, first + sp.keys);
+
+    // this lane's row of queries; the positions of its wave's rows
+    const int wrow = row0 + wave * 32, row = wrow + li;
+    const bool live = row < rows;
+    const int tok = min(row, rows - 1) / G, pos = u.ctx - u.all + tok;
+    const int pos_lo = u.ctx - u.all + min(wrow, rows - 1) / G, pos_hi = u.ctx - u.all + min(wrow + 31, rows - 1) / G;
+    h8 q[TERMS][STEPS];
+    float fq;
+    {
+        const int hq = h * G + min(row, rows - 1) - tok * G;
+        const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)hq * a.qhs + half * 8;
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            if (s * 16 >= D) continue;
+            const f32x8 v = load8(src + s * 16);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+        const int e = top >= kInfBits ? 0 : min(14 - exponent(top), 126);
+        const float up = ldexpf(1.f, e);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const f32x8 v = (s * 16 < D ? load8(src + s * 16) : f32x8{0, 0, 0, 0, 0, 0, 0, 0}) * up;
+            q[0][s] = __builtin_convertvector(v, h8);
+            if constexpr (TERMS == 2) q[1][s] = __builtin_convertvector(v - __builtin_convertvector(q[0][s], f32x8), h8);
+        }
+        fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
+        if (top >= kInfBits) fq = __uint_as_float(0x7fc00000u);
+    }
+
+    // the tiles' way into LDS: 16 bytes of a key and of a value a thread and load
+    const int32_t* table = a.table + b * a.table_stride;
+    int pg[C::LOADS], spg = 0;
+    u4 kr[C::LOADS], vr[C::LOADS];
+    float ksr = 0.f, vsr = 0.f;
+    bool hid = false;
+    auto lookup = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < C::LOADS; ++i) pg[i] = table[sp.page(min(k0 + (tid + i * C::THREADS) / C::CH, hi - 1))];
+        if (tid < KT) spg = table[sp.page(min(k0 + tid, hi - 1))];
+    };
+    auto fetch = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < C::LOADS; ++i) {
+            const int x = tid + i * C::THREADS, c = x % C::CH, key = min(k0 + x / C::CH, hi - 1);
+            const int page = (uint32_t)pg[i] < (uint32_t)a.c.pages ? pg[i] : 0;
+            const int64_t e = (((int64_t)page * H + h) * ps + (key - sp.page(key) * ps)) * D + c * 16;
+            kr[i] = vr[i] = u4{0, 0, 0, 0};
+            if (c * 16 < D) {
+                kr[i] = *reinterpret_cast<const u4*>(a.c.k + e);
+                vr[i] = *reinterpret_cast<const u4*>(a.c.v + e);
+            }
+        }
+        if (tid < KT) {
+            const int key = min(k0 + tid, hi - 1);
+            hid = (uint32_t)spg >= (uint32_t)a.c.pages;
+            const int64_t e = ((int64_t)(hid ? 0 : spg) * H + h) * ps + (key - sp.page(key) * ps);
+            ksr = a.c.k_scale[e];
+            vsr = a.c.v_scale[e];
+        }
+    };
+    auto store = [&](Buffer& to) {
+#pragma unroll
+        for (int i = 0; i < C::LOADS; ++i) {
+            const int x = tid + i * C::THREADS, c = x % C::CH, key = x / C::CH;
+            if (C::CHUNKS % C::THREADS && x >= C::CHUNKS) break;
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                h2 x0, x1, x2, x3;
+                unpack4(biased(kr[i][2 * o]), x0, x1);
+                unpack4(biased(kr[i][2 * o + 1]), x2, x3);
+                *reinterpret_cast<h8*>(to.k + key * C::KSTRIDE + ((2 * c + o) ^ (key & C::MASK)) * 8) = join(x0, x1, x2, x3);
+            }
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                h2 x0, x1, x2, x3;
+                unpack4(biased(vr[i][2 * o]), x0, x1);
+                unpack4(biased(vr[i][2 * o + 1]), x2, x3);
+                *reinterpret_cast<h8*>(to.v + key * C::VSTRIDE + (2 * c + o) * 8) = join(x0, x1, x2, x3);
+            }
+        }
+        if (wave == 0) {  // (the KT scales lie in its lanes)
+            const uint32_t top = lanes_max(lane < KT && !hid ? magnitude(vsr) : 0u);
+            const unsigned long long bad = __ballot(lane < KT && hid);
+            if (lane < KT) {
+                to.ks[lane] = ksr;
+                to.vs[lane] = vsr;
+            }
+            if (lane == 0) {
+                to.hidden = bad;
+                to.top = exponent(top);
+            }
+        }
+    };
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = f32x16{0};
+    float m = kMinusInf, l = 0.f;  // the running maximum is of scores / fq
+    int E = kLowestE;
+
+    auto compute = [&](const Buffer& from, int k0) {
+        f32x16 s[SUB];
+        // byte address of this lane's piece 0 of key li; piece c is that xor 32 c
+        uint32_t kaddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)reinterpret_cast<const char*>(from.k) +
+                         li * (2 * C::KSTRIDE) + ((half ^ (li & C::MASK)) * 16);
+        asm volatile("" : "+v"(kaddr));  // (kept in one register, not in one for every c)
+#pragma unroll
+        for (int t = 0; t < SUB; ++t) {
+            s[t] = f32x16{0};
+#pragma unroll
+            for (int c = 0; c < STEPS; ++c) {
+                const h8 k = *(__attribute__((address_space(3))) const h8*)(uintptr_t)((kaddr ^ (c * 32)) + t * 32 * (2 * C::KSTRIDE));
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i][c], s[t], 0, 0, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const unsigned long long hidden = from.hidden;
+        const bool all = k0 + KT - 1 <= pos_lo && k0 + KT <= last && hidden == 0 && (!a.window || k0 > pos_hi - a.window);
+        auto scales = [&](const float* p, int t, int g) { return *reinterpret_cast<const v4f*>(p + 32 * t + 8 * g + 4 * half); };
+#pragma unroll
+        for (int t = 0; t < SUB; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const v4f ks = scales(from.ks, t, g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[t][4 * g + i] *= ks[i];
+            }
+        int En = max(E, min(from.top, 126));
+        if (!all) {
+            // this lane's keys k0 + 4 half + x: seen from x = from_x up to to_x
+            const int j0 = k0 + 4 * half, to_x = live ? min(pos, last - 1) - j0 : -1;
+            const int from_x = a.window ? pos - a.window + 1 - j0 : 0;
+            uint32_t vtop = 0;
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const v4f vs = scales(from.vs, t, g);
+                    const uint32_t hid8 = (uint32_t)(hidden >> (32 * t + 8 * g)) >> (4 * half);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int x = 32 * t + 8 * g + i;
+                        const bool see = x <= to_x && x >= from_x && !(hid8 >> i & 1);
+                        s[t][4 * g + i] = see ? s[t][4 * g + i] : kMinusInf;
+                        vtop = max(vtop, see ? magnitude(vs[i]) : 0u);
+                    }
+                }
+            vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 32, 64));
+            En = max(E, min(exponent(vtop), 126));
+        }
+        float top = kMinusInf;
+#pragma unroll
+        for (int t = 0; t < SUB; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mn = fmaxf(m, top), m0 = mn == kMinusInf ? 0.f : mn;
+        if (__any(mn > m || En > E)) {
+            const float f = ldexpf(exp2_fast((m - m0) * fq), E - En);
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) o[t] *= f;
+            m = mn;
+            E = En;
+        }
+        const float lift = m0 * fq - kLift + (float)E;  // weights and l are 2^(14 - E) times p
+        float least = 1.f;
+        auto weigh = [&](auto whole) {
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const v4f vs = scales(from.vs, t, g);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = s[t][4 * g + i];
+                        const float p = exp2_fast(x * fq - lift);
+                        l += p;
+                        // (the scale of an entry that is not seen may be a NaN)
+                        s[t][4 * g + i] = p * (whole.value || x != kMinusInf ? vs[i] : 0.f);
+                        least = fminf(least, s[t][4 * g + i]);
+                    }
+                }
+        };
+        if (all)
+            weigh(std::true_type{});
+        else
+            weigh(std::false_type{});
+        auto values = [&](int t, int x, int d) {
+            // rows 32 t + 16 x + 8 {0, 1} + 4 half + 0..3, columns 32 d + 0..31, transposed
+            const _Float16* p = from.v + (32 * t + 16 * x + 4 * half + (lane & 15) / 4) * C::VSTRIDE + 32 * d + (lane & 16) + (lane & 3) * 4;
+            const h4 y0 = read_transposed(p), y1 = read_transposed(p + 8 * C::VSTRIDE);
+            return h8{y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
+        };
+        const bool small = __any(least < Levels<TERMS>::least);
+#pragma unroll
+        for (int t = 0; t < SUB; ++t)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                __builtin_amdgcn_sched_barrier(0);  // (reads of later groups would take registers from the accumulators)
+                f32x8 pv;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) pv[i] = s[t][8 * x + i];
+                h8 w[TERMS];
+                if (!small) {
+                    Levels<TERMS>::terms(pv, w);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const h8 v = values(t, x, d);
+#pragma unroll
+                        for (int i = 0; i < TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[i], o[d], 0, 0, 0);
+                    }
+                } else {
+                    float down = 1.f;
+                    bool more;
+                    do {
+                        more = Levels<TERMS>::take(pv, w);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            const h8 v = values(t, x, d);
+                            f32x16 z = {0};
+#pragma unroll
+                            for (int i = 0; i < TERMS; ++i) z = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[i], z, 0, 0, 0);
+                            o[d] += z * down;
+                        }
+                        down *= 1.f / Levels<TERMS>::step;
+                    } while (__any(more));
+                }
+            }
+    };
+
+    if (first < last) {
+        lookup(first);
+        fetch(first);
+        if (first + KT < last) lookup(first + KT);
+        store(buf[0]);
+        if (first + KT < last) fetch(first + KT);
+        __syncthreads();
+        int at_buf = 0;
+        for (int k0 = first; k0 < last; k0 += KT) {
+            const bool next = k0 + KT < last, after = k0 + 2 * KT < last;
+            if (after) lookup(k0 + 2 * KT);
+            if (wrow < rows && k0 <= pos_hi && (!a.window || k0 + KT > pos_lo + 1 - a.window)) compute(buf[at_buf], k0);
+            if (next) store(buf[at_buf ^ 1]);
+            if (after) fetch(k0 + 2 * KT);
+            __syncthreads();
+            at_buf ^= 1;
+        }
+    }
+    if (!live) return;
+    l += __shfl_xor(l, 32, 64);
+    const float M = m == kMinusInf ? kMinusInf : m * fq;
+    const int rw = row;
+    if (sp.count == 1) {
+        const float f = l == 0.f ? 0.f : 512.f / l;
+        const int hq = h * G + rw - tok * G;
+        T* out = static_cast<T*>(a.out) + (int64_t)(u.first + tok) * a.ots + (int64_t)hq * a.ohs + 4 * half;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                if (32 * d + 8 * g >= D) continue;
+                store4(out + 32 * d + 8 * g, v4f{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]} * f);
+            }
+    } else {
+        const int64_t part = ((int64_t)unit * ws.rows + rw) * sp.count + split;
+        float* out = ws.o + part * D + 4 * half;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                if (32 * d + 8 * g >= D) continue;
+                v4f v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = ldexpf(o[d][4 * g + i], E - 14 + 9);
+                *reinterpret_cast<v4f*>(out + 32 * d + 8 * g) = v;
+            }
+        if (half == 0) ws.ml[part] = make_float2(M, ldexpf(l, E - 14));
+    }
+}
+
+// The parts of a row, joined: one wave a row.  `tile`: rows that shared a range of keys.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Parts ws, int tile) {
     const int lane = threadIdx.x & 63;
     const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim;
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -372,9 +722,9 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Part
     const Unit u = unit_of(a, b);
     const int rows = u.n * G;
     if (row >= rows) return;
-    const int row0 = row / TILE * TILE;
+    const int row0 = row / tile * tile;
     int lo, hi;
-    key_range(a, u, row0 / G, (min(row0 + TILE, rows) - 1) / G, lo, hi);
+    key_range(a, u, row0 / G, (min(row0 + tile, rows) - 1) / G, lo, hi);
     const int count = splits_of(sp, lo, hi);
     const float2* ml = ws.ml + at * sp.count;
     const float* o = ws.o + at * sp.count * D;
@@ -393,16 +743,32 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Part
         if (lane + 64 * i < D) store_row<T>(a, u, h, G, row, lane + 64 * i, L == 0.f ? 0.f : v[i] / L);
 }
 
+// Rows a workgroup takes: one token's heads, or up to 16 rows, go to the
+// kernel for few rows; the tiles grow with the rows a unit has.
+int tile_rows(const AttnArgs& a) {
+    const int64_t rows = (int64_t)a.max_chunk * (a.q_heads / a.c.kv_heads);
+    if (rows <= 16) return 16;
+    if (rows <= 64) return 64;
+    if (rows <= 128 || a.c.head_dim > 128) return 128;
+    return 256;
+}
+
 // Enough workgroups for the chip from splits of at least 256 keys.
-Split choose_split(const AttnArgs& a, int tile) {
-    const int G = a.q_heads / a.c.kv_heads;
+Split choose_split(const AttnArgs& a) {
+    const int tile = tile_rows(a), G = a.q_heads / a.c.kv_heads;
     const int64_t tiles = ((int64_t)a.max_chunk * G + tile - 1) / tile;
     const int64_t groups = tiles * a.seqs * a.c.kv_heads;
     int64_t range = a.max_context;
     if (a.window) range = std::min<int64_t>(range, (int64_t)a.window + (tile + G - 1) / G + 33);
-    const int64_t want = std::max<int64_t>(1, 4096 / groups);
+    const int64_t want = std::max<int64_t>(1, (tile == 16 ? 4096 : 512) / groups);
     const int64_t keys = std::max<int64_t>(256, (range / want + 127) / 128 * 128);
-    return Split{(int)((range + 31 + keys - 1) / keys), (int)keys};
+    Split sp;
+    sp.count = (int)((range + 31 + keys - 1) / keys);
+    sp.keys = (int)keys;
+    const int log = ilog2(a.c.page_size);
+    sp.page_mul = (uint32_t)((1ull << (31 + log)) / (uint32_t)a.c.page_size + 1);
+    sp.page_shift = 31 + log;
+    return sp;
 }
 
 size_t parts_floats(const AttnArgs& a, const Split& sp, int64_t* o_floats) {
@@ -411,19 +777,46 @@ size_t parts_floats(const AttnArgs& a, const Split& sp, int64_t* o_floats) {
     return (size_t)(*o_floats + 4 + rows * sp.count * 2);
 }
 
+template <typename T, int DP, int TERMS, int NW>
+hipError_t launch_tile(const AttnArgs& a, const Split& sp, const Parts& p, unsigned blocks, hipStream_t st) {
+    constexpr int bytes = TileShape<T, DP, TERMS, NW>::BYTES;
+    // (more LDS than a kernel gets unasked; set once per device)
+    static std::atomic<uint64_t> asked{0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64 || !(asked.load() >> dev & 1)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_tile<T, DP, TERMS, NW>),
+                                hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+        if (dev >= 0 && dev < 64) asked.fetch_or(1ull << dev);
+    }
+    hipLaunchKernelGGL((attention_tile<T, DP, TERMS, NW>), dim3(blocks), dim3(NW * 64), bytes, st, a, sp, p);
+    return hipGetLastError();
+}
+
 template <typename T, int DP, int TERMS>
 hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
-    const Split sp = choose_split(a, 16);
-    const int G = a.q_heads / a.c.kv_heads;
+    const Split sp = choose_split(a);
+    const int G = a.q_heads / a.c.kv_heads, tile = tile_rows(a);
     int64_t of;
     parts_floats(a, sp, &of);
     const Parts p{ws, reinterpret_cast<float2*>(ws + (of + 3) / 4 * 4), a.max_chunk * G};
-    const int64_t blocks = (((int64_t)a.max_chunk * G + 15) / 16) * a.seqs * a.c.kv_heads * sp.count;
-    hipLaunchKernelGGL((attention_rows<T, DP, TERMS>), dim3((unsigned)blocks), dim3(kRowsWaves * 64), 0, st, a, sp, p);
-    hipError_t e = hipGetLastError();
+    const unsigned blocks = (unsigned)((((int64_t)a.max_chunk * G + tile - 1) / tile) * a.seqs * a.c.kv_heads * sp.count);
+    hipError_t e;
+    if (tile == 16) {
+        hipLaunchKernelGGL((attention_rows<T, DP, TERMS>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sp, p);
+        e = hipGetLastError();
+    } else if (tile == 64) {
+        e = launch_tile<T, DP, TERMS, 2>(a, sp, p, blocks, st);
+    } else if (DP == 256 || tile == 128) {
+        e = launch_tile<T, DP, TERMS, 4>(a, sp, p, blocks, st);
+    } else {
+        e = launch_tile<T, DP, TERMS, DP == 256 ? 4 : 8>(a, sp, p, blocks, st);
+    }
     if (e != hipSuccess || sp.count == 1) return e;
     const int64_t rows = (int64_t)a.seqs * a.c.kv_heads * p.rows;
-    hipLaunchKernelGGL((attention_join<T, 16>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, sp, p);
+    hipLaunchKernelGGL(attention_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, sp, p, tile);
     return hipGetLastError();
 }
 
@@ -437,7 +830,7 @@ hipError_t by_dim(const AttnArgs& a, float* ws, hipStream_t st) {
 }  // namespace
 
 size_t attention_workspace(int, const AttnArgs& a) {
-    const Split sp = choose_split(a, 16);
+    const Split sp = choose_split(a);
     int64_t of;
     return sp.count == 1 ? 0 : parts_floats(a, sp, &of) * sizeof(float);
 }
