@@ -154,15 +154,78 @@ __device__ inline void store_row(const AttnArgs& a, const Unit& u, int h, int G,
 
 // ---- 16 rows a workgroup ------------------------------------------------------------
 // Four waves take turns at blocks of 32 keys; the key and value bytes go from
-// memory straight into registers (every byte is used once) and the waves'
-// results are joined in LDS.
+// memory straight into registers (every byte is used once), the next block's
+// while this one's are used, and the waves' results are joined in LDS.
+// TILED: pages of whole 16 tokens, so a page is looked up once per 16 keys for
+// the whole wave; other pages are looked up key by key.
 constexpr int kRowsWaves = 4;
 
-template <typename T, int DP, int TERMS>
-__global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Split sp, Parts ws) {
-    constexpr int KB = DP / 4, STEPS = DP / 32, VB = DP / 16;  // bytes of a key a lane holds, products, of a value
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
-    const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim, ps = a.c.page_size;
+template <int DP>
+struct KeyBlock {
+    static constexpr int KB = DP / 4, VB = DP / 16;  // bytes of a key, of a value a lane holds
+    u4 k[2][KB / 16];              // keys 16 t + li: bytes g * KB ...
+    uint32_t v[2][4][VB / 4];      // values 16 t + 4 g + r: bytes li * VB ...
+    float ks[2][4], vs[2][4];      // their scales
+    uint32_t there;                // bit 4 t + r: the key's page exists
+};
+
+template <int DP, bool TILED>
+__device__ inline void load_block(const AttnArgs& a, const Split& sp, const int32_t* table, int h, int kb, int hi, int li,
+                                  int g, KeyBlock<DP>& to) {
+    constexpr int KB = DP / 4, VB = DP / 16;
+    const int H = a.c.kv_heads, D = a.c.head_dim, ps = a.c.page_size;
+    to.there = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        if constexpr (TILED) {
+            // (the last key's 16 stand in for those past it; entries past it lie in its page)
+            const int key = min(kb + 16 * t, (hi - 1) & ~15), pg = sp.page(key);
+            int page = table[pg];
+            const bool there = (uint32_t)page < (uint32_t)a.c.pages;
+            to.there |= there ? 0xfu << (4 * t) : 0u;
+            const int64_t e = ((int64_t)(there ? page : 0) * H + h) * ps + (key - pg * ps);
+            const int8_t *k = a.c.k + e * D, *v = a.c.v + e * D;
+#pragma unroll
+            for (int c = 0; c < KB / 16; ++c)
+                to.k[t][c] = g * KB + c * 16 < D ? *reinterpret_cast<const u4*>(k + li * D + g * KB + c * 16) : u4{0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                to.ks[t][r] = a.c.k_scale[e + 4 * g + r];
+                to.vs[t][r] = a.c.v_scale[e + 4 * g + r];
+#pragma unroll
+                for (int c = 0; c < VB / 4; ++c)
+                    to.v[t][r][c] = li * VB < D ? reinterpret_cast<const uint32_t*>(v + (4 * g + r) * D + li * VB)[c] : 0;
+            }
+        } else {
+            auto entry = [&](int j, bool& there) {
+                const int key = min(j, hi - 1), pg = sp.page(key), page = table[pg];
+                there = (uint32_t)page < (uint32_t)a.c.pages;
+                return ((int64_t)(there ? page : 0) * H + h) * ps + (key - pg * ps);
+            };
+            bool there;
+            const int8_t* k = a.c.k + entry(kb + 16 * t + li, there) * D + g * KB;
+#pragma unroll
+            for (int c = 0; c < KB / 16; ++c)
+                to.k[t][c] = g * KB + c * 16 < D ? *reinterpret_cast<const u4*>(k + c * 16) : u4{0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t e = entry(kb + 16 * t + 4 * g + r, there);
+                to.there |= there ? 1u << (4 * t + r) : 0u;
+                to.ks[t][r] = a.c.k_scale[e];
+                to.vs[t][r] = a.c.v_scale[e];
+#pragma unroll
+                for (int c = 0; c < VB / 4; ++c)
+                    to.v[t][r][c] = li * VB < D ? reinterpret_cast<const uint32_t*>(a.c.v + e * D + li * VB)[c] : 0;
+            }
+        }
+    }
+}
+
+template <typename T, int DP, int TERMS, bool TILED>
+__global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_rows(AttnArgs a, Split sp, Parts ws) {
+    constexpr int KB = DP / 4, STEPS = DP / 32, VB = DP / 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, g = lane >> 4;
+    const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim;
     const int split = blockIdx.x % sp.count, at = blockIdx.x / sp.count;
     const int units = a.seqs * H, tile = at / units, unit = at - tile * units, b = unit / H, h = unit - b * H;
     const Unit u = unit_of(a, b);
@@ -172,16 +235,19 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
     key_range(a, u, row0 / G, (min(row0 + 16, rows) - 1) / G, lo, hi);
     const int first = (lo & ~31) + split * sp.keys, last = min(hi, first + sp.keys);
     if (split >= splits_of(sp, lo, hi)) return;
+    const int32_t* table = a.table + b * a.table_stride;
+
+    KeyBlock<DP> kv;
+    int kb = first + wave * 32;
+    if (kb < last) load_block<DP, TILED>(a, sp, table, h, kb, hi, li, g, kv);
 
     // this lane's row of queries: values d = g * KB + ...
-    const int row = row0 + li;
-    const bool live = row < rows;
-    const int tok = (live ? row : row0) / G, pos = u.ctx - u.all + tok;
+    const int row = min(row0 + li, rows - 1), tok = row / G, pos = u.ctx - u.all + tok;
+    const int pos_lo = u.ctx - u.all + row0 / G, pos_hi = u.ctx - u.all + (min(row0 + 16, rows) - 1) / G;
     h8 q[TERMS][STEPS];
     float fq;  // what a score is multiplied with
     {
-        const int hq = h * G + (live ? row : row0) - tok * G;
-        const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)hq * a.qhs + g * KB;
+        const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)(h * G + row - tok * G) * a.qhs + g * KB;
         f32x8 v[STEPS];
         uint32_t top = 0;
 #pragma unroll
@@ -211,41 +277,10 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
     float m = kMinusInf, l = 0.f;
     int E = -127;  // exponent of the largest value scale seen so far
 
-    for (int kb = first + wave * 32; kb < last; kb += kRowsWaves * 32) {
-        // K: this lane's keys are kb + li and kb + 16 + li
-        u4 kw[2][KB / 16];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int key = min(kb + 16 * t + li, hi - 1), pg = sp.page(key);
-            int page = a.table[b * a.table_stride + pg];
-            if ((uint32_t)page >= (uint32_t)a.c.pages) page = 0;
-            const int8_t* p = a.c.k + (((int64_t)page * H + h) * ps + (key - pg * ps)) * D + g * KB;
-#pragma unroll
-            for (int c = 0; c < KB / 16; ++c)
-                kw[t][c] = g * KB + c * 16 < D ? *reinterpret_cast<const u4*>(p + c * 16) : u4{0, 0, 0, 0};
-        }
-        // V and both scales: keys kb + 16 t + 4 g + r
-        uint32_t vw[2][4][VB / 4];
-        float ks[2][4], vs[2][4];
-        uint32_t seen = 0;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int j = kb + 16 * t + 4 * g + r, key = min(j, hi - 1), pg = sp.page(key);
-                int page = a.table[b * a.table_stride + pg];
-                const bool there = (uint32_t)page < (uint32_t)a.c.pages;
-                if (!there) page = 0;
-                const int64_t e = ((int64_t)page * H + h) * ps + (key - pg * ps);
-                ks[t][r] = a.c.k_scale[e];
-                vs[t][r] = a.c.v_scale[e];
-                const int8_t* p = a.c.v + e * D + li * VB;
-                const bool in = li * VB < D;
-#pragma unroll
-                for (int c = 0; c < VB / 4; ++c) vw[t][r][c] = in ? reinterpret_cast<const uint32_t*>(p)[c] : 0;
-                const bool see = there && j < last && j <= pos && (!a.window || j > pos - a.window) && live;
-                seen |= (uint32_t)see << (4 * t + r);
-            }
+    while (kb < last) {
+        const int kn = kb + kRowsWaves * 32;
+        KeyBlock<DP> next;
+        if (kn < last) load_block<DP, TILED>(a, sp, table, h, kn, hi, li, g, next);
 
         v4f s[2];
 #pragma unroll
@@ -254,25 +289,39 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
 #pragma unroll
             for (int c = 0; c < STEPS; ++c) {
                 h2 x[4];
-                unpack4(biased(kw[t][c / 2][c % 2 * 2]), x[0], x[1]);
-                unpack4(biased(kw[t][c / 2][c % 2 * 2 + 1]), x[2], x[3]);
+                unpack4(biased(kv.k[t][c / 2][c % 2 * 2]), x[0], x[1]);
+                unpack4(biased(kv.k[t][c / 2][c % 2 * 2 + 1]), x[2], x[3]);
                 const h8 k = join(x[0], x[1], x[2], x[3]);
 #pragma unroll
                 for (int i = 0; i < TERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i][c], s[t], 0, 0, 0);
             }
         }
 
+        const bool all = kb + 32 <= last && kb + 31 <= pos_lo && (!a.window || kb > pos_hi - a.window) &&
+                         __all(kv.there == 0xff);
+        if (!all) {
+            // this lane's keys j0 + x: seen from x = from_x up to to_x
+            const int j0 = kb + 4 * g, to_x = min(pos, last - 1) - j0, from_x = a.window ? pos - a.window + 1 - j0 : 0;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int x = 16 * t + r;
+                    const bool see = x <= to_x && x >= from_x && (kv.there >> (4 * t + r) & 1);
+                    s[t][r] = see ? s[t][r] : kMinusInf;
+                    kv.ks[t][r] = see ? kv.ks[t][r] : 1.f;
+                    kv.vs[t][r] = see ? kv.vs[t][r] : 0.f;
+                }
+        }
         float top = kMinusInf;
         uint32_t vtop = 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const bool see = seen >> (4 * t + r) & 1;
-                s[t][r] = see ? s[t][r] * ks[t][r] * fq : kMinusInf;
-                vs[t][r] = see ? vs[t][r] : 0.f;
+                s[t][r] *= kv.ks[t][r] * fq;
                 top = fmaxf(top, s[t][r]);
-                vtop = max(vtop, magnitude(vs[t][r]));
+                vtop = max(vtop, magnitude(kv.vs[t][r]));
             }
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -297,7 +346,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
             for (int r = 0; r < 4; ++r) {
                 const float p = exp2_fast(s[t][r] - lift);
                 l += p;
-                pv[4 * t + r] = p * ldexpf(vs[t][r], -E);
+                pv[4 * t + r] = p * ldexpf(kv.vs[t][r], -E);
                 small |= pv[4 * t + r] != 0.f && pv[4 * t + r] < Levels<TERMS>::least;
             }
 #pragma unroll
@@ -305,11 +354,11 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int c = 0; c < VB / 4; ++c) vw[t][r][c] = biased(vw[t][r][c]);
+                for (int c = 0; c < VB / 4; ++c) kv.v[t][r][c] = biased(kv.v[t][r][c]);
         auto values = [&](int t) {
             const int c = t / 4, y = t % 4;
-            return join(pair(vw[0][0][c], vw[0][1][c], y), pair(vw[0][2][c], vw[0][3][c], y),
-                        pair(vw[1][0][c], vw[1][1][c], y), pair(vw[1][2][c], vw[1][3][c], y));
+            return join(pair(kv.v[0][0][c], kv.v[0][1][c], y), pair(kv.v[0][2][c], kv.v[0][3][c], y),
+                        pair(kv.v[1][0][c], kv.v[1][1][c], y), pair(kv.v[1][2][c], kv.v[1][3][c], y));
         };
         h8 w[TERMS];
         if (!__any(small)) {
@@ -335,46 +384,44 @@ __global__ __launch_bounds__(kRowsWaves * 64) void attention_rows(AttnArgs a, Sp
                 down *= 1.f / Levels<TERMS>::step;
             } while (__any(small));
         }
+        kv = next;
+        kb = kn;
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     l *= 0x1p-14f;
 
     // the waves' parts: o[t][r] is value d = (4 g + r) * VB + t of row li
-    __shared__ float red_m[kRowsWaves][16], red_l[kRowsWaves][16], red_o[16][DP + 4];
+    __shared__ float red_m[kRowsWaves][16], red_l[kRowsWaves][16], red_o[kRowsWaves][16][DP + 4];
     if (g == 0) {
         red_m[wave][li] = m;
         red_l[wave][li] = l;
     }
     __syncthreads();
-    {
+    if (row0 + li < rows) {
         float M = kMinusInf;
 #pragma unroll
         for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][li]);
         const float f = m == kMinusInf ? 0.f : ldexpf(exp2_fast(m - M), E - 14 + 9);
 #pragma unroll
-        for (int w = 0; w < kRowsWaves; ++w) {
-            if (wave == w) {
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int t = 0; t < VB; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float& to = red_o[li][(4 * g + r) * VB + t];
-                        to = w ? to + o[t][r] * f : o[t][r] * f;
-                    }
-            }
-            __syncthreads();
-        }
+            for (int t = 0; t < VB; t += 4)
+                *reinterpret_cast<v4f*>(&red_o[wave][li][(4 * g + r) * VB + t]) = v4f{o[t][r], o[t + 1][r], o[t + 2][r], o[t + 3][r]} * f;
     }
-    for (int t = threadIdx.x; t < 16 * DP; t += kRowsWaves * 64) {
-        const int rr = t / DP, d = t - rr * DP, rw = row0 + rr;
-        if (rw >= rows || d >= D) continue;
-        float M = kMinusInf, L = 0.f;
+    __syncthreads();
+    const int live = min(16, rows - row0);
+    for (int x = threadIdx.x; x < live * DP; x += kRowsWaves * 64) {
+        const int rr = x / DP, d = x - rr * DP, rw = row0 + rr;
+        if (d >= D) continue;
+        float M = kMinusInf, L = 0.f, v = 0.f;
 #pragma unroll
         for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][rr]);
 #pragma unroll
-        for (int w = 0; w < kRowsWaves; ++w) L += red_m[w][rr] == kMinusInf ? red_l[w][rr] : red_l[w][rr] * exp2_fast(red_m[w][rr] - M);
-        const float v = red_o[rr][d];
+        for (int w = 0; w < kRowsWaves; ++w) {
+            L += red_m[w][rr] == kMinusInf ? red_l[w][rr] : red_l[w][rr] * exp2_fast(red_m[w][rr] - M);
+            v += red_o[w][rr][d];
+        }
         if (sp.count == 1) {
             store_row<T>(a, u, h, G, rw, d, L == 0.f ? 0.f : v / L);
         } else {
@@ -760,7 +807,7 @@ Split choose_split(const AttnArgs& a) {
     const int64_t groups = tiles * a.seqs * a.c.kv_heads;
     int64_t range = a.max_context;
     if (a.window) range = std::min<int64_t>(range, (int64_t)a.window + (tile + G - 1) / G + 33);
-    const int64_t want = std::max<int64_t>(1, (tile == 16 ? 4096 : 512) / groups);
+    const int64_t want = std::max<int64_t>(1, (tile == 16 ? 8192 : 512) / groups);
     const int64_t keys = std::max<int64_t>(256, (range / want + 127) / 128 * 128);
     Split sp;
     sp.count = (int)((range + 31 + keys - 1) / keys);
@@ -805,7 +852,10 @@ hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
     const unsigned blocks = (unsigned)((((int64_t)a.max_chunk * G + tile - 1) / tile) * a.seqs * a.c.kv_heads * sp.count);
     hipError_t e;
     if (tile == 16) {
-        hipLaunchKernelGGL((attention_rows<T, DP, TERMS>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sp, p);
+        if (a.c.page_size % 16 == 0)
+            hipLaunchKernelGGL((attention_rows<T, DP, TERMS, true>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sp, p);
+        else
+            hipLaunchKernelGGL((attention_rows<T, DP, TERMS, false>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sp, p);
         e = hipGetLastError();
     } else if (tile == 64) {
         e = launch_tile<T, DP, TERMS, 2>(a, sp, p, blocks, st);
