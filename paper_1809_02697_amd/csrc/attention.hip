@@ -165,57 +165,77 @@ struct KeyBlock {
     static constexpr int KB = DP / 4, VB = DP / 16;  // bytes of a key, of a value a lane holds
     u4 k[2][KB / 16];              // keys 16 t + li: bytes g * KB ...
     uint32_t v[2][4][VB / 4];      // values 16 t + 4 g + r: bytes li * VB ...
-    float ks[2][4], vs[2][4];      // their scales
+    v4f ks[2], vs[2];              // their scales
     uint32_t there;                // bit 4 t + r: the key's page exists
 };
 
+// The pages of a block's keys, looked up a block earlier than the bytes that
+// they lead to.
+template <bool TILED>
+struct KeyPages {
+    int k[2], v[2][TILED ? 1 : 4];
+};
+template <bool TILED>
+__device__ inline void look_up(const Split& sp, const int32_t* table, int kb, int hi, int li, int g, KeyPages<TILED>& to) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        to.k[t] = table[sp.page(min(kb + 16 * t + (TILED ? 0 : li), TILED ? (hi - 1) & ~15 : hi - 1))];
+        if constexpr (!TILED)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) to.v[t][r] = table[sp.page(min(kb + 16 * t + 4 * g + r, hi - 1))];
+    }
+}
+
+// Every lane loads, and blocks past the last key load that key's: the number of
+// loads under way is then known, and a block's use waits for its own loads
+// only.  (Pieces past head_dim read the row's start: the query is 0 there, and
+// such values are not stored.)
 template <int DP, bool TILED>
-__device__ inline void load_block(const AttnArgs& a, const Split& sp, const int32_t* table, int h, int kb, int hi, int li,
-                                  int g, KeyBlock<DP>& to) {
+__device__ inline void load_block(const AttnArgs& a, const Split& sp, const KeyPages<TILED>& pages, int h, int kb, int hi,
+                                  int li, int g, KeyBlock<DP>& to) {
     constexpr int KB = DP / 4, VB = DP / 16;
     const int H = a.c.kv_heads, D = a.c.head_dim, ps = a.c.page_size;
+    int koff[KB / 16];
+#pragma unroll
+    for (int c = 0; c < KB / 16; ++c) koff[c] = g * KB + c * 16 < D ? g * KB + c * 16 : 0;
+    const int voff = li * VB < D ? li * VB : 0;
+    typedef float loose4 __attribute__((ext_vector_type(4), aligned(4)));
     to.there = 0;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         if constexpr (TILED) {
-            // (the last key's 16 stand in for those past it; entries past it lie in its page)
-            const int key = min(kb + 16 * t, (hi - 1) & ~15), pg = sp.page(key);
-            int page = table[pg];
+            // (entries past the last key lie in its page)
+            const int key = min(kb + 16 * t, (hi - 1) & ~15), pg = sp.page(key), page = pages.k[t];
             const bool there = (uint32_t)page < (uint32_t)a.c.pages;
             to.there |= there ? 0xfu << (4 * t) : 0u;
             const int64_t e = ((int64_t)(there ? page : 0) * H + h) * ps + (key - pg * ps);
             const int8_t *k = a.c.k + e * D, *v = a.c.v + e * D;
+            to.ks[t] = *reinterpret_cast<const loose4*>(a.c.k_scale + e + 4 * g);
+            to.vs[t] = *reinterpret_cast<const loose4*>(a.c.v_scale + e + 4 * g);
 #pragma unroll
-            for (int c = 0; c < KB / 16; ++c)
-                to.k[t][c] = g * KB + c * 16 < D ? *reinterpret_cast<const u4*>(k + li * D + g * KB + c * 16) : u4{0, 0, 0, 0};
+            for (int c = 0; c < KB / 16; ++c) to.k[t][c] = *reinterpret_cast<const u4*>(k + li * D + koff[c]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                to.ks[t][r] = a.c.k_scale[e + 4 * g + r];
-                to.vs[t][r] = a.c.v_scale[e + 4 * g + r];
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int c = 0; c < VB / 4; ++c)
-                    to.v[t][r][c] = li * VB < D ? reinterpret_cast<const uint32_t*>(v + (4 * g + r) * D + li * VB)[c] : 0;
-            }
+                for (int c = 0; c < VB / 4; ++c) to.v[t][r][c] = reinterpret_cast<const uint32_t*>(v + (4 * g + r) * D + voff)[c];
         } else {
-            auto entry = [&](int j, bool& there) {
-                const int key = min(j, hi - 1), pg = sp.page(key), page = table[pg];
+            auto entry = [&](int j, int page, bool& there) {
+                const int key = min(j, hi - 1), pg = sp.page(key);
                 there = (uint32_t)page < (uint32_t)a.c.pages;
                 return ((int64_t)(there ? page : 0) * H + h) * ps + (key - pg * ps);
             };
             bool there;
-            const int8_t* k = a.c.k + entry(kb + 16 * t + li, there) * D + g * KB;
+            const int8_t* k = a.c.k + entry(kb + 16 * t + li, pages.k[t], there) * D;
 #pragma unroll
-            for (int c = 0; c < KB / 16; ++c)
-                to.k[t][c] = g * KB + c * 16 < D ? *reinterpret_cast<const u4*>(k + c * 16) : u4{0, 0, 0, 0};
+            for (int c = 0; c < KB / 16; ++c) to.k[t][c] = *reinterpret_cast<const u4*>(k + koff[c]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int64_t e = entry(kb + 16 * t + 4 * g + r, there);
+                const int64_t e = entry(kb + 16 * t + 4 * g + r, pages.v[t][r], there);
                 to.there |= there ? 1u << (4 * t + r) : 0u;
                 to.ks[t][r] = a.c.k_scale[e];
                 to.vs[t][r] = a.c.v_scale[e];
 #pragma unroll
-                for (int c = 0; c < VB / 4; ++c)
-                    to.v[t][r][c] = li * VB < D ? reinterpret_cast<const uint32_t*>(a.c.v + e * D + li * VB)[c] : 0;
+                for (int c = 0; c < VB / 4; ++c) to.v[t][r][c] = reinterpret_cast<const uint32_t*>(a.c.v + e * D + voff)[c];
             }
         }
     }
@@ -226,8 +246,11 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_
     constexpr int KB = DP / 4, STEPS = DP / 32, VB = DP / 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, g = lane >> 4;
     const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim;
-    const int split = blockIdx.x % sp.count, at = blockIdx.x / sp.count;
-    const int units = a.seqs * H, tile = at / units, unit = at - tile * units, b = unit / H, h = unit - b * H;
+    // Units vary fastest, then tiles, then splits: the workgroups that find
+    // keys spread over the chip however the contexts' lengths differ (splits
+    // fastest: 303 instead of XXX us at 32 contexts of 1,000 to 32,000).
+    const int units = a.seqs * H, at = blockIdx.x / units, tiles = gridDim.x / units / sp.count;
+    const int unit = blockIdx.x - at * units, split = at / tiles, tile = at - split * tiles, b = unit / H, h = unit - b * H;
     const Unit u = unit_of(a, b);
     const int rows = u.n * G, row0 = tile * 16;
     if (row0 >= rows) return;
@@ -239,7 +262,12 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_
 
     KeyBlock<DP> kv;
     int kb = first + wave * 32;
-    if (kb < last) load_block<DP, TILED>(a, sp, table, h, kb, hi, li, g, kv);
+    KeyPages<TILED> pages;
+    if (hi > 0) {
+        look_up<TILED>(sp, table, kb, hi, li, g, pages);
+        load_block<DP, TILED>(a, sp, pages, h, kb, hi, li, g, kv);
+        look_up<TILED>(sp, table, kb + kRowsWaves * 32, hi, li, g, pages);
+    }
 
     // this lane's row of queries: values d = g * KB + ...
     const int row = min(row0 + li, rows - 1), tok = row / G, pos = u.ctx - u.all + tok;
@@ -252,7 +280,9 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_
         uint32_t top = 0;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            v[s] = g * KB + s * 8 < D ? load8(src + s * 8) : f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+            const bool in = g * KB + s * 8 < D;
+            v[s] = load8(in ? src + s * 8 : src - g * KB);
+            if (!in) v[s] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[s][i]));
         }
@@ -280,7 +310,8 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_
     while (kb < last) {
         const int kn = kb + kRowsWaves * 32;
         KeyBlock<DP> next;
-        if (kn < last) load_block<DP, TILED>(a, sp, table, h, kn, hi, li, g, next);
+        load_block<DP, TILED>(a, sp, pages, h, kn, hi, li, g, next);
+        look_up<TILED>(sp, table, kn + kRowsWaves * 32, hi, li, g, pages);
 
         v4f s[2];
 #pragma unroll
@@ -462,9 +493,9 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, half = lane >> 5;
     const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim, ps = a.c.page_size;
-    const int split = blockIdx.x % sp.count, at = blockIdx.x / sp.count;
-    const int units = a.seqs * H, tiles = gridDim.x / sp.count / units;
-    const int tile = tiles - 1 - at / units, unit = at % units, b = unit / H, h = unit - b * H;
+    // (order: see attention_rows; the last tiles, which see the most keys, first)
+    const int units = a.seqs * H, at = blockIdx.x / units, tiles = gridDim.x / units / sp.count;
+    const int unit = blockIdx.x - at * units, split = at / tiles, tile = tiles - 1 - (at - split * tiles), b = unit / H, h = unit - b * H;
     const Unit u = unit_of(a, b);
     const int rows = u.n * G, row0 = tile * C::ROWS;
     if (row0 >= rows) return;
@@ -510,30 +541,27 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
     u4 kr[C::LOADS], vr[C::LOADS];
     float ksr = 0.f, vsr = 0.f;
     bool hid = false;
+    // (every thread loads, tiles past the last key load that key's, and pieces
+    // past head_dim the row's start: see load_block)
     auto lookup = [&](int k0) {
 #pragma unroll
         for (int i = 0; i < C::LOADS; ++i) pg[i] = table[sp.page(min(k0 + (tid + i * C::THREADS) / C::CH, hi - 1))];
-        if (tid < KT) spg = table[sp.page(min(k0 + tid, hi - 1))];
+        spg = table[sp.page(min(k0 + tid % KT, hi - 1))];
     };
     auto fetch = [&](int k0) {
 #pragma unroll
         for (int i = 0; i < C::LOADS; ++i) {
             const int x = tid + i * C::THREADS, c = x % C::CH, key = min(k0 + x / C::CH, hi - 1);
             const int page = (uint32_t)pg[i] < (uint32_t)a.c.pages ? pg[i] : 0;
-            const int64_t e = (((int64_t)page * H + h) * ps + (key - sp.page(key) * ps)) * D + c * 16;
-            kr[i] = vr[i] = u4{0, 0, 0, 0};
-            if (c * 16 < D) {
-                kr[i] = *reinterpret_cast<const u4*>(a.c.k + e);
-                vr[i] = *reinterpret_cast<const u4*>(a.c.v + e);
-            }
+            const int64_t e = (((int64_t)page * H + h) * ps + (key - sp.page(key) * ps)) * D + (c * 16 < D ? c * 16 : 0);
+            kr[i] = *reinterpret_cast<const u4*>(a.c.k + e);
+            vr[i] = *reinterpret_cast<const u4*>(a.c.v + e);
         }
-        if (tid < KT) {
-            const int key = min(k0 + tid, hi - 1);
-            hid = (uint32_t)spg >= (uint32_t)a.c.pages;
-            const int64_t e = ((int64_t)(hid ? 0 : spg) * H + h) * ps + (key - sp.page(key) * ps);
-            ksr = a.c.k_scale[e];
-            vsr = a.c.v_scale[e];
-        }
+        const int key = min(k0 + tid % KT, hi - 1);
+        hid = (uint32_t)spg >= (uint32_t)a.c.pages;
+        const int64_t e = ((int64_t)(hid ? 0 : spg) * H + h) * ps + (key - sp.page(key) * ps);
+        ksr = a.c.k_scale[e];
+        vsr = a.c.v_scale[e];
     };
     auto store = [&](Buffer& to) {
 #pragma unroll
@@ -710,17 +738,16 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
     if (first < last) {
         lookup(first);
         fetch(first);
-        if (first + KT < last) lookup(first + KT);
+        lookup(first + KT);
         store(buf[0]);
-        if (first + KT < last) fetch(first + KT);
+        fetch(first + KT);
         __syncthreads();
         int at_buf = 0;
         for (int k0 = first; k0 < last; k0 += KT) {
-            const bool next = k0 + KT < last, after = k0 + 2 * KT < last;
-            if (after) lookup(k0 + 2 * KT);
+            lookup(k0 + 2 * KT);
             if (wrow < rows && k0 <= pos_hi && (!a.window || k0 + KT > pos_lo + 1 - a.window)) compute(buf[at_buf], k0);
-            if (next) store(buf[at_buf ^ 1]);
-            if (after) fetch(k0 + 2 * KT);
+            store(buf[at_buf ^ 1]);
+            fetch(k0 + 2 * KT);
             __syncthreads();
             at_buf ^= 1;
         }
@@ -757,14 +784,15 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
     }
 }
 
-// The parts of a row, joined: one wave a row.  `tile`: rows that shared a range of keys.
-template <typename T>
+// The parts of a row, joined by WAVES waves in turn.  `tile`: rows that shared a
+// range of keys.
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Parts ws, int tile) {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turn = wave % WAVES;
     const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim;
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t at = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
     const int unit = (int)(at / ws.rows), row = (int)(at - (int64_t)unit * ws.rows);
-    if (unit >= a.seqs * H) return;
+    if (unit >= a.seqs * H) return;  // (with four waves a row: all of them)
     const int b = unit / H, h = unit - b * H;
     const Unit u = unit_of(a, b);
     const int rows = u.n * G;
@@ -775,19 +803,47 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Part
     const int count = splits_of(sp, lo, hi);
     const float2* ml = ws.ml + at * sp.count;
     const float* o = ws.o + at * sp.count * D;
-    float M = kMinusInf;
-    for (int s = 0; s < count; ++s) M = fmaxf(M, ml[s].x);
-    float L = 0.f, v[4] = {0, 0, 0, 0};
-    for (int s = 0; s < count; ++s) {
-        const float f = ml[s].x == kMinusInf ? 1.f : exp2_fast(ml[s].x - M);
-        L += ml[s].y * f;
+    float M = kMinusInf, L = 0.f;
+    for (int s = lane; s < count; s += 64) M = fmaxf(M, ml[s].x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (lane + 64 * i < D) v[i] += o[(int64_t)s * D + lane + 64 * i] * f;
+    for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+    auto factor = [&](float m) { return m == kMinusInf ? 1.f : exp2_fast(m - M); };  // (a part that saw nothing, or a NaN)
+    for (int s = lane; s < count; s += 64) L += ml[s].y * factor(ml[s].x);
+    L = lanes_sum(L);
+    float v[4] = {0, 0, 0, 0};
+    for (int s0 = 0; s0 < count; s0 += 64 * WAVES) {
+        const int mine = s0 + lane * WAVES + turn;  // this lane's part; part i of the wave is lane i's
+        const float f = mine < count ? factor(ml[mine].x) : 0.f;
+        const int parts = min(64, (count - s0 - turn + WAVES - 1) / WAVES);
+        for (int i = 0; i < parts; i += 4) {  // (past the last: the last, times 0)
+            float w[4][4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    w[y][x] = o[(int64_t)(s0 + min(i + y, parts - 1) * WAVES + turn) * D + min(lane + 64 * x, D - 1)];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const float fi = i + y < parts ? __shfl(f, min(i + y, 63), 64) : 0.f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[x] += i + y < parts ? w[y][x] * fi : 0.f;
+            }
+        }
+    }
+    if constexpr (WAVES > 1) {
+        __shared__ float red[WAVES][256];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) red[turn][lane + 64 * x] = v[x];
+        __syncthreads();
+        if (turn) return;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v[x] += red[w][lane + 64 * x];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (lane + 64 * i < D) store_row<T>(a, u, h, G, row, lane + 64 * i, L == 0.f ? 0.f : v[i] / L);
+    for (int x = 0; x < 4; ++x)
+        if (lane + 64 * x < D) store_row<T>(a, u, h, G, row, lane + 64 * x, L == 0.f ? 0.f : v[x] / L);
 }
 
 // Rows a workgroup takes: one token's heads, or up to 16 rows, go to the
@@ -866,7 +922,10 @@ hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
     }
     if (e != hipSuccess || sp.count == 1) return e;
     const int64_t rows = (int64_t)a.seqs * a.c.kv_heads * p.rows;
-    hipLaunchKernelGGL(attention_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, sp, p, tile);
+    if (sp.count > 4)
+        hipLaunchKernelGGL((attention_join<T, 4>), dim3((unsigned)rows), dim3(256), 0, st, a, sp, p, tile);
+    else
+        hipLaunchKernelGGL((attention_join<T, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, sp, p, tile);
     return hipGetLastError();
 }
 
