@@ -125,25 +125,215 @@ __device__ inline void key_range(const AttnArgs& a, const Unit& u, int t0, int t
     hi = max(hi, lo);
 }
 
-// Splits of the keys: `keys` (a multiple of 128) each, counted from the range's
-// start rounded down to a multiple of 32.
-struct Split {
-    int count, keys;
+// ---- shares ---------------------------------------------------------------------------
+// A unit of work is a row tile of a sequence's key/value head; its keys are
+// counted in blocks of BLK from the first it sees, rounded down to 32.  The
+// blocks of all units, in the order sequence, head, tile, are cut into equal
+// shares, one a workgroup, however the lengths differ.  A unit that lies in
+// one share is written at once; of one that is cut, each share leaves its part
+// in the workspace (a share has at most two such: where it starts in the
+// middle of a unit, and where it ends in one) and attention_join adds them.
+struct Shares {
+    int groups;  // workgroups; 0: one for each unit
     // key / page_size = key * page_mul >> page_shift for keys below 2^31
     uint32_t page_mul;
     int page_shift;
     __device__ int page(int key) const { return (int)((uint64_t)(uint32_t)key * page_mul >> page_shift); }
+    // of W blocks: shares of two blocks at least, a multiple of the chip's 8 dies
+    __device__ int used(int64_t W) const {
+        const int64_t n = min((int64_t)groups, max((int64_t)1, W / 2));
+        return (int)(n >= 8 ? n & ~7 : n);
+    }
 };
-__device__ inline int splits_of(const Split& sp, int lo, int hi) {
-    return min(sp.count, max(1, (hi - (lo & ~31) + sp.keys - 1) / sp.keys));
+// A value that all lanes hold, in scalar registers.
+__device__ inline int64_t uniform(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
 }
+__device__ inline int64_t share_start(int64_t W, int used, int i) { return W * i / used; }
 
-// A row's parts in the workspace: o[unit][row][split][head_dim] in true units
-// relative to the part's maximum, ml[unit][row][split] (maximum, sum).
+// Parts in the workspace: part 2 i of share i is the unit it starts in, 2 i + 1
+// the one it ends in; o[part][row of the tile][head_dim] in true units relative
+// to the part's maximum, ml[part][row] (maximum, sum).  starts[i]: where share i
+// starts, for the join (W = 0: no such share).
+struct Start {
+    int64_t W;
+    int b, h, tile, skip, blocks, unused;
+};
 struct Parts {
     float* o;
     float2* ml;
-    int rows;  // rows a unit can have
+    Start* starts;
+};
+
+// Setting a unit up and joining its waves takes a workgroup about as long as
+// this many blocks: they are counted as blocks in front of each unit's own.
+constexpr int kUnitCost = 4;
+
+template <int ROWS, int BLK>
+struct Cursor {
+    Unit u;
+    int b, h, tile, rows, tiles;  // rows and tiles of sequence b
+    int lo, hi, blocks;           // of the unit: its keys from lo (rounded) to hi
+    int skip;                     // blocks of the unit that lie before the share
+
+    __device__ static int tile_blocks(const AttnArgs& a, const Unit& u, int rows, int G, int tile, int& lo, int& hi) {
+        key_range(a, u, tile * ROWS / G, (min(tile * ROWS + ROWS, rows) - 1) / G, lo, hi);
+        lo &= ~31;
+        return kUnitCost + max(1, (hi - lo + BLK - 1) / BLK);
+    }
+    // blocks of one head of sequence b
+    __device__ static int64_t head_blocks(const AttnArgs& a, int G, int b) {
+        const Unit u = unit_of(a, b);
+        const int rows = u.n * G;
+        int64_t n = 0;
+        int lo, hi;
+        for (int t = 0; t * ROWS < rows; ++t) n += tile_blocks(a, u, rows, G, t, lo, hi);
+        return n;
+    }
+    __device__ void sequence(const AttnArgs& a, int G) {
+        u = unit_of(a, b);
+        rows = u.n * G;
+        tiles = (rows + ROWS - 1) / ROWS;
+    }
+    __device__ void unit(const AttnArgs& a, int G) { blocks = tile_blocks(a, u, rows, G, tile, lo, hi); }
+    __device__ void next(const AttnArgs& a, int G) {  // (there is a next one: the share goes on)
+        skip = 0;
+        if (++tile == tiles) {
+            tile = 0;
+            if (++h == a.c.kv_heads) {
+                h = 0;
+                do {
+                    ++b;
+                    sequence(a, G);
+                } while (rows == 0 && b + 1 < a.seqs);
+            }
+        }
+        unit(a, G);
+    }
+
+    // All threads of the workgroup: the sum W of all blocks, and with `find` the
+    // unit that holds block find(W) (none if that is not below W).
+    struct Scratch {
+        int64_t wave[16], off;
+        int b;
+    };
+    template <int THREADS, typename F>
+    __device__ int64_t locate(const AttnArgs& a, int G, Scratch& lds, F&& find) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        auto scan = [&](int64_t n, int64_t& total) {  // exclusive, over the workgroup
+            int64_t in = n;
+#pragma unroll
+            for (int x = 1; x < 64; x <<= 1) {
+                const int64_t v = __shfl_up(in, x, 64);
+                if (lane >= x) in += v;
+            }
+            __syncthreads();
+            if (lane == 63) lds.wave[wave] = in;
+            __syncthreads();
+            int64_t before = 0;
+            total = 0;
+            for (int w = 0; w < THREADS / 64; ++w) {
+                if (w < wave) before += lds.wave[w];
+                total += lds.wave[w];
+            }
+            total = uniform(total);
+            return before + in - n;
+        };
+        const int H = a.c.kv_heads;
+        int64_t W = 0, x = -1;
+        for (int pass = 0; pass < 2; ++pass) {
+            int64_t at = 0;
+            for (int b0 = 0; b0 < a.seqs; b0 += THREADS) {
+                const int64_t n = b0 + tid < a.seqs ? head_blocks(a, G, b0 + tid) * H : 0;
+                int64_t total;
+                const int64_t off = at + scan(n, total);
+                at += total;
+                if (a.seqs <= THREADS) W = at, x = find(W);  // (one round does both)
+                if (x >= off && x < off + n) {
+                    lds.b = b0 + tid;
+                    lds.off = off;
+                }
+            }
+            if (a.seqs <= THREADS) break;
+            W = at;
+            x = find(W);
+        }
+        __syncthreads();
+        if (x < 0 || x >= W) return W;
+        b = __builtin_amdgcn_readfirstlane(lds.b);
+        sequence(a, G);
+        int64_t rest = x - uniform(lds.off), each = 0;
+        int l, e;
+        for (int t = 0; t < tiles; ++t) each += tile_blocks(a, u, rows, G, t, l, e);
+        each = uniform(each);
+        h = __builtin_amdgcn_readfirstlane((int)(rest / each));
+        rest -= (int64_t)h * each;
+        for (tile = 0;; ++tile) {
+            unit(a, G);
+            if (rest < blocks) break;
+            rest -= blocks;
+        }
+        tile = __builtin_amdgcn_readfirstlane(tile);
+        unit(a, G);
+        skip = __builtin_amdgcn_readfirstlane((int)rest);
+        return W;
+    }
+};
+
+// The workgroup's share: x of `end` blocks done, the cursor at the next unit.
+template <int ROWS, int BLK, int THREADS>
+struct Walk {
+    Cursor<ROWS, BLK> c;
+    int64_t x, end;
+    int share;
+    // The keys [first, last) of the unit that the share takes, as `take` blocks.
+    int take, first, last;
+    bool head, whole;  // it starts in the middle of the unit; it holds all of it
+    __device__ void unit_keys() {
+        take = (int)min((int64_t)(c.blocks - c.skip), end - x);
+        head = c.skip > 0;
+        whole = !head && take == c.blocks;
+        first = c.lo + max(c.skip - kUnitCost, 0) * BLK;
+        last = (int)min((int64_t)c.hi, c.lo + (int64_t)max(c.skip + take - kUnitCost, 0) * BLK);
+    }
+    __device__ bool next(const AttnArgs& a, int G) {
+        x += take;
+        if (x >= end) return false;
+        c.next(a, G);
+        return true;
+    }
+    __device__ bool begin(const AttnArgs& a, const Shares& sh, int G, const Parts& ws, typename Cursor<ROWS, BLK>::Scratch& lds) {
+        c.skip = 0;
+        if (sh.groups == 0) {
+            // tiles from the last, which sees the most keys; heads fastest
+            const int units = a.seqs * a.c.kv_heads, at = blockIdx.x / units, unit = blockIdx.x - at * units;
+            c.b = unit / a.c.kv_heads;
+            c.h = unit - c.b * a.c.kv_heads;
+            c.sequence(a, G);
+            c.tile = c.tiles - 1 - at;
+            if (c.tile < 0) return false;
+            c.unit(a, G);
+            share = 0, x = 0, end = c.blocks;
+            return true;
+        }
+        int used = 0;
+        const int64_t W = c.template locate<THREADS>(a, G, lds, [&](int64_t W) {
+            used = sh.used(W);
+            if ((int)blockIdx.x >= used) return W;
+            // neighbouring shares on one die, whose cache they share
+            share = used >= 8 ? (int)(blockIdx.x % 8) * (used / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
+            return share_start(W, used, share);
+        });
+        if ((int)blockIdx.x >= used || W == 0) {
+            if (threadIdx.x == 0) ws.starts[blockIdx.x].W = 0;
+            return false;
+        }
+        x = uniform(share_start(W, used, share));
+        end = uniform(share_start(W, used, share + 1));
+        if (threadIdx.x == 0) ws.starts[share] = Start{W, c.b, c.h, c.tile, c.skip, c.blocks, 0};
+        return x < end;
+    }
 };
 
 template <typename T>
@@ -176,7 +366,7 @@ struct KeyPages {
     int k[2], v[2][TILED ? 1 : 4];
 };
 template <bool TILED>
-__device__ inline void look_up(const Split& sp, const int32_t* table, int kb, int hi, int li, int g, KeyPages<TILED>& to) {
+__device__ inline void look_up(const Shares& sp, const int32_t* table, int kb, int hi, int li, int g, KeyPages<TILED>& to) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         to.k[t] = table[sp.page(min(kb + 16 * t + (TILED ? 0 : li), TILED ? (hi - 1) & ~15 : hi - 1))];
@@ -191,7 +381,7 @@ __device__ inline void look_up(const Split& sp, const int32_t* table, int kb, in
 // only.  (Pieces past head_dim read the row's start: the query is 0 there, and
 // such values are not stored.)
 template <int DP, bool TILED>
-__device__ inline void load_block(const AttnArgs& a, const Split& sp, const KeyPages<TILED>& pages, int h, int kb, int hi,
+__device__ inline void load_block(const AttnArgs& a, const Shares& sp, const KeyPages<TILED>& pages, int h, int kb, int hi,
                                   int li, int g, KeyBlock<DP>& to) {
     constexpr int KB = DP / 4, VB = DP / 16;
     const int H = a.c.kv_heads, D = a.c.head_dim, ps = a.c.page_size;
@@ -241,24 +431,23 @@ __device__ inline void load_block(const AttnArgs& a, const Split& sp, const KeyP
     }
 }
 
+constexpr int kRowsBlock = kRowsWaves * 32;  // keys the workgroup takes at a time
+
 template <typename T, int DP, int TERMS, bool TILED>
-__global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_rows(AttnArgs a, Split sp, Parts ws) {
+__global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void attention_rows(AttnArgs a, Shares sp, Parts ws) {
     constexpr int KB = DP / 4, STEPS = DP / 32, VB = DP / 16;
+    __shared__ float red_m[kRowsWaves][16], red_l[kRowsWaves][16], red_o[kRowsWaves][16][DP + 4];
+    __shared__ typename Cursor<16, kRowsBlock>::Scratch scratch;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, g = lane >> 4;
     const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim;
-    // Units vary fastest, then tiles, then splits: the workgroups that find
-    // keys spread over the chip however the contexts' lengths differ (splits
-    // fastest: 303 instead of XXX us at 32 contexts of 1,000 to 32,000).
-    const int units = a.seqs * H, at = blockIdx.x / units, tiles = gridDim.x / units / sp.count;
-    const int unit = blockIdx.x - at * units, split = at / tiles, tile = at - split * tiles, b = unit / H, h = unit - b * H;
-    const Unit u = unit_of(a, b);
-    const int rows = u.n * G, row0 = tile * 16;
-    if (row0 >= rows) return;
-    int lo, hi;
-    key_range(a, u, row0 / G, (min(row0 + 16, rows) - 1) / G, lo, hi);
-    const int first = (lo & ~31) + split * sp.keys, last = min(hi, first + sp.keys);
-    if (split >= splits_of(sp, lo, hi)) return;
-    const int32_t* table = a.table + b * a.table_stride;
+    Walk<16, kRowsBlock, kRowsWaves * 64> walk;
+    if (!walk.begin(a, sp, G, ws, scratch)) return;
+    for (;;) {
+    const Unit u = walk.c.u;
+    const int h = walk.c.h, rows = walk.c.rows, row0 = walk.c.tile * 16, hi = walk.c.hi;
+    walk.unit_keys();
+    const int first = walk.first, last = walk.last;
+    const int32_t* table = a.table + walk.c.b * a.table_stride;
 
     KeyBlock<DP> kv;
     int kb = first + wave * 32;
@@ -266,7 +455,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_
     if (hi > 0) {
         look_up<TILED>(sp, table, kb, hi, li, g, pages);
         load_block<DP, TILED>(a, sp, pages, h, kb, hi, li, g, kv);
-        look_up<TILED>(sp, table, kb + kRowsWaves * 32, hi, li, g, pages);
+        look_up<TILED>(sp, table, kb + kRowsBlock, hi, li, g, pages);
     }
 
     // this lane's row of queries: values d = g * KB + ...
@@ -308,10 +497,10 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_
     int E = -127;  // exponent of the largest value scale seen so far
 
     while (kb < last) {
-        const int kn = kb + kRowsWaves * 32;
+        const int kn = kb + kRowsBlock;
         KeyBlock<DP> next;
         load_block<DP, TILED>(a, sp, pages, h, kn, hi, li, g, next);
-        look_up<TILED>(sp, table, kn + kRowsWaves * 32, hi, li, g, pages);
+        look_up<TILED>(sp, table, kn + kRowsBlock, hi, li, g, pages);
 
         v4f s[2];
 #pragma unroll
@@ -423,7 +612,6 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_
     l *= 0x1p-14f;
 
     // the waves' parts: o[t][r] is value d = (4 g + r) * VB + t of row li
-    __shared__ float red_m[kRowsWaves][16], red_l[kRowsWaves][16], red_o[kRowsWaves][16][DP + 4];
     if (g == 0) {
         red_m[wave][li] = m;
         red_l[wave][li] = l;
@@ -453,13 +641,16 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : 2) void attention_
             L += red_m[w][rr] == kMinusInf ? red_l[w][rr] : red_l[w][rr] * exp2_fast(red_m[w][rr] - M);
             v += red_o[w][rr][d];
         }
-        if (sp.count == 1) {
+        if (walk.whole) {
             store_row<T>(a, u, h, G, rw, d, L == 0.f ? 0.f : v / L);
         } else {
-            const int64_t part = ((int64_t)unit * ws.rows + rw) * sp.count + split;
+            const int64_t part = ((int64_t)walk.share * 2 + !walk.head) * 16 + rr;
             ws.o[part * D + d] = v;
             if (d == 0) ws.ml[part] = make_float2(M, L);
         }
+    }
+    if (!walk.next(a, G)) break;
+    __syncthreads();  // (the parts in LDS are read)
     }
 }
 
@@ -484,7 +675,7 @@ struct TileShape {
 };
 
 template <typename T, int DP, int TERMS, int NW>
-__global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, Parts ws) {
+__global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp, Parts ws) {
     typedef TileShape<T, DP, TERMS, NW> C;
     constexpr int KT = C::KT, SUB = KT / 32, STEPS = DP / 16, DT = DP / 32;
     typedef typename C::Buffer Buffer;
@@ -493,16 +684,14 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, half = lane >> 5;
     const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim, ps = a.c.page_size;
-    // (order: see attention_rows; the last tiles, which see the most keys, first)
-    const int units = a.seqs * H, at = blockIdx.x / units, tiles = gridDim.x / units / sp.count;
-    const int unit = blockIdx.x - at * units, split = at / tiles, tile = tiles - 1 - (at - split * tiles), b = unit / H, h = unit - b * H;
-    const Unit u = unit_of(a, b);
-    const int rows = u.n * G, row0 = tile * C::ROWS;
-    if (row0 >= rows) return;
-    int lo, hi;
-    key_range(a, u, row0 / G, (min(row0 + C::ROWS, rows) - 1) / G, lo, hi);
-    if (split >= splits_of(sp, lo, hi)) return;
-    const int first = (lo & ~31) + split * sp.keys, last = min(hi, first + sp.keys);
+    Walk<C::ROWS, KT, C::THREADS> walk;
+    if (!walk.begin(a, sp, G, ws, *reinterpret_cast<typename Cursor<C::ROWS, KT>::Scratch*>(lds))) return;
+    __syncthreads();  // (the scratch lies where the tiles will)
+    for (;;) {
+    const Unit u = walk.c.u;
+    const int h = walk.c.h, rows = walk.c.rows, row0 = walk.c.tile * C::ROWS, hi = walk.c.hi;
+    walk.unit_keys();
+    const int first = walk.first, last = walk.last;
 
     // this lane's row of queries; the positions of its wave's rows
     const int wrow = row0 + wave * 32, row = wrow + li;
@@ -536,7 +725,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
     }
 
     // the tiles' way into LDS: 16 bytes of a key and of a value a thread and load
-    const int32_t* table = a.table + b * a.table_stride;
+    const int32_t* table = a.table + walk.c.b * a.table_stride;
     int pg[C::LOADS], spg = 0;
     u4 kr[C::LOADS], vr[C::LOADS];
     float ksr = 0.f, vsr = 0.f;
@@ -752,13 +941,10 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
             at_buf ^= 1;
         }
     }
-    if (!live) return;
     l += __shfl_xor(l, 32, 64);
-    const float M = m == kMinusInf ? kMinusInf : m * fq;
-    const int rw = row;
-    if (sp.count == 1) {
+    if (live && walk.whole) {
         const float f = l == 0.f ? 0.f : 512.f / l;
-        const int hq = h * G + rw - tok * G;
+        const int hq = h * G + row - tok * G;
         T* out = static_cast<T*>(a.out) + (int64_t)(u.first + tok) * a.ots + (int64_t)hq * a.ohs + 4 * half;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -767,8 +953,8 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
                 if (32 * d + 8 * g >= D) continue;
                 store4(out + 32 * d + 8 * g, v4f{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]} * f);
             }
-    } else {
-        const int64_t part = ((int64_t)unit * ws.rows + rw) * sp.count + split;
+    } else if (live) {
+        const int64_t part = ((int64_t)walk.share * 2 + !walk.head) * C::ROWS + wave * 32 + li;
         float* out = ws.o + part * D + 4 * half;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -780,51 +966,54 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Split sp, 
                 for (int i = 0; i < 4; ++i) v[i] = ldexpf(o[d][4 * g + i], E - 14 + 9);
                 *reinterpret_cast<v4f*>(out + 32 * d + 8 * g) = v;
             }
-        if (half == 0) ws.ml[part] = make_float2(M, ldexpf(l, E - 14));
+        if (half == 0) ws.ml[part] = make_float2(m == kMinusInf ? kMinusInf : m * fq, ldexpf(l, E - 14));
     }
+    if (!walk.next(a, G)) break;
+    }  // (the tiles' last barrier lies behind every read of LDS)
 }
 
-// The parts of a row, joined by WAVES waves in turn.  `tile`: rows that shared a
-// range of keys.
-template <typename T, int WAVES>
-__global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Parts ws, int tile) {
+// The parts of the unit in which share j starts, if it is the first to start in
+// it: workgroup (j - 1, y) joins rows 4 y .. of the tile, a wave a row, or with
+// WAVES = 4 row y, its waves taking the parts in turn.
+template <typename T, int ROWS, int WAVES>
+__global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Parts ws) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turn = wave % WAVES;
-    const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim;
-    const int64_t at = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
-    const int unit = (int)(at / ws.rows), row = (int)(at - (int64_t)unit * ws.rows);
-    if (unit >= a.seqs * H) return;  // (with four waves a row: all of them)
-    const int b = unit / H, h = unit - b * H;
-    const Unit u = unit_of(a, b);
-    const int rows = u.n * G;
-    if (row >= rows) return;
-    const int row0 = row / tile * tile;
-    int lo, hi;
-    key_range(a, u, row0 / G, (min(row0 + tile, rows) - 1) / G, lo, hi);
-    const int count = splits_of(sp, lo, hi);
-    const float2* ml = ws.ml + at * sp.count;
-    const float* o = ws.o + at * sp.count * D;
+    const int G = a.q_heads / a.c.kv_heads, D = a.c.head_dim, j = blockIdx.x + 1;
+    const Start at = ws.starts[j];
+    if (at.W == 0 || at.skip == 0) return;
+    const int64_t W = at.W;
+    const int used = sh.used(W);
+    const int64_t x0 = share_start(W, used, j) - at.skip;
+    if (x0 < share_start(W, used, j - 1)) return;
+    // parts: the end of share j - 1, the starts of shares j .. j + count - 2
+    int count = 2;
+    while (j + count - 1 < used && share_start(W, used, j + count - 1) < x0 + at.blocks) ++count;
+    const int rr = blockIdx.y * (4 / WAVES) + wave / WAVES, row = at.tile * ROWS + rr;
+    const Unit u = unit_of(a, at.b);
+    if (row >= u.n * G) return;  // (with four waves a row: all of them)
+    auto part = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0)) * ROWS + rr; };
     float M = kMinusInf, L = 0.f;
-    for (int s = lane; s < count; s += 64) M = fmaxf(M, ml[s].x);
+    for (int i = lane; i < count; i += 64) M = fmaxf(M, ws.ml[part(i)].x);
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
     auto factor = [&](float m) { return m == kMinusInf ? 1.f : exp2_fast(m - M); };  // (a part that saw nothing, or a NaN)
-    for (int s = lane; s < count; s += 64) L += ml[s].y * factor(ml[s].x);
+    for (int i = lane; i < count; i += 64) L += ws.ml[part(i)].y * factor(ws.ml[part(i)].x);
     L = lanes_sum(L);
     float v[4] = {0, 0, 0, 0};
-    for (int s0 = 0; s0 < count; s0 += 64 * WAVES) {
-        const int mine = s0 + lane * WAVES + turn;  // this lane's part; part i of the wave is lane i's
-        const float f = mine < count ? factor(ml[mine].x) : 0.f;
-        const int parts = min(64, (count - s0 - turn + WAVES - 1) / WAVES);
-        for (int i = 0; i < parts; i += 4) {  // (past the last: the last, times 0)
+    for (int i0 = 0; i0 < count; i0 += 64 * WAVES) {
+        const int mine = i0 + lane * WAVES + turn;  // this lane's part
+        const float f = mine < count ? factor(ws.ml[part(mine)].x) : 0.f;
+        const int parts = min(64, (count - i0 - turn + WAVES - 1) / WAVES);
+        for (int i = 0; i < parts; i += 4) {  // (past the last: the last, not added)
             float w[4][4];
 #pragma unroll
             for (int y = 0; y < 4; ++y)
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
-                    w[y][x] = o[(int64_t)(s0 + min(i + y, parts - 1) * WAVES + turn) * D + min(lane + 64 * x, D - 1)];
+                    w[y][x] = ws.o[part(i0 + min(i + y, parts - 1) * WAVES + turn) * D + min(lane + 64 * x, D - 1)];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                const float fi = i + y < parts ? __shfl(f, min(i + y, 63), 64) : 0.f;
+                const float fi = __shfl(f, min(i + y, 63), 64);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) v[x] += i + y < parts ? w[y][x] * fi : 0.f;
             }
@@ -843,7 +1032,7 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Split sp, Part
     }
 #pragma unroll
     for (int x = 0; x < 4; ++x)
-        if (lane + 64 * x < D) store_row<T>(a, u, h, G, row, lane + 64 * x, L == 0.f ? 0.f : v[x] / L);
+        if (lane + 64 * x < D) store_row<T>(a, u, at.h, G, row, lane + 64 * x, L == 0.f ? 0.f : v[x] / L);
 }
 
 // Rows a workgroup takes: one token's heads, or up to 16 rows, go to the
@@ -856,33 +1045,30 @@ int tile_rows(const AttnArgs& a) {
     return 256;
 }
 
-// Enough workgroups for the chip from splits of at least 256 keys.
-Split choose_split(const AttnArgs& a) {
+// As many shares as the chip holds workgroups at a time.  Units of up to four
+// blocks are not worth cutting (a join is a launch of its own).
+Shares choose_shares(const AttnArgs& a) {
     const int tile = tile_rows(a), G = a.q_heads / a.c.kv_heads;
-    const int64_t tiles = ((int64_t)a.max_chunk * G + tile - 1) / tile;
-    const int64_t groups = tiles * a.seqs * a.c.kv_heads;
     int64_t range = a.max_context;
     if (a.window) range = std::min<int64_t>(range, (int64_t)a.window + (tile + G - 1) / G + 33);
-    const int64_t want = std::max<int64_t>(1, (tile == 16 ? 8192 : 512) / groups);
-    const int64_t keys = std::max<int64_t>(256, (range / want + 127) / 128 * 128);
-    Split sp;
-    sp.count = (int)((range + 31 + keys - 1) / keys);
-    sp.keys = (int)keys;
+    Shares sh;
+    if (range <= 512)
+        sh.groups = 0;
+    else if (tile == 16)
+        sh.groups = a.c.head_dim <= 64 ? 768 : a.c.head_dim <= 128 ? 512 : 256;
+    else
+        sh.groups = tile == 64 ? 512 : 256;
     const int log = ilog2(a.c.page_size);
-    sp.page_mul = (uint32_t)((1ull << (31 + log)) / (uint32_t)a.c.page_size + 1);
-    sp.page_shift = 31 + log;
-    return sp;
+    sh.page_mul = (uint32_t)((1ull << (31 + log)) / (uint32_t)a.c.page_size + 1);
+    sh.page_shift = 31 + log;
+    return sh;
 }
 
-size_t parts_floats(const AttnArgs& a, const Split& sp, int64_t* o_floats) {
-    const int64_t rows = (int64_t)a.seqs * a.c.kv_heads * a.max_chunk * (a.q_heads / a.c.kv_heads);
-    *o_floats = rows * sp.count * a.c.head_dim;
-    return (size_t)(*o_floats + 4 + rows * sp.count * 2);
-}
+int64_t part_rows(const AttnArgs& a, const Shares& sh) { return (int64_t)sh.groups * 2 * tile_rows(a); }
 
 template <typename T, int DP, int TERMS, int NW>
-hipError_t launch_tile(const AttnArgs& a, const Split& sp, const Parts& p, unsigned blocks, hipStream_t st) {
-    constexpr int bytes = TileShape<T, DP, TERMS, NW>::BYTES;
+hipError_t launch_tile(const AttnArgs& a, const Shares& sh, const Parts& p, unsigned blocks, hipStream_t st) {
+    typedef TileShape<T, DP, TERMS, NW> C;
     // (more LDS than a kernel gets unasked; set once per device)
     static std::atomic<uint64_t> asked{0};
     int dev = 0;
@@ -890,42 +1076,36 @@ hipError_t launch_tile(const AttnArgs& a, const Split& sp, const Parts& p, unsig
     if (e != hipSuccess) return e;
     if (dev < 0 || dev >= 64 || !(asked.load() >> dev & 1)) {
         e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_tile<T, DP, TERMS, NW>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                                hipFuncAttributeMaxDynamicSharedMemorySize, C::BYTES);
         if (e != hipSuccess) return e;
         if (dev >= 0 && dev < 64) asked.fetch_or(1ull << dev);
     }
-    hipLaunchKernelGGL((attention_tile<T, DP, TERMS, NW>), dim3(blocks), dim3(NW * 64), bytes, st, a, sp, p);
+    hipLaunchKernelGGL((attention_tile<T, DP, TERMS, NW>), dim3(blocks), dim3(NW * 64), C::BYTES, st, a, sh, p);
+    e = hipGetLastError();
+    if (e != hipSuccess || sh.groups < 2) return e;
+    hipLaunchKernelGGL((attention_join<T, C::ROWS, 1>), dim3(sh.groups - 1, C::ROWS / 4), dim3(256), 0, st, a, sh, p);
     return hipGetLastError();
 }
 
 template <typename T, int DP, int TERMS>
 hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
-    const Split sp = choose_split(a);
+    const Shares sh = choose_shares(a);
     const int G = a.q_heads / a.c.kv_heads, tile = tile_rows(a);
-    int64_t of;
-    parts_floats(a, sp, &of);
-    const Parts p{ws, reinterpret_cast<float2*>(ws + (of + 3) / 4 * 4), a.max_chunk * G};
-    const unsigned blocks = (unsigned)((((int64_t)a.max_chunk * G + tile - 1) / tile) * a.seqs * a.c.kv_heads * sp.count);
-    hipError_t e;
-    if (tile == 16) {
-        if (a.c.page_size % 16 == 0)
-            hipLaunchKernelGGL((attention_rows<T, DP, TERMS, true>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sp, p);
-        else
-            hipLaunchKernelGGL((attention_rows<T, DP, TERMS, false>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sp, p);
-        e = hipGetLastError();
-    } else if (tile == 64) {
-        e = launch_tile<T, DP, TERMS, 2>(a, sp, p, blocks, st);
-    } else if (DP == 256 || tile == 128) {
-        e = launch_tile<T, DP, TERMS, 4>(a, sp, p, blocks, st);
-    } else {
-        e = launch_tile<T, DP, TERMS, DP == 256 ? 4 : 8>(a, sp, p, blocks, st);
-    }
-    if (e != hipSuccess || sp.count == 1) return e;
-    const int64_t rows = (int64_t)a.seqs * a.c.kv_heads * p.rows;
-    if (sp.count > 4)
-        hipLaunchKernelGGL((attention_join<T, 4>), dim3((unsigned)rows), dim3(256), 0, st, a, sp, p, tile);
+    const int64_t n = part_rows(a, sh);
+    const Parts p{ws, reinterpret_cast<float2*>(ws + n * a.c.head_dim), reinterpret_cast<Start*>(ws + n * (a.c.head_dim + 2))};
+    const int64_t units = (((int64_t)a.max_chunk * G + tile - 1) / tile) * a.seqs * a.c.kv_heads;
+    const unsigned blocks = (unsigned)(sh.groups ? sh.groups : units);
+    if (tile == 64) return launch_tile<T, DP, TERMS, 2>(a, sh, p, blocks, st);
+    if (tile == 128) return launch_tile<T, DP, TERMS, 4>(a, sh, p, blocks, st);
+    if constexpr (DP <= 128)
+        if (tile == 256) return launch_tile<T, DP, TERMS, 8>(a, sh, p, blocks, st);
+    if (a.c.page_size % 16 == 0)
+        hipLaunchKernelGGL((attention_rows<T, DP, TERMS, true>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
     else
-        hipLaunchKernelGGL((attention_join<T, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, sp, p, tile);
+        hipLaunchKernelGGL((attention_rows<T, DP, TERMS, false>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || sh.groups < 2) return e;
+    hipLaunchKernelGGL((attention_join<T, 16, 4>), dim3(sh.groups - 1, std::min(16, a.max_chunk * G)), dim3(256), 0, st, a, sh, p);
     return hipGetLastError();
 }
 
@@ -939,9 +1119,8 @@ hipError_t by_dim(const AttnArgs& a, float* ws, hipStream_t st) {
 }  // namespace
 
 size_t attention_workspace(int, const AttnArgs& a) {
-    const Split sp = choose_split(a);
-    int64_t of;
-    return sp.count == 1 ? 0 : parts_floats(a, sp, &of) * sizeof(float);
+    const Shares sh = choose_shares(a);
+    return part_rows(a, sh) * (a.c.head_dim + 2) * sizeof(float) + sh.groups * sizeof(Start);
 }
 
 hipError_t launch_attention(int dtype, const AttnArgs& a, float* ws, hipStream_t st) {
