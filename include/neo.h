@@ -737,7 +737,7 @@ int neo_matmul_int8(const int8_t* xq, int64_t xq_stride, const float* x_scale, i
  * head_dim keys k[((p * kv_heads + h) * page_size + o) * head_dim ...] and the
  * scale k_scale[(p * kv_heads + h) * page_size + o]; values likewise.  All
  * device memory, k and v 16-byte aligned; offsets are 64-bit.  head_dim is a
- * multiple of 16 up to 256; page_size any.
+ * multiple of 16 up to 256; page_size any, a page's keys below 2 GiB.
  */
 typedef struct neo_kv_cache {
     int8_t* k;

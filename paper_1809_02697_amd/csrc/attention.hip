@@ -13,7 +13,7 @@
 // float16 and bfloat16 queries are exact too (values 2^-28 of the largest and
 // less lose bits); a float32 query is the sum of two fp16 terms.  The weights
 // w_ij are scaled by 2^(14 - E), E the exponent of the largest vs that the row
-// has seen so far, and rounded to fp16 (float32: two terms; Levels below).
+// has seen so far, and rounded to fp16 (float32: two terms; Weights below).
 //
 // S^T = K Q^T and O^T = V^T P^T: the accumulator's layout of S^T (a lane holds
 // four neighbouring keys of one row) is the layout of the second product's
@@ -29,6 +29,7 @@ namespace {
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -77,33 +78,36 @@ __device__ inline int exponent(uint32_t bits) { return (int)(bits >> 23) - 127; 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Weights in fp16.  A term holds 11 bits from fp16's least normal number 2^-14
-// up, two terms hold 22 from 2^-3 up; smaller weights (of keys whose scores lie
-// far below the row's largest) are taken in further passes, scaled up by `step`
-// each, so that every weight keeps its bits: a position at which the largest
-// keys' values are 0 is the sum of the small ones.
+// up, two terms hold 22 from 2^-3 up.  Smaller weights (of keys whose scores lie
+// far below the row's largest) are taken apart and multiplied in bf16, which
+// has float32's range, as two terms of 8 bits (three), so that every weight
+// keeps its bits: a position at which the largest keys' values are 0 is the sum
+// of the small ones.
 template <int TERMS>
-struct Levels {
-    static constexpr float least = TERMS == 1 ? 0x1p-14f : 0x1p-3f, step = TERMS == 1 ? 0x1p28f : 0x1p17f;
+struct Weights {
+    static constexpr float least = TERMS == 1 ? 0x1p-14f : 0x1p-3f;
+    static constexpr int SMALL = TERMS + 1;
     __device__ static void terms(const f32x8& v, h8 (&w)[TERMS]) {
         w[0] = __builtin_convertvector(v, h8);
         if constexpr (TERMS == 2) w[1] = __builtin_convertvector(v - __builtin_convertvector(w[0], f32x8), h8);
     }
-    // The terms of the weights from `least` up; the others scaled for the next
-    // pass.  Returns whether any is left.
-    __device__ static bool take(f32x8& v, h8 (&w)[TERMS]) {
-        f32x8 now;
-        bool left = false;
+    // The small ones among v as bf16 terms; v keeps the others.
+    __device__ static void take_small(f32x8& v, b8 (&w)[SMALL]) {
+        f32x8 rest;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bool later = v[i] < least;  // (a NaN goes now)
-            now[i] = later ? 0.f : v[i];
-            v[i] = later ? v[i] * step : 0.f;
-            left |= v[i] != 0.f;
+            const bool later = v[i] < least;  // (a NaN stays)
+            rest[i] = later ? v[i] : 0.f;
+            v[i] = later ? 0.f : v[i];
         }
-        terms(now, w);
-        return left;
+#pragma unroll
+        for (int t = 0; t < SMALL; ++t) {
+            w[t] = __builtin_convertvector(rest, b8);
+            rest -= __builtin_convertvector(w[t], f32x8);
+        }
     }
 };
+__device__ inline b8 to_bf16(h8 v) { return __builtin_convertvector(__builtin_convertvector(v, f32x8), b8); }
 
 // ---- a unit's tokens -----------------------------------------------------------------
 struct Unit {
@@ -398,7 +402,7 @@ __device__ inline void load_block(const AttnArgs& a, const Shares& sp, const Key
             const int key = min(kb + 16 * t, (hi - 1) & ~15), pg = sp.page(key), page = pages.k[t];
             const bool there = (uint32_t)page < (uint32_t)a.c.pages;
             to.there |= there ? 0xfu << (4 * t) : 0u;
-            const int64_t e = ((int64_t)(there ? page : 0) * H + h) * ps + (key - pg * ps);
+            const uint64_t e = (uint64_t)(uint32_t)(there ? page : 0) * (uint32_t)(H * ps) + (uint32_t)(h * ps + key - pg * ps);
             const int8_t *k = a.c.k + e * D, *v = a.c.v + e * D;
             to.ks[t] = *reinterpret_cast<const loose4*>(a.c.k_scale + e + 4 * g);
             to.vs[t] = *reinterpret_cast<const loose4*>(a.c.v_scale + e + 4 * g);
@@ -412,7 +416,7 @@ __device__ inline void load_block(const AttnArgs& a, const Shares& sp, const Key
             auto entry = [&](int j, int page, bool& there) {
                 const int key = min(j, hi - 1), pg = sp.page(key);
                 there = (uint32_t)page < (uint32_t)a.c.pages;
-                return ((int64_t)(there ? page : 0) * H + h) * ps + (key - pg * ps);
+                return (uint64_t)(uint32_t)(there ? page : 0) * (uint32_t)(H * ps) + (uint32_t)(h * ps + key - pg * ps);
             };
             bool there;
             const int8_t* k = a.c.k + entry(kb + 16 * t + li, pages.k[t], there) * D;
@@ -420,7 +424,7 @@ __device__ inline void load_block(const AttnArgs& a, const Shares& sp, const Key
             for (int c = 0; c < KB / 16; ++c) to.k[t][c] = *reinterpret_cast<const u4*>(k + koff[c]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int64_t e = entry(kb + 16 * t + 4 * g + r, pages.v[t][r], there);
+                const uint64_t e = entry(kb + 16 * t + 4 * g + r, pages.v[t][r], there);
                 to.there |= there ? 1u << (4 * t + r) : 0u;
                 to.ks[t][r] = a.c.k_scale[e];
                 to.vs[t][r] = a.c.v_scale[e];
@@ -567,7 +571,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
                 const float p = exp2_fast(s[t][r] - lift);
                 l += p;
                 pv[4 * t + r] = p * ldexpf(kv.vs[t][r], -E);
-                small |= pv[4 * t + r] != 0.f && pv[4 * t + r] < Levels<TERMS>::least;
+                small |= pv[4 * t + r] != 0.f && pv[4 * t + r] < Weights<TERMS>::least;
             }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -581,28 +585,27 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
                         pair(kv.v[1][0][c], kv.v[1][1][c], y), pair(kv.v[1][2][c], kv.v[1][3][c], y));
         };
         h8 w[TERMS];
-        if (!__any(small)) {
-            Levels<TERMS>::terms(pv, w);
+        if (__any(small)) {
+            b8 ws[Weights<TERMS>::SMALL];
+            Weights<TERMS>::take_small(pv, ws);
 #pragma unroll
             for (int t = 0; t < VB; ++t) {
-                const h8 v = values(t);
+                const b8 v = to_bf16(values(t));
 #pragma unroll
-                for (int i = 0; i < TERMS; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], o[t], 0, 0, 0);
+                for (int i = 0; i < Weights<TERMS>::SMALL; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ws[i], o[t], 0, 0, 0);
             }
-        } else {
-            float down = 1.f;
-            do {
-                small = Levels<TERMS>::take(pv, w);
+            // (converted anew below: kept, the values would take registers from the common case)
 #pragma unroll
-                for (int t = 0; t < VB; ++t) {
-                    const h8 v = values(t);
-                    v4f z = {0, 0, 0, 0};
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
-                    for (int i = 0; i < TERMS; ++i) z = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], z, 0, 0, 0);
-                    o[t] += z * down;
-                }
-                down *= 1.f / Levels<TERMS>::step;
-            } while (__any(small));
+                for (int c = 0; c < VB / 4; ++c) asm volatile("" : "+v"(kv.v[i / 4][i % 4][c]));
+        }
+        Weights<TERMS>::terms(pv, w);
+#pragma unroll
+        for (int t = 0; t < VB; ++t) {
+            const h8 v = values(t);
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], o[t], 0, 0, 0);
         }
         kv = next;
         kb = kn;
@@ -682,7 +685,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
     extern __shared__ __align__(512) char lds[];
     Buffer* buf = reinterpret_cast<Buffer*>(lds);
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 31, half = lane >> 5;
     const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim, ps = a.c.page_size;
     Walk<C::ROWS, KT, C::THREADS> walk;
     if (!walk.begin(a, sp, G, ws, *reinterpret_cast<typename Cursor<C::ROWS, KT>::Scratch*>(lds))) return;
@@ -742,13 +745,14 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
         for (int i = 0; i < C::LOADS; ++i) {
             const int x = tid + i * C::THREADS, c = x % C::CH, key = min(k0 + x / C::CH, hi - 1);
             const int page = (uint32_t)pg[i] < (uint32_t)a.c.pages ? pg[i] : 0;
-            const int64_t e = (((int64_t)page * H + h) * ps + (key - sp.page(key) * ps)) * D + (c * 16 < D ? c * 16 : 0);
+            const uint64_t e = (uint64_t)(uint32_t)page * (uint32_t)(H * ps * D) +
+                               (uint32_t)((h * ps + key - sp.page(key) * ps) * D + (c * 16 < D ? c * 16 : 0));
             kr[i] = *reinterpret_cast<const u4*>(a.c.k + e);
             vr[i] = *reinterpret_cast<const u4*>(a.c.v + e);
         }
         const int key = min(k0 + tid % KT, hi - 1);
         hid = (uint32_t)spg >= (uint32_t)a.c.pages;
-        const int64_t e = ((int64_t)(hid ? 0 : spg) * H + h) * ps + (key - sp.page(key) * ps);
+        const uint64_t e = (uint64_t)(uint32_t)(hid ? 0 : spg) * (uint32_t)(H * ps) + (uint32_t)(h * ps + key - sp.page(key) * ps);
         ksr = a.c.k_scale[e];
         vsr = a.c.v_scale[e];
     };
@@ -809,7 +813,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        const unsigned long long hidden = from.hidden;
+        const uint64_t hidden = (uint64_t)uniform((int64_t)from.hidden);
         const bool all = k0 + KT - 1 <= pos_lo && k0 + KT <= last && hidden == 0 && (!a.window || k0 > pos_hi - a.window);
         auto scales = [&](const float* p, int t, int g) { return *reinterpret_cast<const v4f*>(p + 32 * t + 8 * g + 4 * half); };
 #pragma unroll
@@ -820,7 +824,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[t][4 * g + i] *= ks[i];
             }
-        int En = max(E, min(from.top, 126));
+        int En = max(E, __builtin_amdgcn_readfirstlane(min(from.top, 126)));
         if (!all) {
             // this lane's keys k0 + 4 half + x: seen from x = from_x up to to_x
             const int j0 = k0 + 4 * half, to_x = live ? min(pos, last - 1) - j0 : -1;
@@ -887,39 +891,41 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             const h4 y0 = read_transposed(p), y1 = read_transposed(p + 8 * C::VSTRIDE);
             return h8{y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
         };
-        const bool small = __any(least < Levels<TERMS>::least);
+        if (__any(least < Weights<TERMS>::least)) {
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    f32x8 pv;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pv[i] = s[t][8 * x + i];
+                    b8 w[Weights<TERMS>::SMALL];
+                    Weights<TERMS>::take_small(pv, w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[t][8 * x + i] = pv[i];
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const b8 v = to_bf16(values(t, x, d));
+#pragma unroll
+                        for (int i = 0; i < Weights<TERMS>::SMALL; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[i], o[d], 0, 0, 0);
+                        asm volatile("" ::: "memory");  // (the values are read again below: kept, they would take its registers)
+                    }
+                }
+        }
 #pragma unroll
         for (int t = 0; t < SUB; ++t)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                __builtin_amdgcn_sched_barrier(0);  // (reads of later groups would take registers from the accumulators)
                 f32x8 pv;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) pv[i] = s[t][8 * x + i];
                 h8 w[TERMS];
-                if (!small) {
-                    Levels<TERMS>::terms(pv, w);
+                Weights<TERMS>::terms(pv, w);
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const h8 v = values(t, x, d);
+                for (int d = 0; d < DT; ++d) {
+                    const h8 v = values(t, x, d);
 #pragma unroll
-                        for (int i = 0; i < TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[i], o[d], 0, 0, 0);
-                    }
-                } else {
-                    float down = 1.f;
-                    bool more;
-                    do {
-                        more = Levels<TERMS>::take(pv, w);
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            const h8 v = values(t, x, d);
-                            f32x16 z = {0};
-#pragma unroll
-                            for (int i = 0; i < TERMS; ++i) z = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[i], z, 0, 0, 0);
-                            o[d] += z * down;
-                        }
-                        down *= 1.f / Levels<TERMS>::step;
-                    } while (__any(more));
+                    for (int i = 0; i < TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[i], o[d], 0, 0, 0);
                 }
             }
     };

@@ -66,6 +66,8 @@ bool check_cache(Check& c, const neo_kv_cache* k) {
     c.size(k->head_dim, "cache.head_dim", 1);
     if (c.rc == NEO_OK && (k->head_dim % 16 || k->head_dim > 256))
         c.bad(NEO_ERR_UNSUPPORTED, "cache.head_dim must be a multiple of 16 up to 256");
+    if (c.rc == NEO_OK && (int64_t)k->kv_heads * k->head_dim > (int64_t)0x7fffffff / k->page_size)
+        c.bad(NEO_ERR_UNSUPPORTED, "cache: a page of 2 GiB or more");
     c.ptr(k->k, "cache.k") && c.aligned(k->k, "cache.k", 16);
     c.ptr(k->v, "cache.v") && c.aligned(k->v, "cache.v", 16);
     c.ptr(k->k_scale, "cache.k_scale") && c.aligned(k->k_scale, "cache.k_scale", 4);

@@ -96,7 +96,7 @@ def _struct(**over):
 
 
 BAD_CACHES = [(dict(k=None), -1), (dict(v_scale=None), -1), (dict(pages=0), -1), (dict(kv_heads=0), -1), (dict(page_size=0), -1),
-              (dict(head_dim=0), -1), (dict(head_dim=72), -4), (dict(head_dim=272), -4), (dict(k=(1 << 20) + 8), -3),
+              (dict(head_dim=0), -1), (dict(head_dim=72), -4), (dict(head_dim=272), -4), (dict(page_size=1 << 24), -4), (dict(k=(1 << 20) + 8), -3),
               (dict(v=(1 << 20) + 8), -3), (dict(k_scale=(1 << 20) + 2), -3)]
 
 
