@@ -23,7 +23,8 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # Per-source additions.  The integer kernels keep their MFMA accumulators in
 # ordinary VGPRs: with the default AGPR form the compiler rotated them through
 # accumulator-register copies inside the reduction loop (v_accvgpr_mov).
-SOURCE_FLAGS = {"conv_int8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+SOURCE_FLAGS = {"conv_int8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+                "matmul_int8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _compile(src, objdir):

@@ -46,13 +46,6 @@ __device__ inline h4 read_transposed(const _Float16* p) {
     return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p));
 }
 
-template <typename T>
-__device__ inline void store4(T* p, v4f v) {
-    typedef T raw __attribute__((ext_vector_type(4)));
-    typedef T loose __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    *reinterpret_cast<loose*>(p) = __builtin_convertvector(v, raw);
-}
-
 // ---- int8 to fp16 ------------------------------------------------------------------------
 // A byte v + 128 (the sign bit flipped) under a zero byte is the fp16 number
 // (v + 128) 2^-24; times 2^15, minus 2^-2, it is v 2^-9, exactly.
@@ -674,7 +667,9 @@ struct TileShape {
         int top;                    // exponent of the largest value scale
     };
     static constexpr int BYTES = 2 * sizeof(Buffer);
-    static constexpr int MASK = CH * 2 < 16 ? CH * 2 - 1 : 15;
+    // A key row's 16-byte pieces are exchanged by xor with turn(key), so that 16
+    // keys, which LDS reads at once, lie in all banks (rows of 128 bytes: two a turn).
+    __device__ static int turn(int key) { return CH * 2 < 16 ? key >> 1 & 7 : key & 15; }
 };
 
 template <typename T, int DP, int TERMS, int NW>
@@ -766,7 +761,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
                 h2 x0, x1, x2, x3;
                 unpack4(biased(kr[i][2 * o]), x0, x1);
                 unpack4(biased(kr[i][2 * o + 1]), x2, x3);
-                *reinterpret_cast<h8*>(to.k + key * C::KSTRIDE + ((2 * c + o) ^ (key & C::MASK)) * 8) = join(x0, x1, x2, x3);
+                *reinterpret_cast<h8*>(to.k + key * C::KSTRIDE + ((2 * c + o) ^ C::turn(key)) * 8) = join(x0, x1, x2, x3);
             }
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
@@ -800,7 +795,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
         f32x16 s[SUB];
         // byte address of this lane's piece 0 of key li; piece c is that xor 32 c
         uint32_t kaddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)reinterpret_cast<const char*>(from.k) +
-                         li * (2 * C::KSTRIDE) + ((half ^ (li & C::MASK)) * 16);
+                         li * (2 * C::KSTRIDE) + ((half ^ C::turn(li)) * 16);
         asm volatile("" : "+v"(kaddr));  // (kept in one register, not in one for every c)
 #pragma unroll
         for (int t = 0; t < SUB; ++t) {

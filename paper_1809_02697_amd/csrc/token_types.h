@@ -31,6 +31,12 @@ __device__ inline void store8(T* p, f32x8 v) {
     typedef T raw __attribute__((ext_vector_type(8)));
     *reinterpret_cast<typename Vec8<T>::type*>(p) = __builtin_convertvector(v, raw);
 }
+template <typename T>
+__device__ inline void store4(T* p, v4f v) {
+    typedef T raw __attribute__((ext_vector_type(4)));
+    typedef T loose __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    *reinterpret_cast<loose*>(p) = __builtin_convertvector(v, raw);
+}
 // The first n (0 .. 8) of them; the rest read as zero, are not touched.
 template <typename T>
 __device__ inline f32x8 load8(const T* p, int n) {

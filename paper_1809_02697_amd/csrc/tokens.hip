@@ -144,6 +144,10 @@ template <typename T, int MODE>
 hipError_t dispatch(const RowsArgs& a, hipStream_t st) {
     if (a.cols <= 512) return launch<T, MODE, 1, 1>(a, st);
     if (a.cols <= 2048) return launch<T, MODE, 1, 4>(a, st);
+    if (a.rows <= 512) {  // few rows: more waves on each
+        if (a.cols <= 8192) return launch<T, MODE, 16, 1>(a, st);
+        if (a.cols <= 16384) return launch<T, MODE, 16, 2>(a, st);
+    }
     if (a.cols <= 4096) return launch<T, MODE, 4, 2>(a, st);
     if (a.cols <= 8192) return launch<T, MODE, 4, 4>(a, st);
     if (a.cols <= 16384) return launch<T, MODE, 4, 8>(a, st);
