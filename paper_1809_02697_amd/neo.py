@@ -496,43 +496,49 @@ def kv_cache(pages, kv_heads, page_size, head_dim, device="cuda"):
     return KVCache(*q, *s)
 
 
-_DTYPES = {}   # torch dtype -> enum neo_dtype; filled on first use
+# These calls are a few microseconds of GPU work for a token, so what the
+# binding does around the C entry (3.8 us with its launch) counts: strides are
+# read once as tuples, and outputs are made by new_empty (1.5 us each).
+_DTYPES = {}   # torch dtype -> enum neo_dtype, and the types by name; filled on first use
 
 
 def _dtype(t):
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
     code = _DTYPES.get(t)
     if code is None:
-        raise TypeError(f"{t} is not float32, float16 or bfloat16")
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, "f32": torch.float32, "i8": torch.int8,
+                        "i32": torch.int32, "i64": torch.int64, "bf16": torch.bfloat16})
+        code = _DTYPES.get(t)
+        if code is None:
+            raise TypeError(f"{t} is not float32, float16 or bfloat16")
     return code
 
 
-def _rows(t, name, like=None):
+def _rows(t, rows, cols, dtype, name):
     """A device tensor [rows][cols] of neighbouring elements: (pointer, row stride)."""
+    if t.shape != (rows, cols) or t.dtype != dtype:
+        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, not {(rows, cols)} of {dtype}")
+    s = t.stride()
+    if (s[1] != 1 and cols > 1) or (s[0] < cols and rows > 1):
+        raise ValueError(f"{name} must have neighbouring elements in its rows")
     if not t.is_cuda:
         raise TypeError(f"{name} must be a device (cuda) tensor")
-    if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
-        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, not {tuple(like.shape)} of {like.dtype}")
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name} must be two-dimensional with neighbouring elements in its rows")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+    return t.data_ptr(), (s[0] if s[0] > cols else cols)
 
 
 def _rows8(t, rows, cols, name):
-    """int8 rows [rows][dense_row_bytes(cols)]: (pointer, row stride)."""
-    import torch
-    if t.dtype != torch.int8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < dense_row_bytes(cols):
-        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, not int8 rows {(rows, dense_row_bytes(cols))}")
-    return _rows(t, name)
+    """int8 rows [rows][dense_row_bytes(cols)] (or wider): (pointer, row stride)."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] < dense_row_bytes(cols):
+        raise ValueError(f"{name} is {tuple(shape)}, not int8 rows {(rows, dense_row_bytes(cols))}")
+    return _rows(t, rows, shape[1], _DTYPES["i8"], name)
 
 
 def _vec(t, n, dtype, name):
-    """A device vector of at least n elements."""
+    """A device vector of at least n elements (or None)."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype:
+    if t.dtype != dtype or not t.is_cuda:
         raise TypeError(f"{name} must be a device (cuda) tensor of {dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -541,63 +547,82 @@ def _vec(t, n, dtype, name):
     return t.data_ptr()
 
 
+def _shape2(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be two-dimensional, is {tuple(t.shape)}")
+    return t.shape
+
+
 def rmsnorm_int8(x, gamma, eps=1e-5, residual=None, h=None, y=None, out=None, scale=None, quantize=True, stream=None):
     """Residual addition, root-mean-square norm, quantization: (int8 rows
     [rows][dense_row_bytes(cols)], scales [rows], h).  x [rows][cols] float32,
     float16 or bfloat16; h = x + residual (allocated when residual is given and
-    h is None; h=residual or h=x works in place; h=False leaves it out).  y,
-    when given, receives the norm unquantized; quantize=False leaves the int8
-    rows out."""
-    import torch
-    rows, cols = x.shape
-    xp, xs = _rows(x, "x")
-    rp, rs = (None, 0) if residual is None else _rows(residual, "residual", x)
-    if h is None and residual is not None:
-        h = torch.empty((rows, cols), device=x.device, dtype=x.dtype)
-    hp, hs = (None, 0) if h is None or h is False else _rows(h, "h", x)
-    yp, ys = (None, 0) if y is None else _rows(y, "y", x)
-    qp, qs, sp = None, 0, None
+    h is None; h=residual or h=x works in place; h=False leaves it out).  gamma
+    float32 [cols] or None.  y, when given, receives the norm unquantized;
+    quantize=False leaves the int8 rows out."""
+    rows, cols = _shape2(x, "x")
+    t = x.dtype
+    code = _dtype(t)
+    f32 = _DTYPES["f32"]
+    xp, xs = _rows(x, rows, cols, t, "x")
+    rp, rs, hp, hs, yp, ys, qp, qs, sp = None, 0, None, 0, None, 0, None, 0, None
+    if residual is not None:
+        rp, rs = _rows(residual, rows, cols, t, "residual")
+        if h is None:
+            h = x.new_empty((rows, cols))
+    if h is not None and h is not False:
+        hp, hs = _rows(h, rows, cols, t, "h")
+    if y is not None:
+        yp, ys = _rows(y, rows, cols, t, "y")
     if quantize:
         if out is None:
-            out = torch.empty((rows, dense_row_bytes(cols)), device=x.device, dtype=torch.int8)
+            qs = dense_row_bytes(cols)
+            out = x.new_empty((rows, qs), dtype=_DTYPES["i8"])
+            qp = out.data_ptr()
+        else:
+            qp, qs = _rows8(out, rows, cols, "out")
         if scale is None:
-            scale = torch.empty(rows, device=x.device, dtype=torch.float32)
-        qp, qs = _rows8(out, rows, cols, "out")
-        sp = _vec(scale, rows, torch.float32, "scale")
-    _check(lib().neo_rmsnorm_int8(xp, xs, rp, rs, _vec(gamma, cols, torch.float32, "gamma"), eps, rows, cols,
-                                  _dtype(x.dtype), hp, hs, yp, ys, qp, qs, sp, _stream(stream)))
+            scale = x.new_empty(rows, dtype=f32)
+        sp = _vec(scale, rows, f32, "scale")
+    _check(lib().neo_rmsnorm_int8(xp, xs, rp, rs, _vec(gamma, cols, f32, "gamma"), eps, rows, cols, code, hp, hs, yp, ys, qp, qs,
+                                  sp, _stream(stream)))
     return out, scale, (None if h is False else h)
 
 
 def quantize_tokens_int8(x, gate=None, out=None, scale=None, stream=None):
     """Rows x [rows][cols], or x * silu(gate), in int8 with a scale each:
     (int8 rows [rows][dense_row_bytes(cols)], scales [rows])."""
-    import torch
-    rows, cols = x.shape
-    xp, xs = _rows(x, "x")
-    gp, gs = (None, 0) if gate is None else _rows(gate, "gate", x)
+    rows, cols = _shape2(x, "x")
+    t = x.dtype
+    code = _dtype(t)
+    f32 = _DTYPES["f32"]
+    xp, xs = _rows(x, rows, cols, t, "x")
+    gp, gs = (None, 0) if gate is None else _rows(gate, rows, cols, t, "gate")
     if out is None:
-        out = torch.empty((rows, dense_row_bytes(cols)), device=x.device, dtype=torch.int8)
+        qs = dense_row_bytes(cols)
+        out = x.new_empty((rows, qs), dtype=_DTYPES["i8"])
+        qp = out.data_ptr()
+    else:
+        qp, qs = _rows8(out, rows, cols, "out")
     if scale is None:
-        scale = torch.empty(rows, device=x.device, dtype=torch.float32)
-    qp, qs = _rows8(out, rows, cols, "out")
-    _check(lib().neo_quantize_tokens_int8(xp, xs, gp, gs, rows, cols, _dtype(x.dtype), qp, qs,
-                                          _vec(scale, rows, torch.float32, "scale"), _stream(stream)))
+        scale = x.new_empty(rows, dtype=f32)
+    _check(lib().neo_quantize_tokens_int8(xp, xs, gp, gs, rows, cols, code, qp, qs, _vec(scale, rows, f32, "scale"),
+                                          _stream(stream)))
     return out, scale
 
 
 def dequantize_tokens_int8(xq, x_scale, cols, dtype, out=None, stream=None):
     """The values [rows][cols] that int8 rows and their scales stand for."""
-    import torch
+    code = _dtype(dtype)
     rows = xq.shape[0]
     qp, qs = _rows8(xq, rows, cols, "xq")
     if out is None:
-        out = torch.empty((rows, cols), device=xq.device, dtype=dtype)
-    elif out.dtype != dtype or tuple(out.shape) != (rows, cols):
-        raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {(rows, cols)} of {dtype}")
-    yp, ys = _rows(out, "out")
-    _check(lib().neo_dequantize_tokens_int8(qp, qs, _vec(x_scale, rows, torch.float32, "x_scale"), rows, cols,
-                                            _dtype(dtype), yp, ys, _stream(stream)))
+        out, ys = xq.new_empty((rows, cols), dtype=dtype), cols
+        yp = out.data_ptr()
+    else:
+        yp, ys = _rows(out, rows, cols, dtype, "out")
+    _check(lib().neo_dequantize_tokens_int8(qp, qs, _vec(x_scale, rows, _DTYPES["f32"], "x_scale"), rows, cols, code, yp, ys,
+                                            _stream(stream)))
     return out
 
 
@@ -605,74 +630,78 @@ def matmul_int8(xq, x_scale, IN, w_rows, w_scale, OUT, bias=None, act="none", dt
     """int8 rows xq [M][dense_row_bytes(IN)] with scales [M] (rmsnorm_int8,
     quantize_tokens_int8) times int8 weight rows with scales [OUT]
     (pack_dense_int8): [M][OUT] of dtype (bfloat16 unless said or out given)."""
-    import torch
+    if dtype is None and out is not None:
+        dtype = out.dtype
+    if dtype is None:
+        import torch
+        dtype = torch.bfloat16
+    code = _dtype(dtype)
+    f32 = _DTYPES["f32"]
     M = xq.shape[0]
     qp, qs = _rows8(xq, M, IN, "xq")
-    if dtype is None:
-        dtype = torch.bfloat16 if out is None else out.dtype
     if out is None:
-        out = torch.empty((M, OUT), device=xq.device, dtype=dtype)
-    elif out.dtype != dtype or tuple(out.shape) != (M, OUT):
-        raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {(M, OUT)} of {dtype}")
-    yp, ys = _rows(out, "out")
-    f32 = torch.float32
+        out, ys = xq.new_empty((M, OUT), dtype=dtype), OUT
+        yp = out.data_ptr()
+    else:
+        yp, ys = _rows(out, M, OUT, dtype, "out")
     _check(lib().neo_matmul_int8(qp, qs, _vec(x_scale, M, f32, "x_scale"), M, IN,
-                                 _vec(w_rows, OUT * dense_row_bytes(IN), torch.int8, "w_rows"),
+                                 _vec(w_rows, OUT * dense_row_bytes(IN), _DTYPES["i8"], "w_rows"),
                                  _vec(w_scale, OUT, f32, "w_scale"), OUT, _vec(bias, OUT, f32, "bias"),
-                                 ACT[act] if isinstance(act, str) else int(act), _dtype(dtype), yp, ys, _stream(stream)))
+                                 ACT[act] if isinstance(act, str) else int(act), code, yp, ys, _stream(stream)))
     return out
 
 
 def _cache(cache):
     """A KVCache (or a tuple of its four tensors) as the C struct."""
-    import torch
     k, v, ks, vs = cache
-    if k.dim() != 4 or v.shape != k.shape or ks.shape != k.shape[:3] or vs.shape != ks.shape:
+    shape = k.shape
+    if len(shape) != 4 or v.shape != shape or ks.shape != shape[:3] or vs.shape != shape[:3]:
         raise ValueError("a cache is k and v [pages][kv_heads][page_size][head_dim] and their scales [pages][kv_heads][page_size]")
-    P, H, page, D = k.shape
-    return KvCacheStruct(_vec(k, 0, torch.int8, "k"), _vec(v, 0, torch.int8, "v"), _vec(ks, 0, torch.float32, "k_scale"),
-                         _vec(vs, 0, torch.float32, "v_scale"), P, H, page, D)
+    i8, f32 = _DTYPES["i8"], _DTYPES["f32"]
+    return KvCacheStruct(_vec(k, 0, i8, "k"), _vec(v, 0, i8, "v"), _vec(ks, 0, f32, "k_scale"), _vec(vs, 0, f32, "v_scale"),
+                         *shape)
 
 
 def _heads(t, heads, dim, name):
     """A device tensor [tokens][heads][dim] of neighbouring dim: (pointer, strides)."""
+    shape, s = t.shape, t.stride()
+    if len(shape) != 3 or (heads is not None and shape[1] != heads) or shape[2] != dim:
+        raise ValueError(f"{name} is {tuple(shape)}, not [tokens][{heads or 'q_heads'}][{dim}]")
+    if s[2] != 1:
+        raise ValueError(f"{name} must have neighbouring elements in its heads")
     if not t.is_cuda:
         raise TypeError(f"{name} must be a device (cuda) tensor")
-    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
-        raise ValueError(f"{name} is {tuple(t.shape)}, not [tokens][{heads or 'q_heads'}][{dim}]")
-    if t.stride(2) != 1:
-        raise ValueError(f"{name} must have neighbouring elements in its heads")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), s[0], s[1]
 
 
 def kv_write_int8(cache, k, v, slots, stream=None):
     """Quantizes k and v [tokens][kv_heads][head_dim] into the cache entries
     slots [tokens] (int64: page * page_size + entry; a slot outside the cache,
     -1 say, skips its token)."""
-    import torch
+    code = _dtype(k.dtype)
     c = _cache(cache)
     if k.dtype != v.dtype or k.shape != v.shape:
         raise ValueError("k and v differ in shape or type")
     T = k.shape[0]
     _check(lib().neo_kv_write_int8(ctypes.byref(c), *_heads(k, c.kv_heads, c.head_dim, "k"),
-                                   *_heads(v, c.kv_heads, c.head_dim, "v"), T, _dtype(k.dtype),
-                                   _vec(slots, T, torch.int64, "slots"), _stream(stream)))
+                                   *_heads(v, c.kv_heads, c.head_dim, "v"), T, code,
+                                   _vec(slots, T, _DTYPES["i64"], "slots"), _stream(stream)))
 
 
 def kv_read_int8(cache, slots, dtype, k_out=None, v_out=None, stream=None):
     """Keys and values [tokens][kv_heads][head_dim] of the entries slots."""
-    import torch
+    code = _dtype(dtype)
     c = _cache(cache)
     T = slots.numel()
     shape = (T, c.kv_heads, c.head_dim)
     outs = []
     for o in (k_out, v_out):
         if o is None:
-            o = torch.empty(shape, device=slots.device, dtype=dtype)
-        elif o.dtype != dtype or tuple(o.shape) != shape:
+            o = slots.new_empty(shape, dtype=dtype)
+        elif o.dtype != dtype or o.shape != shape:
             raise ValueError(f"an output is {tuple(o.shape)} of {o.dtype}, not {shape} of {dtype}")
         outs.append(o)
-    _check(lib().neo_kv_read_int8(ctypes.byref(c), _vec(slots, T, torch.int64, "slots"), T, _dtype(dtype),
+    _check(lib().neo_kv_read_int8(ctypes.byref(c), _vec(slots, T, _DTYPES["i64"], "slots"), T, code,
                                   _vec(outs[0], 0, dtype, "k_out"), _vec(outs[1], 0, dtype, "v_out"), _stream(stream)))
     return tuple(outs)
 
@@ -684,26 +713,27 @@ def attention_paged_int8(cache, q, page_table, context_lens, q_starts, max_chunk
     context_lens int32 [seqs], q_starts int32 [seqs + 1]; max_chunk and
     max_context bound the sequences' new and cached tokens.  scale:
     1 / sqrt(head_dim) unless given; window > 0: each token sees that many."""
-    import torch
+    t = q.dtype
+    code = _dtype(t)
+    i32 = _DTYPES["i32"]
     c = _cache(cache)
     qp, qt, qh = _heads(q, None, c.head_dim, "q")
     T, Hq, D = q.shape
-    if page_table.dim() != 2 or page_table.dtype != torch.int32 or not page_table.is_cuda or \
-            (page_table.stride(1) != 1 and page_table.shape[1] > 1):
-        raise ValueError("page_table must be a device int32 [seqs][pages]")
-    B, most = page_table.shape
+    B, most = _shape2(page_table, "page_table")
+    tp, ts = _rows(page_table, B, most, i32, "page_table")
     if max_context > most * c.page_size:
         raise ValueError(f"max_context {max_context} exceeds the {most} pages a sequence has")
     if out is None:
-        out = torch.empty((T, Hq, D), device=q.device, dtype=q.dtype)
-    elif out.dtype != q.dtype or out.shape != q.shape:
-        raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {tuple(q.shape)} of {q.dtype}")
-    op, ot, oh = _heads(out, Hq, D, "out")
-    i32 = torch.int32
-    _check(lib().neo_attention_paged_int8(ctypes.byref(c), qp, qt, qh, T, Hq, _dtype(q.dtype), page_table.data_ptr(),
-                                          page_table.stride(0) if B > 1 else most, _vec(context_lens, B, i32, "context_lens"),
-                                          _vec(q_starts, B + 1, i32, "q_starts"), B, max_chunk, max_context,
-                                          D ** -0.5 if scale is None else scale, window, op, ot, oh, _stream(stream)))
+        out, ot, oh = q.new_empty((T, Hq, D)), Hq * D, D
+        op = out.data_ptr()
+    else:
+        if out.dtype != t or out.shape != q.shape:
+            raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {tuple(q.shape)} of {t}")
+        op, ot, oh = _heads(out, Hq, D, "out")
+    _check(lib().neo_attention_paged_int8(ctypes.byref(c), qp, qt, qh, T, Hq, code, tp, ts,
+                                          _vec(context_lens, B, i32, "context_lens"), _vec(q_starts, B + 1, i32, "q_starts"), B,
+                                          max_chunk, max_context, D ** -0.5 if scale is None else scale, window, op, ot, oh,
+                                          _stream(stream)))
     return out
 
 
