@@ -1036,24 +1036,27 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Par
         if (lane + 64 * x < D) store_row<T>(a, u, at.h, G, row, lane + 64 * x, L == 0.f ? 0.f : v[x] / L);
 }
 
-// Rows a workgroup takes: one token's heads, or up to 16 rows, go to the
-// kernel for few rows; the tiles grow with the rows a unit has.
+// Rows a workgroup takes.  Up to two tiles of 16 go to the kernel for few rows
+// (8 tokens of 4 heads a unit, 8 sequences of 8192: 61 us against 79 in tiles of
+// 64); the tiles grow with the rows a unit has.
 int tile_rows(const AttnArgs& a) {
     const int64_t rows = (int64_t)a.max_chunk * (a.q_heads / a.c.kv_heads);
-    if (rows <= 16) return 16;
+    if (rows <= 32) return 16;
     if (rows <= 64) return 64;
     if (rows <= 128 || a.c.head_dim > 128) return 128;
     return 256;
 }
 
-// As many shares as the chip holds workgroups at a time.  Units of up to four
-// blocks are not worth cutting (a join is a launch of its own).
+// As many shares as the chip holds workgroups at a time.  Short units are not
+// worth cutting, as a join is a launch of its own: seven float32 tokens of 3
+// heads a unit over 700 tokens take 14 us whole and 20 us cut; 40 tokens over
+// 600 in the tile kernel 29 us cut and 42 whole.
 Shares choose_shares(const AttnArgs& a) {
     const int tile = tile_rows(a), G = a.q_heads / a.c.kv_heads;
     int64_t range = a.max_context;
     if (a.window) range = std::min<int64_t>(range, (int64_t)a.window + (tile + G - 1) / G + 33);
     Shares sh;
-    if (range <= 512)
+    if (range <= (tile == 16 ? 1024 : 256))
         sh.groups = 0;
     else if (tile == 16)
         sh.groups = a.c.head_dim <= 64 ? 768 : a.c.head_dim <= 128 ? 512 : 256;

@@ -18,28 +18,32 @@ __device__ inline int64_t entry_of(const neo_kv_cache& c, int64_t slot, int h) {
     return (page * c.kv_heads + h) * c.page_size + (slot - page * c.page_size);
 }
 
+// A group takes a token's key and value of a head: one lookup of the slot, and
+// two rows' loads under way at once (16,000 tokens x 8 heads of 128 in float16
+// XXX us, 41 with a row a group).
 template <typename T, int LANES>
 __global__ __launch_bounds__(256) void kv_write(KvArgs a) {
     const int D = a.c.head_dim, H = a.c.kv_heads;
-    const int64_t rows = (int64_t)a.tokens * H * 2;
+    const int64_t rows = (int64_t)a.tokens * H;
     const int j = (threadIdx.x % LANES) * 8;
     for (int64_t r = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; r < rows;
          r += (int64_t)gridDim.x * (256 / LANES)) {
-        const int64_t th = r >> 1, t = th / H;
-        const int h = (int)(th - t * H);
-        const bool val = r & 1;
-        const T* src = val ? static_cast<const T*>(a.v) + t * a.vts + h * a.vhs
-                           : static_cast<const T*>(a.k) + t * a.kts + h * a.khs;
-        const f32x8 v = j < D ? load8(src + j) : f32x8{0, 0, 0, 0, 0, 0, 0, 0};
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
-        top = lanes_max<LANES>(top);  // (the lanes of a row leave the loop together)
-        const float s = row_scale(top);
+        const int64_t t = rows <= 0x7fffffff ? (int64_t)((uint32_t)r / (uint32_t)H) : r / H;
+        const int h = (int)(r - t * H), jj = j < D ? j : 0;
+        f32x8 v[2] = {load8(static_cast<const T*>(a.k) + t * a.kts + h * a.khs + jj),
+                      load8(static_cast<const T*>(a.v) + t * a.vts + h * a.vhs + jj)};
         const int64_t e = entry_of(a.c, a.slots[t], h);
-        if (e < 0 || j >= D) continue;
-        if (j == 0) (val ? a.c.v_scale : a.c.k_scale)[e] = s;
-        *reinterpret_cast<uint2*>((val ? a.c.v : a.c.k) + e * D + j) = quantized8(v, s);
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, j < D ? magnitude(v[o][i]) : 0u);
+            top = lanes_max<LANES>(top);  // (the lanes of a row leave the loop together)
+            const float s = row_scale(top);
+            if (e < 0 || j >= D) continue;
+            if (j == 0) (o ? a.c.v_scale : a.c.k_scale)[e] = s;
+            *reinterpret_cast<uint2*>((o ? a.c.v : a.c.k) + e * D + j) = quantized8(v[o], s);
+        }
     }
 }
 
@@ -51,7 +55,7 @@ __global__ __launch_bounds__(256) void kv_read(KvArgs a) {
     if (j >= D) return;
     for (int64_t r = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; r < rows;
          r += (int64_t)gridDim.x * (256 / LANES)) {
-        const int64_t t = r / H;
+        const int64_t t = rows <= 0x7fffffff ? (int64_t)((uint32_t)r / (uint32_t)H) : r / H;
         const int64_t e = entry_of(a.c, a.slots[t], (int)(r - t * H));
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
@@ -68,7 +72,7 @@ __global__ __launch_bounds__(256) void kv_read(KvArgs a) {
 
 template <typename T, int LANES>
 hipError_t launch(const KvArgs& a, bool write, hipStream_t st) {
-    const int64_t rows = (int64_t)a.tokens * a.c.kv_heads * (write ? 2 : 1);
+    const int64_t rows = (int64_t)a.tokens * a.c.kv_heads;
     const unsigned blocks = (unsigned)std::min<int64_t>((rows + 256 / LANES - 1) / (256 / LANES), 16384);
     if (write)
         hipLaunchKernelGGL((kv_write<T, LANES>), dim3(blocks), dim3(256), 0, st, a);

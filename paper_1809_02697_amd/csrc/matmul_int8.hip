@@ -352,7 +352,7 @@ struct Cost {
 // 96 x 16,384 -> 4096 24.5 us in 64 x 128 and four splits, 68.9 by matmul_rows)
 constexpr Cost kCosts[] = {{k256x256, 256, 256, 1, {2.3f, 2.3f}}, {k128x128, 128, 128, 2, {0.9f, 1.27f}},
                            {k64x128, 64, 128, 1, {0.56f, 0.56f}}, {k64x64, 64, 64, 2, {0.48f, 0.58f}},
-                           {k32x128, 32, 128, 2, {0.38f, 0.7f}}};
+                           {k32x128, 32, 128, 2, {0.45f, 0.7f}}};
 
 Choice choose(const MatmulArgs& a) {
     // (the tiles' row offsets are 32-bit)
