@@ -20,7 +20,7 @@ __device__ inline int64_t entry_of(const neo_kv_cache& c, int64_t slot, int h) {
 
 // A group takes a token's key and value of a head: one lookup of the slot, and
 // two rows' loads under way at once (16,000 tokens x 8 heads of 128 in float16
-// XXX us, 41 with a row a group).
+// 32 us, 41 with a row a group and a division a value).
 template <typename T, int LANES>
 __global__ __launch_bounds__(256) void kv_write(KvArgs a) {
     const int D = a.c.head_dim, H = a.c.kv_heads;

@@ -75,12 +75,28 @@ __device__ inline int quantized(float v, float s) {
     const float q = rintf(v / s);
     return s == s ? (int)fminf(fmaxf(q, -127.f), 127.f) : 0;
 }
-__device__ inline uint32_t quantized4(float a, float b, float c, float d, float s) {
-    return (uint32_t)(quantized(a, s) & 0xff) | (uint32_t)(quantized(b, s) & 0xff) << 8 |
-           (uint32_t)(quantized(c, s) & 0xff) << 16 | (uint32_t)(quantized(d, s) & 0xff) << 24;
-}
+// Eight of a row.  v times the scale's reciprocal lies within 3e-5 of v / s, so
+// it rounds to the same integer but near the middle of two, and only there the
+// quotient itself is taken (one value in 10^4; a quotient is 11 instructions).
 __device__ inline uint2 quantized8(f32x8 v, float s) {
-    return make_uint2(quantized4(v[0], v[1], v[2], v[3], s), quantized4(v[4], v[5], v[6], v[7], s));
+    const float inv = 1.f / s;
+    f32x8 q;
+    float far = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float t = v[i] * inv;
+        q[i] = rintf(t);
+        far = fmaxf(far, fabsf(t - q[i]));
+    }
+    uint32_t w[2] = {0, 0};
+    if (far < 0.49995f && s == s) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i / 4] |= (uint32_t)((int)q[i] & 0xff) << (8 * (i & 3));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i / 4] |= (uint32_t)(quantized(v[i], s) & 0xff) << (8 * (i & 3));
+    }
+    return make_uint2(w[0], w[1]);
 }
 __device__ inline f32x8 dequantized8(uint2 w, float s) {
     f32x8 v;
