@@ -1,0 +1,157 @@
+"""A decoder of transformer layers on the integer path: what the token operators
+of ``neo`` are for, put together the way a serving program uses them.
+
+A layer (weights int8 with a scale per channel, activations int8 with a scale
+per token, keys and values int8 in a paged cache):
+
+    q8 = rmsnorm_int8(delta + h)            residual addition, norm, quantization
+    q, k, v = matmul_int8(q8, w_qkv)
+    kv_write_int8(cache, k, v)
+    a = attention_paged_int8(cache, q)
+    delta = matmul_int8(quantize_tokens_int8(a), w_out)
+    q8 = rmsnorm_int8(delta + h)
+    gate, up = matmul_int8(q8, w_gate_up)
+    delta = matmul_int8(quantize_tokens_int8(up, gate=gate), w_down)
+
+``Decoder.step`` takes any number of new tokens of each sequence: whole
+prompts, chunks of them, or one token each.  Positions enter through the causal
+order alone.
+
+    python -m paper_1809_02697_amd.decoder      # a small decoder: prompts, then tokens
+"""
+from __future__ import annotations
+
+import torch
+
+from . import neo
+
+
+class Linear:
+    """A dense layer without bias: float32 weights [out][in] on the device, held as int8 rows."""
+
+    def __init__(self, w):
+        self.out, self.inp = w.shape
+        self.rows, self.scale = neo.pack_dense_int8(w.contiguous())
+
+    def __call__(self, q, scale, dtype):
+        return neo.matmul_int8(q, scale, self.inp, self.rows, self.scale, self.out, dtype=dtype)
+
+
+class Layer:
+    def __init__(self, w, q_heads, kv_heads, head_dim):
+        self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
+        self.norm1, self.norm2 = w["norm1"], w["norm2"]
+        self.qkv, self.out = Linear(w["qkv"]), Linear(w["out"])
+        self.gate_up, self.down = Linear(w["gate_up"]), Linear(w["down"])
+
+    def __call__(self, x, h, cache, step):
+        """x: the last sublayer's output; h: the residual stream before it (None at the first).
+        Returns both for the next layer."""
+        T, dtype, D = x.shape[0], x.dtype, self.head_dim
+        q8, s, h2 = neo.rmsnorm_int8(x, self.norm1, residual=h, h=h)
+        h = x if h2 is None else h2
+        qkv = self.qkv(q8, s, dtype).view(T, self.q_heads + 2 * self.kv_heads, D)
+        q, k, v = qkv.split([self.q_heads, self.kv_heads, self.kv_heads], 1)
+        neo.kv_write_int8(cache, k, v, step.slots)
+        a = neo.attention_paged_int8(cache, q, step.table, step.contexts, step.starts, step.max_chunk, step.max_context)
+        x = self.out(*neo.quantize_tokens_int8(a.view(T, self.q_heads * D)), dtype)
+        q8, s, h = neo.rmsnorm_int8(x, self.norm2, residual=h)
+        both = self.gate_up(q8, s, dtype)
+        F = both.shape[1] // 2
+        return self.down(*neo.quantize_tokens_int8(both[:, F:], gate=both[:, :F]), dtype), h
+
+
+class Step:
+    """Where one call's tokens stand: cache slots of the new ones, page table, lengths."""
+
+    def __init__(self, pages, lengths, new, page_size, device):
+        slots, contexts = [], []
+        for p, n, m in zip(pages, lengths, new):
+            slots += [p[t // page_size] * page_size + t % page_size for t in range(n, n + m)]
+            contexts.append(n + m)
+        starts = [0]
+        for m in new:
+            starts.append(starts[-1] + m)
+        most = max(1, max(len(p) for p in pages))
+        table = [p + [-1] * (most - len(p)) for p in pages]
+        ints = lambda v, t=torch.int32: torch.tensor(v, dtype=t, device=device)  # noqa: E731
+        self.slots, self.table, self.contexts, self.starts = ints(slots, torch.int64), ints(table), ints(contexts), ints(starts)
+        self.max_chunk, self.max_context = max(new), max(contexts)
+        self.last = ints([s - 1 for s, m in zip(starts[1:], new) if m], torch.int64)
+
+
+class Decoder:
+    """weights: {"embed": [vocab][width], "norm": [width], "head": [vocab][width],
+    "layers": [{"norm1", "qkv", "out", "norm2", "gate_up", "down"}, ...]}, float32 on the device."""
+
+    def __init__(self, weights, q_heads, kv_heads, head_dim, pages, page_size=64, dtype=torch.bfloat16):
+        self.embed, self.norm, self.head = weights["embed"].to(dtype), weights["norm"], Linear(weights["head"])
+        self.layers = [Layer(w, q_heads, kv_heads, head_dim) for w in weights["layers"]]
+        device = weights["embed"].device
+        self.caches = [neo.kv_cache(pages, kv_heads, page_size, head_dim, device) for _ in self.layers]
+        self.page_size, self.dtype, self.device = page_size, dtype, device
+        self.free = list(range(pages))[::-1]
+        self.pages, self.lengths = [], []
+
+    def add(self):
+        """A new, empty sequence; its number."""
+        self.pages.append([])
+        self.lengths.append(0)
+        return len(self.pages) - 1
+
+    def step(self, tokens):
+        """tokens: for every sequence the list of its new tokens (maybe empty).  Returns the
+        logits [sequences with new tokens][vocab] (float32) after the last of each."""
+        new = [len(t) for t in tokens]
+        if len(tokens) != len(self.pages) or not any(new):
+            raise ValueError("one list of tokens a sequence, and at least one token")
+        need = [-(-(n + m) // self.page_size) - len(p) for p, n, m in zip(self.pages, self.lengths, new)]
+        if sum(need) > len(self.free):
+            raise RuntimeError("the cache has no page left")
+        for p, n in zip(self.pages, need):
+            p += [self.free.pop() for _ in range(n)]
+        step = Step(self.pages, self.lengths, new, self.page_size, self.device)
+        x = self.embed[torch.tensor([t for s in tokens for t in s], device=self.device)]
+        h = None
+        for layer, cache in zip(self.layers, self.caches):
+            x, h = layer(x, h, cache, step)
+        self.lengths = [n + m for n, m in zip(self.lengths, new)]
+        q8, s, _ = neo.rmsnorm_int8(x[step.last], self.norm, residual=h[step.last], h=False)
+        return self.head(q8, s, torch.float32)
+
+
+def random_weights(layers, vocab, width, q_heads, kv_heads, head_dim, inner, seed=0, device="cuda"):
+    g = torch.Generator().manual_seed(seed)
+    mat = lambda o, i: (torch.randn(o, i, generator=g) / i ** 0.5).to(device)  # noqa: E731
+    gain = lambda: (torch.rand(width, generator=g) + 0.5).to(device)  # noqa: E731
+    return {"embed": mat(vocab, width) * width ** 0.5, "norm": gain(), "head": mat(vocab, width),
+            "layers": [{"norm1": gain(), "qkv": mat((q_heads + 2 * kv_heads) * head_dim, width),
+                        "out": mat(width, q_heads * head_dim), "norm2": gain(), "gate_up": mat(2 * inner, width),
+                        "down": mat(width, inner)} for _ in range(layers)]}
+
+
+def main():
+    import time
+    shape = dict(q_heads=16, kv_heads=4, head_dim=128)
+    d = Decoder(random_weights(4, 8192, 2048, inner=8192, **shape), pages=256, **shape)
+    g = torch.Generator().manual_seed(1)
+    prompts = [torch.randint(8192, (n,), generator=g).tolist() for n in (700, 33, 1, 256)]
+    for _ in prompts:
+        d.add()
+    logits = d.step([p[:256] for p in prompts])           # the long prompt in chunks
+    tokens = logits.argmax(1).tolist()
+    while d.lengths[0] < 700:
+        tokens[0] = d.step([prompts[0][d.lengths[0]:d.lengths[0] + 256], [], [], []]).argmax(1).item()
+    torch.cuda.synchronize()
+    t0, out = time.perf_counter(), [[t] for t in tokens]
+    for _ in range(32):
+        tokens = d.step([[t] for t in tokens]).argmax(1).tolist()
+        for o, t in zip(out, tokens):
+            o.append(t)
+    print(f"32 tokens of each of 4 sequences in {(time.perf_counter() - t0) * 1e3:.1f} ms")
+    for i, o in enumerate(out):
+        print(f"sequence {i} ({len(prompts[i])} tokens of prompt):", *o[:12], "...")
+
+
+if __name__ == "__main__":
+    main()

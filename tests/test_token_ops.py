@@ -659,3 +659,78 @@ def test_wrong_tensors_are_refused(torch):
                 lambda: neo.attention_paged_int8(cache, torch.ones(1, 1, 32, device="cuda"), z[:1].view(1, 1), z[:1], z, 1, 4)):
         with pytest.raises((TypeError, ValueError)):
             bad()
+
+
+# ---- the ways of the product, and caches past 32 bits -------------------------------------
+
+@gpu
+@pytest.mark.parametrize("M,K,N", [(4001, 272, 4111), (2050, 4000, 2047), (900, 700, 1500), (120, 16000, 700), (40, 16384, 300),
+                                   (70, 130, 9000), (5, 16384, 2000)])
+def test_matmul_large(torch, M, K, N):
+    """Sizes at which the product takes its larger tiles and splits in_features."""
+    rng = np.random.default_rng([M, N])
+    Kp = -(-K // 16) * 16
+    xq, wq = np.zeros((M, Kp), np.int8), np.zeros((N, Kp), np.int8)
+    xq[:, :K], wq[:, :K] = rng.integers(-127, 128, (M, K)), rng.integers(-127, 128, (N, K))
+    xs, ws = rng.uniform(0.01, 0.1, M).astype(np.float32), rng.uniform(0.001, 0.1, N).astype(np.float32)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    y = neo.matmul_int8(c(xq), c(xs), K, c(wq), c(ws), N, dtype=torch.float32).cpu().numpy()
+    acc = xq.astype(np.float64) @ wq.astype(np.float64).T     # integers below 2^53: exact
+    assert np.array_equal(y, acc.astype(np.float32) * xs[:, None] * ws[None])
+
+
+@gpu
+def test_cache_past_32_bits(torch):
+    """Entries and scales whose byte offsets exceed 2^32 are written, read back and attended to."""
+    H, page, D = 8, 64, 128
+    pages = (1 << 32) // (H * page * D) + 70
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("not enough device memory")
+    cache = tuple(torch.empty((pages, H, page, D), dtype=torch.int8, device="cuda") for _ in "kv") + \
+        tuple(torch.empty((pages, H, page), device="cuda") for _ in "kv")
+    T = 150
+    table = torch.tensor([[pages - 1, 0, pages - 65]], dtype=torch.int32)
+    slots = torch.cat([table[0, t // page].long()[None] * page + t % page for t in range(T)])
+    k, v = _rand(torch, (T, H, D), "float32", 31), _rand(torch, (T, H, D), "float32", 32)
+    neo.kv_write_int8(cache, k.cuda(), v.cuda(), slots.cuda())
+    ko, vo = neo.kv_read_int8(cache, slots.cuda(), torch.float32)
+    (kq, ks), (vq, vs) = _quantized(k.numpy()), _quantized(v.numpy())
+    assert np.array_equal(ko.cpu().numpy(), kq.astype(np.float32) * ks[..., None])
+    assert np.array_equal(vo.cpu().numpy(), vq.astype(np.float32) * vs[..., None])
+    # the same tokens in a small cache give the same bits
+    small = neo.kv_cache(3, H, page, D)
+    neo.kv_write_int8(small, k.cuda(), v.cuda(), torch.arange(T, device="cuda"))
+    for chunk in (1, 40):
+        q = _rand(torch, (chunk, 2 * H, D), "bfloat16", 33).cuda()
+        a = [neo.attention_paged_int8(c, q, t.cuda(), torch.tensor([T], dtype=torch.int32, device="cuda"),
+                                      torch.tensor([0, chunk], dtype=torch.int32, device="cuda"), chunk, T)
+             for c, t in ((cache, table), (small, torch.tensor([[0, 1, 2]], dtype=torch.int32)))]
+        assert torch.equal(*a)
+
+
+ATTN_LONG = [  # chunks, contexts, q heads, kv heads, head dim, page size, window: units that are cut over workgroups
+    ([1, 1, 1, 1], [5000, 20, 1300, 9000], 4, 1, 128, 64, 0),
+    ([1] * 40, [1500 + 37 * i for i in range(40)], 2, 1, 64, 16, 0),
+    ([4, 9], [4000, 1700], 4, 2, 80, 10, 0),
+    ([260, 3, 0, 90], [1800, 1500, 7, 1100], 2, 1, 128, 128, 0),
+    ([100, 40], [3000, 1400], 3, 1, 256, 16, 1200),
+    ([1, 2], [6000, 2500], 8, 1, 256, 32, 2000),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(ATTN_LONG)))
+def test_attention_long(torch, case, dtype):
+    chunks, contexts, Hq, H, D, page, window = ATTN_LONG[case]
+    _attend(torch, dtype, chunks, contexts, Hq, H, D, page, window, seed=100 + case)
+
+
+@gpu
+def test_attention_many_sequences(torch):
+    """More sequences than a workgroup has threads, most of them without new tokens."""
+    n = 700
+    contexts = [1100 if i % 97 == 0 else 3 for i in range(n)]
+    chunks = [1 if i % 3 == 0 else 0 for i in range(n)]
+    _attend(torch, "float16", chunks, contexts, 2, 1, 64, 16, seed=120)
+    _attend(torch, "float16", [c * 3 for c in chunks], contexts, 16, 1, 64, 16, seed=121)
