@@ -798,14 +798,23 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
                          li * (2 * C::KSTRIDE) + ((half ^ C::turn(li)) * 16);
         asm volatile("" : "+v"(kaddr));  // (kept in one register, not in one for every c)
 #pragma unroll
-        for (int t = 0; t < SUB; ++t) {
-            s[t] = f32x16{0};
+        for (int t = 0; t < SUB; ++t) s[t] = f32x16{0};
+        h8 kf[3][SUB];  // keys are read two steps ahead of their products
+        auto read = [&](int c) {
 #pragma unroll
-            for (int c = 0; c < STEPS; ++c) {
-                const h8 k = *(__attribute__((address_space(3))) const h8*)(uintptr_t)((kaddr ^ (c * 32)) + t * 32 * (2 * C::KSTRIDE));
+            for (int t = 0; t < SUB; ++t) kf[c % 3][t] = *(__attribute__((address_space(3))) const h8*)(uintptr_t)((kaddr ^ (c * 32)) + t * 32 * (2 * C::KSTRIDE));
+        };
+        read(0);
+        read(1);
 #pragma unroll
-                for (int i = 0; i < TERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i][c], s[t], 0, 0, 0);
-            }
+        for (int c = 0; c < STEPS; ++c) {
+            if (c + 2 < STEPS) read(c + 2);
+            __builtin_amdgcn_sched_barrier(0);  // (left alone, the compiler puts each read right before its use)
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[c % 3][t], q[i][c], s[t], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_sched_barrier(0);
         const uint64_t hidden = (uint64_t)uniform((int64_t)from.hidden);
@@ -907,6 +916,10 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
                     }
                 }
         }
+        h8 vf[3];  // values, two products ahead
+        vf[0] = values(0, 0, 0);
+        vf[1] = values(0, 0, 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < SUB; ++t)
 #pragma unroll
@@ -918,9 +931,12 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
                 Weights<TERMS>::terms(pv, w);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    const h8 v = values(t, x, d);
+                    const int n = (t * 2 + x) * DT + d, n2 = n + 2;
+                    if (n2 < SUB * 2 * DT) vf[n2 % 3] = values(n2 / DT / 2, n2 / DT % 2, n2 % DT);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int i = 0; i < TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[i], o[d], 0, 0, 0);
+                    for (int i = 0; i < TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n % 3], w[i], o[d], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
     };
@@ -974,9 +990,9 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
 }
 
 // The parts of the unit in which share j starts, if it is the first to start in
-// it: workgroup (j - 1, y) joins rows 4 y .. of the tile, a wave a row, or with
-// WAVES = 4 row y, its waves taking the parts in turn.
-template <typename T, int ROWS, int WAVES>
+// it: workgroup (j - 1, y) joins ROUNDS times four rows of the tile, a wave a
+// row, or with WAVES = 4 row y, its waves taking the parts in turn.
+template <typename T, int ROWS, int WAVES, int ROUNDS>
 __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Parts ws) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turn = wave % WAVES;
     const int G = a.q_heads / a.c.kv_heads, D = a.c.head_dim, j = blockIdx.x + 1;
@@ -989,8 +1005,11 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Par
     // parts: the end of share j - 1, the starts of shares j .. j + count - 2
     int count = 2;
     while (j + count - 1 < used && share_start(W, used, j + count - 1) < x0 + at.blocks) ++count;
-    const int rr = blockIdx.y * (4 / WAVES) + wave / WAVES, row = at.tile * ROWS + rr;
     const Unit u = unit_of(a, at.b);
+    static_assert(WAVES == 1 || ROUNDS == 1, "");
+#pragma unroll 1
+    for (int round = 0; round < ROUNDS; ++round) {
+    const int rr = (blockIdx.y * ROUNDS + round) * (4 / WAVES) + wave / WAVES, row = at.tile * ROWS + rr;
     if (row >= u.n * G) return;  // (with four waves a row: all of them)
     auto part = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0)) * ROWS + rr; };
     float M = kMinusInf, L = 0.f;
@@ -1034,6 +1053,7 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Par
 #pragma unroll
     for (int x = 0; x < 4; ++x)
         if (lane + 64 * x < D) store_row<T>(a, u, at.h, G, row, lane + 64 * x, L == 0.f ? 0.f : v[x] / L);
+    }
 }
 
 // Rows a workgroup takes.  Up to two tiles of 16 go to the kernel for few rows
@@ -1087,7 +1107,7 @@ hipError_t launch_tile(const AttnArgs& a, const Shares& sh, const Parts& p, unsi
     hipLaunchKernelGGL((attention_tile<T, DP, TERMS, NW>), dim3(blocks), dim3(NW * 64), C::BYTES, st, a, sh, p);
     e = hipGetLastError();
     if (e != hipSuccess || sh.groups < 2) return e;
-    hipLaunchKernelGGL((attention_join<T, C::ROWS, 1>), dim3(sh.groups - 1, C::ROWS / 4), dim3(256), 0, st, a, sh, p);
+    hipLaunchKernelGGL((attention_join<T, C::ROWS, 1, 4>), dim3(sh.groups - 1, C::ROWS / 16), dim3(256), 0, st, a, sh, p);
     return hipGetLastError();
 }
 
@@ -1109,7 +1129,7 @@ hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
         hipLaunchKernelGGL((attention_rows<T, DP, TERMS, false>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || sh.groups < 2) return e;
-    hipLaunchKernelGGL((attention_join<T, 16, 4>), dim3(sh.groups - 1, std::min(16, a.max_chunk * G)), dim3(256), 0, st, a, sh, p);
+    hipLaunchKernelGGL((attention_join<T, 16, 4, 1>), dim3(sh.groups - 1, std::min(16, a.max_chunk * G)), dim3(256), 0, st, a, sh, p);
     return hipGetLastError();
 }
 
