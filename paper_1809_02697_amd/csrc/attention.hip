@@ -13,7 +13,7 @@
 // float16 and bfloat16 queries are exact too (values 2^-28 of the largest and
 // less lose bits); a float32 query is the sum of two fp16 terms.  The weights
 // w_ij are scaled by 2^(14 - E), E the exponent of the largest vs that the row
-// has seen so far, and rounded to fp16 (float32: two terms; Weights below).
+// has seen so far, and rounded to fp16 (float16 and float32: two terms; Weights below).
 //
 // S^T = K Q^T and O^T = V^T P^T: the accumulator's layout of S^T (a lane holds
 // four neighbouring keys of one row) is the layout of the second product's
@@ -70,16 +70,22 @@ __device__ inline h8 join(h2 a, h2 b, h2 c, h2 d) {
 __device__ inline int exponent(uint32_t bits) { return (int)(bits >> 23) - 127; }
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Weights in fp16.  A term holds 11 bits from fp16's least normal number 2^-14
-// up, two terms hold 22 from 2^-3 up.  Smaller weights (of keys whose scores lie
-// far below the row's largest) are taken apart and multiplied in bf16, which
-// has float32's range, as two terms of 8 bits (three), so that every weight
-// keeps its bits: a position at which the largest keys' values are 0 is the sum
-// of the small ones.
-template <int TERMS>
+// How many fp16 terms a type's queries and weights are taken as.  float16 queries
+// are exact in one, but one rounding of the weights would be as large as the
+// output's own (error against 64 bits 1.4 times as much); bfloat16's is eight
+// times larger.
+//
+// A term holds 11 bits from fp16's least normal number 2^-14 up, two terms 22
+// from 2^-3 up (and at least 11 from 2^-14).  Smaller weights (of keys whose
+// scores lie far below the row's largest) are taken apart and multiplied in
+// bf16, which has float32's range, as two terms of 8 bits (float32: three), so
+// that every weight keeps its bits: a position at which the largest keys'
+// values are 0 is the sum of the small ones.
+template <typename T>
 struct Weights {
-    static constexpr float least = TERMS == 1 ? 0x1p-14f : 0x1p-3f;
-    static constexpr int SMALL = TERMS + 1;
+    static constexpr bool F32 = std::is_same<T, float>::value;
+    static constexpr int QTERMS = F32 ? 2 : 1, TERMS = std::is_same<T, __bf16>::value ? 1 : 2, SMALL = F32 ? 3 : 2;
+    static constexpr float least = F32 ? 0x1p-3f : 0x1p-14f;
     __device__ static void terms(const f32x8& v, h8 (&w)[TERMS]) {
         w[0] = __builtin_convertvector(v, h8);
         if constexpr (TERMS == 2) w[1] = __builtin_convertvector(v - __builtin_convertvector(w[0], f32x8), h8);
@@ -430,8 +436,9 @@ __device__ inline void load_block(const AttnArgs& a, const Shares& sp, const Key
 
 constexpr int kRowsBlock = kRowsWaves * 32;  // keys the workgroup takes at a time
 
-template <typename T, int DP, int TERMS, bool TILED>
+template <typename T, int DP, bool TILED>
 __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void attention_rows(AttnArgs a, Shares sp, Parts ws) {
+    typedef Weights<T> W;
     constexpr int KB = DP / 4, STEPS = DP / 32, VB = DP / 16;
     __shared__ float red_m[kRowsWaves][16], red_l[kRowsWaves][16], red_o[kRowsWaves][16][DP + 4];
     __shared__ typename Cursor<16, kRowsBlock>::Scratch scratch;
@@ -458,7 +465,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
     // this lane's row of queries: values d = g * KB + ...
     const int row = min(row0 + li, rows - 1), tok = row / G, pos = u.ctx - u.all + tok;
     const int pos_lo = u.ctx - u.all + row0 / G, pos_hi = u.ctx - u.all + (min(row0 + 16, rows) - 1) / G;
-    h8 q[TERMS][STEPS];
+    h8 q[W::QTERMS][STEPS];
     float fq;  // what a score is multiplied with
     {
         const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)(h * G + row - tok * G) * a.qhs + g * KB;
@@ -480,7 +487,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
         for (int s = 0; s < STEPS; ++s) {
             v[s] *= up;
             q[0][s] = __builtin_convertvector(v[s], h8);
-            if constexpr (TERMS == 2) q[1][s] = __builtin_convertvector(v[s] - __builtin_convertvector(q[0][s], f32x8), h8);
+            if constexpr (W::QTERMS == 2) q[1][s] = __builtin_convertvector(v[s] - __builtin_convertvector(q[0][s], f32x8), h8);
         }
         fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
         // (no score of a query with an infinity is finite: its softmax is undefined)
@@ -510,7 +517,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
                 unpack4(biased(kv.k[t][c / 2][c % 2 * 2 + 1]), x[2], x[3]);
                 const h8 k = join(x[0], x[1], x[2], x[3]);
 #pragma unroll
-                for (int i = 0; i < TERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i][c], s[t], 0, 0, 0);
+                for (int i = 0; i < W::QTERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i][c], s[t], 0, 0, 0);
             }
         }
 
@@ -564,7 +571,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
                 const float p = exp2_fast(s[t][r] - lift);
                 l += p;
                 pv[4 * t + r] = p * ldexpf(kv.vs[t][r], -E);
-                small |= pv[4 * t + r] != 0.f && pv[4 * t + r] < Weights<TERMS>::least;
+                small |= pv[4 * t + r] != 0.f && pv[4 * t + r] < W::least;
             }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -577,15 +584,15 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
             return join(pair(kv.v[0][0][c], kv.v[0][1][c], y), pair(kv.v[0][2][c], kv.v[0][3][c], y),
                         pair(kv.v[1][0][c], kv.v[1][1][c], y), pair(kv.v[1][2][c], kv.v[1][3][c], y));
         };
-        h8 w[TERMS];
+        h8 w[W::TERMS];
         if (__any(small)) {
-            b8 ws[Weights<TERMS>::SMALL];
-            Weights<TERMS>::take_small(pv, ws);
+            b8 ws[W::SMALL];
+            W::take_small(pv, ws);
 #pragma unroll
             for (int t = 0; t < VB; ++t) {
                 const b8 v = to_bf16(values(t));
 #pragma unroll
-                for (int i = 0; i < Weights<TERMS>::SMALL; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ws[i], o[t], 0, 0, 0);
+                for (int i = 0; i < W::SMALL; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ws[i], o[t], 0, 0, 0);
             }
             // (converted anew below: kept, the values would take registers from the common case)
 #pragma unroll
@@ -593,12 +600,12 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
 #pragma unroll
                 for (int c = 0; c < VB / 4; ++c) asm volatile("" : "+v"(kv.v[i / 4][i % 4][c]));
         }
-        Weights<TERMS>::terms(pv, w);
+        W::terms(pv, w);
 #pragma unroll
         for (int t = 0; t < VB; ++t) {
             const h8 v = values(t);
 #pragma unroll
-            for (int i = 0; i < TERMS; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], o[t], 0, 0, 0);
+            for (int i = 0; i < W::TERMS; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], o[t], 0, 0, 0);
         }
         kv = next;
         kb = kn;
@@ -655,7 +662,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
 // per workgroup on their way into LDS (the next tile's bytes travel meanwhile),
 // and each wave multiplies its 32 rows with them on 32x32x16 products.  Values
 // lie in LDS as they came and are read transposed.
-template <typename T, int DP, int TERMS, int NW>
+template <int DP, int NW>
 struct TileShape {
     static constexpr int KT = DP == 256 ? 32 : 64, THREADS = NW * 64, ROWS = NW * 32;
     static constexpr int CH = DP / 16, CHUNKS = KT * CH, LOADS = (CHUNKS + THREADS - 1) / THREADS;
@@ -672,9 +679,10 @@ struct TileShape {
     __device__ static int turn(int key) { return CH * 2 < 16 ? key >> 1 & 7 : key & 15; }
 };
 
-template <typename T, int DP, int TERMS, int NW>
+template <typename T, int DP, int NW>
 __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp, Parts ws) {
-    typedef TileShape<T, DP, TERMS, NW> C;
+    typedef TileShape<DP, NW> C;
+    typedef Weights<T> W;
     constexpr int KT = C::KT, SUB = KT / 32, STEPS = DP / 16, DT = DP / 32;
     typedef typename C::Buffer Buffer;
     extern __shared__ __align__(512) char lds[];
@@ -696,7 +704,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
     const bool live = row < rows;
     const int tok = min(row, rows - 1) / G, pos = u.ctx - u.all + tok;
     const int pos_lo = u.ctx - u.all + min(wrow, rows - 1) / G, pos_hi = u.ctx - u.all + min(wrow + 31, rows - 1) / G;
-    h8 q[TERMS][STEPS];
+    h8 q[W::QTERMS][STEPS];
     float fq;
     {
         const int hq = h * G + min(row, rows - 1) - tok * G;
@@ -716,7 +724,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
         for (int s = 0; s < STEPS; ++s) {
             const f32x8 v = (s * 16 < D ? load8(src + s * 16) : f32x8{0, 0, 0, 0, 0, 0, 0, 0}) * up;
             q[0][s] = __builtin_convertvector(v, h8);
-            if constexpr (TERMS == 2) q[1][s] = __builtin_convertvector(v - __builtin_convertvector(q[0][s], f32x8), h8);
+            if constexpr (W::QTERMS == 2) q[1][s] = __builtin_convertvector(v - __builtin_convertvector(q[0][s], f32x8), h8);
         }
         fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
         if (top >= kInfBits) fq = __uint_as_float(0x7fc00000u);
@@ -813,7 +821,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
-                for (int i = 0; i < TERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[c % 3][t], q[i][c], s[t], 0, 0, 0);
+                for (int i = 0; i < W::QTERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[c % 3][t], q[i][c], s[t], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -895,7 +903,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             const h4 y0 = read_transposed(p), y1 = read_transposed(p + 8 * C::VSTRIDE);
             return h8{y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
         };
-        if (__any(least < Weights<TERMS>::least)) {
+        if (__any(least < W::least)) {
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
@@ -903,15 +911,15 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
                     f32x8 pv;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) pv[i] = s[t][8 * x + i];
-                    b8 w[Weights<TERMS>::SMALL];
-                    Weights<TERMS>::take_small(pv, w);
+                    b8 w[W::SMALL];
+                    W::take_small(pv, w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s[t][8 * x + i] = pv[i];
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
                         const b8 v = to_bf16(values(t, x, d));
 #pragma unroll
-                        for (int i = 0; i < Weights<TERMS>::SMALL; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[i], o[d], 0, 0, 0);
+                        for (int i = 0; i < W::SMALL; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[i], o[d], 0, 0, 0);
                         asm volatile("" ::: "memory");  // (the values are read again below: kept, they would take its registers)
                     }
                 }
@@ -927,15 +935,15 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
                 f32x8 pv;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) pv[i] = s[t][8 * x + i];
-                h8 w[TERMS];
-                Weights<TERMS>::terms(pv, w);
+                h8 w[W::TERMS];
+                W::terms(pv, w);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     const int n = (t * 2 + x) * DT + d, n2 = n + 2;
                     if (n2 < SUB * 2 * DT) vf[n2 % 3] = values(n2 / DT / 2, n2 / DT % 2, n2 % DT);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int i = 0; i < TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n % 3], w[i], o[d], 0, 0, 0);
+                    for (int i = 0; i < W::TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n % 3], w[i], o[d], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -1090,28 +1098,28 @@ Shares choose_shares(const AttnArgs& a) {
 
 int64_t part_rows(const AttnArgs& a, const Shares& sh) { return (int64_t)sh.groups * 2 * tile_rows(a); }
 
-template <typename T, int DP, int TERMS, int NW>
+template <typename T, int DP, int NW>
 hipError_t launch_tile(const AttnArgs& a, const Shares& sh, const Parts& p, unsigned blocks, hipStream_t st) {
-    typedef TileShape<T, DP, TERMS, NW> C;
+    typedef TileShape<DP, NW> C;
     // (more LDS than a kernel gets unasked; set once per device)
     static std::atomic<uint64_t> asked{0};
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev < 0 || dev >= 64 || !(asked.load() >> dev & 1)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_tile<T, DP, TERMS, NW>),
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_tile<T, DP, NW>),
                                 hipFuncAttributeMaxDynamicSharedMemorySize, C::BYTES);
         if (e != hipSuccess) return e;
         if (dev >= 0 && dev < 64) asked.fetch_or(1ull << dev);
     }
-    hipLaunchKernelGGL((attention_tile<T, DP, TERMS, NW>), dim3(blocks), dim3(NW * 64), C::BYTES, st, a, sh, p);
+    hipLaunchKernelGGL((attention_tile<T, DP, NW>), dim3(blocks), dim3(NW * 64), C::BYTES, st, a, sh, p);
     e = hipGetLastError();
     if (e != hipSuccess || sh.groups < 2) return e;
     hipLaunchKernelGGL((attention_join<T, C::ROWS, 1, 4>), dim3(sh.groups - 1, C::ROWS / 16), dim3(256), 0, st, a, sh, p);
     return hipGetLastError();
 }
 
-template <typename T, int DP, int TERMS>
+template <typename T, int DP>
 hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
     const Shares sh = choose_shares(a);
     const int G = a.q_heads / a.c.kv_heads, tile = tile_rows(a);
@@ -1119,25 +1127,25 @@ hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
     const Parts p{ws, reinterpret_cast<float2*>(ws + n * a.c.head_dim), reinterpret_cast<Start*>(ws + n * (a.c.head_dim + 2))};
     const int64_t units = (((int64_t)a.max_chunk * G + tile - 1) / tile) * a.seqs * a.c.kv_heads;
     const unsigned blocks = (unsigned)(sh.groups ? sh.groups : units);
-    if (tile == 64) return launch_tile<T, DP, TERMS, 2>(a, sh, p, blocks, st);
-    if (tile == 128) return launch_tile<T, DP, TERMS, 4>(a, sh, p, blocks, st);
+    if (tile == 64) return launch_tile<T, DP, 2>(a, sh, p, blocks, st);
+    if (tile == 128) return launch_tile<T, DP, 4>(a, sh, p, blocks, st);
     if constexpr (DP <= 128)
-        if (tile == 256) return launch_tile<T, DP, TERMS, 8>(a, sh, p, blocks, st);
+        if (tile == 256) return launch_tile<T, DP, 8>(a, sh, p, blocks, st);
     if (a.c.page_size % 16 == 0)
-        hipLaunchKernelGGL((attention_rows<T, DP, TERMS, true>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
+        hipLaunchKernelGGL((attention_rows<T, DP, true>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
     else
-        hipLaunchKernelGGL((attention_rows<T, DP, TERMS, false>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
+        hipLaunchKernelGGL((attention_rows<T, DP, false>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || sh.groups < 2) return e;
     hipLaunchKernelGGL((attention_join<T, 16, 4, 1>), dim3(sh.groups - 1, std::min(16, a.max_chunk * G)), dim3(256), 0, st, a, sh, p);
     return hipGetLastError();
 }
 
-template <typename T, int TERMS>
+template <typename T>
 hipError_t by_dim(const AttnArgs& a, float* ws, hipStream_t st) {
-    if (a.c.head_dim <= 64) return launch_d<T, 64, TERMS>(a, ws, st);
-    if (a.c.head_dim <= 128) return launch_d<T, 128, TERMS>(a, ws, st);
-    return launch_d<T, 256, TERMS>(a, ws, st);
+    if (a.c.head_dim <= 64) return launch_d<T, 64>(a, ws, st);
+    if (a.c.head_dim <= 128) return launch_d<T, 128>(a, ws, st);
+    return launch_d<T, 256>(a, ws, st);
 }
 
 }  // namespace
@@ -1148,9 +1156,9 @@ size_t attention_workspace(int, const AttnArgs& a) {
 }
 
 hipError_t launch_attention(int dtype, const AttnArgs& a, float* ws, hipStream_t st) {
-    if (dtype == NEO_F32) return by_dim<float, 2>(a, ws, st);
-    if (dtype == NEO_F16) return by_dim<_Float16, 1>(a, ws, st);
-    return by_dim<__bf16, 1>(a, ws, st);
+    if (dtype == NEO_F32) return by_dim<float>(a, ws, st);
+    if (dtype == NEO_F16) return by_dim<_Float16>(a, ws, st);
+    return by_dim<__bf16>(a, ws, st);
 }
 
 }  // namespace neo
