@@ -724,7 +724,8 @@ int neo_dequantize_tokens_int8(const int8_t* xq, int64_t xq_stride, const float*
  *           [out_features], as neo_pack_dense_int8 writes them
  *   bias    device float32 [out_features], or NULL;  act enum neo_act
  *   y       device [M][out_features] of `dtype`, row stride y_stride
- * in_features at most 133,144 (the int32 sum's bound).  A product split over
+ * in_features at most 133,144 (the int32 sum's bound), M at most 2^30,
+ * out_features at most 2^26.  A product split over
  * in_features keeps its partial sums in the workspace of the stream, grown as
  * neo_conv2d_nchwxc's (NEO_ERR_STATE if it would have to grow during capture).
  */

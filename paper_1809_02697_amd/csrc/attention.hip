@@ -351,6 +351,10 @@ __device__ inline void store_row(const AttnArgs& a, const Unit& u, int h, int G,
 // while this one's are used, and the waves' results are joined in LDS.
 // TILED: pages of whole 16 tokens, so a page is looked up once per 16 keys for
 // the whole wave; other pages are looked up key by key.
+//
+// The cache, read once, bounds it: one token each of 32 sequences, 32 query
+// heads on 8 of 128, contexts up to 32,000 (650 MB) 124 us, 5.2 TB/s, and 8 us
+// to join.
 constexpr int kRowsWaves = 4;
 
 template <int DP>
@@ -447,213 +451,213 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
     Walk<16, kRowsBlock, kRowsWaves * 64> walk;
     if (!walk.begin(a, sp, G, ws, scratch)) return;
     for (;;) {
-    const Unit u = walk.c.u;
-    const int h = walk.c.h, rows = walk.c.rows, row0 = walk.c.tile * 16, hi = walk.c.hi;
-    walk.unit_keys();
-    const int first = walk.first, last = walk.last;
-    const int32_t* table = a.table + walk.c.b * a.table_stride;
+        const Unit u = walk.c.u;
+        const int h = walk.c.h, rows = walk.c.rows, row0 = walk.c.tile * 16, hi = walk.c.hi;
+        walk.unit_keys();
+        const int first = walk.first, last = walk.last;
+        const int32_t* table = a.table + walk.c.b * a.table_stride;
 
-    KeyBlock<DP> kv;
-    int kb = first + wave * 32;
-    KeyPages<TILED> pages;
-    if (hi > 0) {
-        look_up<TILED>(sp, table, kb, hi, li, g, pages);
-        load_block<DP, TILED>(a, sp, pages, h, kb, hi, li, g, kv);
-        look_up<TILED>(sp, table, kb + kRowsBlock, hi, li, g, pages);
-    }
-
-    // this lane's row of queries: values d = g * KB + ...
-    const int row = min(row0 + li, rows - 1), tok = row / G, pos = u.ctx - u.all + tok;
-    const int pos_lo = u.ctx - u.all + row0 / G, pos_hi = u.ctx - u.all + (min(row0 + 16, rows) - 1) / G;
-    h8 q[W::QTERMS][STEPS];
-    float fq;  // what a score is multiplied with
-    {
-        const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)(h * G + row - tok * G) * a.qhs + g * KB;
-        f32x8 v[STEPS];
-        uint32_t top = 0;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const bool in = g * KB + s * 8 < D;
-            v[s] = load8(in ? src + s * 8 : src - g * KB);
-            if (!in) v[s] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[s][i]));
+        KeyBlock<DP> kv;
+        int kb = first + wave * 32;
+        KeyPages<TILED> pages;
+        if (hi > 0) {
+            look_up<TILED>(sp, table, kb, hi, li, g, pages);
+            load_block<DP, TILED>(a, sp, pages, h, kb, hi, li, g, kv);
+            look_up<TILED>(sp, table, kb + kRowsBlock, hi, li, g, pages);
         }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-        const int e = top >= kInfBits ? 0 : min(14 - exponent(top), 126);
-        const float up = ldexpf(1.f, e);
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            v[s] *= up;
-            q[0][s] = __builtin_convertvector(v[s], h8);
-            if constexpr (W::QTERMS == 2) q[1][s] = __builtin_convertvector(v[s] - __builtin_convertvector(q[0][s], f32x8), h8);
-        }
-        fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
-        // (no score of a query with an infinity is finite: its softmax is undefined)
-        if (top >= kInfBits) fq = __uint_as_float(0x7fc00000u);
-    }
 
-    v4f o[VB];
+        // this lane's row of queries: values d = g * KB + ...
+        const int row = min(row0 + li, rows - 1), tok = row / G, pos = u.ctx - u.all + tok;
+        const int pos_lo = u.ctx - u.all + row0 / G, pos_hi = u.ctx - u.all + (min(row0 + 16, rows) - 1) / G;
+        h8 q[W::QTERMS][STEPS];
+        float fq;  // what a score is multiplied with
+        {
+            const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)(h * G + row - tok * G) * a.qhs + g * KB;
+            f32x8 v[STEPS];
+            uint32_t top = 0;
 #pragma unroll
-    for (int t = 0; t < VB; ++t) o[t] = v4f{0, 0, 0, 0};
-    float m = kMinusInf, l = 0.f;
-    int E = -127;  // exponent of the largest value scale seen so far
-
-    while (kb < last) {
-        const int kn = kb + kRowsBlock;
-        KeyBlock<DP> next;
-        load_block<DP, TILED>(a, sp, pages, h, kn, hi, li, g, next);
-        look_up<TILED>(sp, table, kn + kRowsBlock, hi, li, g, pages);
-
-        v4f s[2];
+            for (int s = 0; s < STEPS; ++s) {
+                const bool in = g * KB + s * 8 < D;
+                v[s] = load8(in ? src + s * 8 : src - g * KB);
+                if (!in) v[s] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = v4f{0, 0, 0, 0};
-#pragma unroll
-            for (int c = 0; c < STEPS; ++c) {
-                h2 x[4];
-                unpack4(biased(kv.k[t][c / 2][c % 2 * 2]), x[0], x[1]);
-                unpack4(biased(kv.k[t][c / 2][c % 2 * 2 + 1]), x[2], x[3]);
-                const h8 k = join(x[0], x[1], x[2], x[3]);
-#pragma unroll
-                for (int i = 0; i < W::QTERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i][c], s[t], 0, 0, 0);
+                for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[s][i]));
             }
+            top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+            const int e = top >= kInfBits ? 0 : min(14 - exponent(top), 126);
+            const float up = ldexpf(1.f, e);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                v[s] *= up;
+                q[0][s] = __builtin_convertvector(v[s], h8);
+                if constexpr (W::QTERMS == 2) q[1][s] = __builtin_convertvector(v[s] - __builtin_convertvector(q[0][s], f32x8), h8);
+            }
+            fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
+            // (no score of a query with an infinity is finite: its softmax is undefined)
+            if (top >= kInfBits) fq = __uint_as_float(0x7fc00000u);
         }
 
-        const bool all = kb + 32 <= last && kb + 31 <= pos_lo && (!a.window || kb > pos_hi - a.window) &&
-                         __all(kv.there == 0xff);
-        if (!all) {
-            // this lane's keys j0 + x: seen from x = from_x up to to_x
-            const int j0 = kb + 4 * g, to_x = min(pos, last - 1) - j0, from_x = a.window ? pos - a.window + 1 - j0 : 0;
+        v4f o[VB];
+#pragma unroll
+        for (int t = 0; t < VB; ++t) o[t] = v4f{0, 0, 0, 0};
+        float m = kMinusInf, l = 0.f;
+        int E = -127;  // exponent of the largest value scale seen so far
+
+        while (kb < last) {
+            const int kn = kb + kRowsBlock;
+            KeyBlock<DP> next;
+            load_block<DP, TILED>(a, sp, pages, h, kn, hi, li, g, next);
+            look_up<TILED>(sp, table, kn + kRowsBlock, hi, li, g, pages);
+
+            v4f s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[t] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < STEPS; ++c) {
+                    h2 x[4];
+                    unpack4(biased(kv.k[t][c / 2][c % 2 * 2]), x[0], x[1]);
+                    unpack4(biased(kv.k[t][c / 2][c % 2 * 2 + 1]), x[2], x[3]);
+                    const h8 k = join(x[0], x[1], x[2], x[3]);
+#pragma unroll
+                    for (int i = 0; i < W::QTERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i][c], s[t], 0, 0, 0);
+                }
+            }
+
+            const bool all = kb + 32 <= last && kb + 31 <= pos_lo && (!a.window || kb > pos_hi - a.window) &&
+                             __all(kv.there == 0xff);
+            if (!all) {
+                // this lane's keys j0 + x: seen from x = from_x up to to_x
+                const int j0 = kb + 4 * g, to_x = min(pos, last - 1) - j0, from_x = a.window ? pos - a.window + 1 - j0 : 0;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int x = 16 * t + r;
+                        const bool see = x <= to_x && x >= from_x && (kv.there >> (4 * t + r) & 1);
+                        s[t][r] = see ? s[t][r] : kMinusInf;
+                        kv.ks[t][r] = see ? kv.ks[t][r] : 1.f;
+                        kv.vs[t][r] = see ? kv.vs[t][r] : 0.f;
+                    }
+            }
+            float top = kMinusInf;
+            uint32_t vtop = 0;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int x = 16 * t + r;
-                    const bool see = x <= to_x && x >= from_x && (kv.there >> (4 * t + r) & 1);
-                    s[t][r] = see ? s[t][r] : kMinusInf;
-                    kv.ks[t][r] = see ? kv.ks[t][r] : 1.f;
-                    kv.vs[t][r] = see ? kv.vs[t][r] : 0.f;
+                    s[t][r] *= kv.ks[t][r] * fq;
+                    top = fmaxf(top, s[t][r]);
+                    vtop = max(vtop, magnitude(kv.vs[t][r]));
                 }
-        }
-        float top = kMinusInf;
-        uint32_t vtop = 0;
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 16, 64));
+            vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 32, 64));
+            const float mn = fmaxf(m, top), m0 = mn == kMinusInf ? 0.f : mn;
+            const float lift = m0 - kLift;  // weights (and l) are 2^14 times p
+            const int En = max(E, min(exponent(vtop), 126));
+            if (__any(mn > m || En > E)) {
+                const float f = exp2_fast(m - m0), fo = ldexpf(f, E - En);
+                l *= f;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[t][r] *= kv.ks[t][r] * fq;
-                top = fmaxf(top, s[t][r]);
-                vtop = max(vtop, magnitude(kv.vs[t][r]));
+                for (int t = 0; t < VB; ++t) o[t] *= fo;
+                m = mn;
+                E = En;
             }
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 16, 64));
-        vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 32, 64));
-        const float mn = fmaxf(m, top), m0 = mn == kMinusInf ? 0.f : mn;
-        const float lift = m0 - kLift;  // weights (and l) are 2^14 times p
-        const int En = max(E, min(exponent(vtop), 126));
-        if (__any(mn > m || En > E)) {
-            const float f = exp2_fast(m - m0), fo = ldexpf(f, E - En);
-            l *= f;
+            f32x8 pv;
+            bool small = false;
 #pragma unroll
-            for (int t = 0; t < VB; ++t) o[t] *= fo;
-            m = mn;
-            E = En;
-        }
-        f32x8 pv;
-        bool small = false;
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+                for (int r = 0; r < 4; ++r) {
+                    const float p = exp2_fast(s[t][r] - lift);
+                    l += p;
+                    pv[4 * t + r] = p * ldexpf(kv.vs[t][r], -E);
+                    small |= pv[4 * t + r] != 0.f && pv[4 * t + r] < W::least;
+                }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float p = exp2_fast(s[t][r] - lift);
-                l += p;
-                pv[4 * t + r] = p * ldexpf(kv.vs[t][r], -E);
-                small |= pv[4 * t + r] != 0.f && pv[4 * t + r] < W::least;
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int c = 0; c < VB / 4; ++c) kv.v[t][r][c] = biased(kv.v[t][r][c]);
+            auto values = [&](int t) {
+                const int c = t / 4, y = t % 4;
+                return join(pair(kv.v[0][0][c], kv.v[0][1][c], y), pair(kv.v[0][2][c], kv.v[0][3][c], y),
+                            pair(kv.v[1][0][c], kv.v[1][1][c], y), pair(kv.v[1][2][c], kv.v[1][3][c], y));
+            };
+            h8 w[W::TERMS];
+            if (__any(small)) {
+                b8 ws[W::SMALL];
+                W::take_small(pv, ws);
+#pragma unroll
+                for (int t = 0; t < VB; ++t) {
+                    const b8 v = to_bf16(values(t));
+#pragma unroll
+                    for (int i = 0; i < W::SMALL; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ws[i], o[t], 0, 0, 0);
+                }
+                // (converted anew below: kept, the values would take registers from the common case)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int c = 0; c < VB / 4; ++c) asm volatile("" : "+v"(kv.v[i / 4][i % 4][c]));
             }
+            W::terms(pv, w);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < VB; ++t) {
+                const h8 v = values(t);
+#pragma unroll
+                for (int i = 0; i < W::TERMS; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], o[t], 0, 0, 0);
+            }
+            kv = next;
+            kb = kn;
+        }
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        l *= 0x1p-14f;
+
+        // the waves' parts: o[t][r] is value d = (4 g + r) * VB + t of row li
+        if (g == 0) {
+            red_m[wave][li] = m;
+            red_l[wave][li] = l;
+        }
+        __syncthreads();
+        if (row0 + li < rows) {
+            float M = kMinusInf;
+#pragma unroll
+            for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][li]);
+            const float f = m == kMinusInf ? 0.f : ldexpf(exp2_fast(m - M), E - 14 + 9);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int c = 0; c < VB / 4; ++c) kv.v[t][r][c] = biased(kv.v[t][r][c]);
-        auto values = [&](int t) {
-            const int c = t / 4, y = t % 4;
-            return join(pair(kv.v[0][0][c], kv.v[0][1][c], y), pair(kv.v[0][2][c], kv.v[0][3][c], y),
-                        pair(kv.v[1][0][c], kv.v[1][1][c], y), pair(kv.v[1][2][c], kv.v[1][3][c], y));
-        };
-        h8 w[W::TERMS];
-        if (__any(small)) {
-            b8 ws[W::SMALL];
-            W::take_small(pv, ws);
+                for (int t = 0; t < VB; t += 4)
+                    *reinterpret_cast<v4f*>(&red_o[wave][li][(4 * g + r) * VB + t]) = v4f{o[t][r], o[t + 1][r], o[t + 2][r], o[t + 3][r]} * f;
+        }
+        __syncthreads();
+        const int live = min(16, rows - row0);
+        for (int x = threadIdx.x; x < live * DP; x += kRowsWaves * 64) {
+            const int rr = x / DP, d = x - rr * DP, rw = row0 + rr;
+            if (d >= D) continue;
+            float M = kMinusInf, L = 0.f, v = 0.f;
 #pragma unroll
-            for (int t = 0; t < VB; ++t) {
-                const b8 v = to_bf16(values(t));
+            for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][rr]);
 #pragma unroll
-                for (int i = 0; i < W::SMALL; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ws[i], o[t], 0, 0, 0);
+            for (int w = 0; w < kRowsWaves; ++w) {
+                L += red_m[w][rr] == kMinusInf ? red_l[w][rr] : red_l[w][rr] * exp2_fast(red_m[w][rr] - M);
+                v += red_o[w][rr][d];
             }
-            // (converted anew below: kept, the values would take registers from the common case)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int c = 0; c < VB / 4; ++c) asm volatile("" : "+v"(kv.v[i / 4][i % 4][c]));
+            if (walk.whole) {
+                store_row<T>(a, u, h, G, rw, d, L == 0.f ? 0.f : v / L);
+            } else {
+                const int64_t part = ((int64_t)walk.share * 2 + !walk.head) * 16 + rr;
+                ws.o[part * D + d] = v;
+                if (d == 0) ws.ml[part] = make_float2(M, L);
+            }
         }
-        W::terms(pv, w);
-#pragma unroll
-        for (int t = 0; t < VB; ++t) {
-            const h8 v = values(t);
-#pragma unroll
-            for (int i = 0; i < W::TERMS; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], o[t], 0, 0, 0);
-        }
-        kv = next;
-        kb = kn;
-    }
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    l *= 0x1p-14f;
-
-    // the waves' parts: o[t][r] is value d = (4 g + r) * VB + t of row li
-    if (g == 0) {
-        red_m[wave][li] = m;
-        red_l[wave][li] = l;
-    }
-    __syncthreads();
-    if (row0 + li < rows) {
-        float M = kMinusInf;
-#pragma unroll
-        for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][li]);
-        const float f = m == kMinusInf ? 0.f : ldexpf(exp2_fast(m - M), E - 14 + 9);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int t = 0; t < VB; t += 4)
-                *reinterpret_cast<v4f*>(&red_o[wave][li][(4 * g + r) * VB + t]) = v4f{o[t][r], o[t + 1][r], o[t + 2][r], o[t + 3][r]} * f;
-    }
-    __syncthreads();
-    const int live = min(16, rows - row0);
-    for (int x = threadIdx.x; x < live * DP; x += kRowsWaves * 64) {
-        const int rr = x / DP, d = x - rr * DP, rw = row0 + rr;
-        if (d >= D) continue;
-        float M = kMinusInf, L = 0.f, v = 0.f;
-#pragma unroll
-        for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][rr]);
-#pragma unroll
-        for (int w = 0; w < kRowsWaves; ++w) {
-            L += red_m[w][rr] == kMinusInf ? red_l[w][rr] : red_l[w][rr] * exp2_fast(red_m[w][rr] - M);
-            v += red_o[w][rr][d];
-        }
-        if (walk.whole) {
-            store_row<T>(a, u, h, G, rw, d, L == 0.f ? 0.f : v / L);
-        } else {
-            const int64_t part = ((int64_t)walk.share * 2 + !walk.head) * 16 + rr;
-            ws.o[part * D + d] = v;
-            if (d == 0) ws.ml[part] = make_float2(M, L);
-        }
-    }
-    if (!walk.next(a, G)) break;
-    __syncthreads();  // (the parts in LDS are read)
+        if (!walk.next(a, G)) break;
+        __syncthreads();  // (the parts in LDS are read)
     }
 }
 
@@ -662,6 +666,15 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
 // per workgroup on their way into LDS (the next tile's bytes travel meanwhile),
 // and each wave multiplies its 32 rows with them on 32x32x16 products.  Values
 // lie in LDS as they came and are read transposed.
+//
+// The softmax's arithmetic and the products bound it, one after the other more
+// than side by side: of the cycles the vector unit works 57 %, the matrix unit
+// 36 % and LDS 37 %.  2048 tokens at 32,768, 32 query heads on 8 of 128 in
+// bfloat16 take 1.29 ms, 823 TFLOP/s (float16 17 % more, whose weights are two
+// terms).  32 rows a wave rather than
+// 16 halve the reads of keys and values (16 rows: 1.63 ms); eight waves share a
+// tile because each then converts an eighth of it (two workgroups of four
+// waves a CU: 1.54 ms).
 template <int DP, int NW>
 struct TileShape {
     static constexpr int KT = DP == 256 ? 32 : 64, THREADS = NW * 64, ROWS = NW * 32;
@@ -694,216 +707,240 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
     if (!walk.begin(a, sp, G, ws, *reinterpret_cast<typename Cursor<C::ROWS, KT>::Scratch*>(lds))) return;
     __syncthreads();  // (the scratch lies where the tiles will)
     for (;;) {
-    const Unit u = walk.c.u;
-    const int h = walk.c.h, rows = walk.c.rows, row0 = walk.c.tile * C::ROWS, hi = walk.c.hi;
-    walk.unit_keys();
-    const int first = walk.first, last = walk.last;
+        const Unit u = walk.c.u;
+        const int h = walk.c.h, rows = walk.c.rows, row0 = walk.c.tile * C::ROWS, hi = walk.c.hi;
+        walk.unit_keys();
+        const int first = walk.first, last = walk.last;
 
-    // this lane's row of queries; the positions of its wave's rows
-    const int wrow = row0 + wave * 32, row = wrow + li;
-    const bool live = row < rows;
-    const int tok = min(row, rows - 1) / G, pos = u.ctx - u.all + tok;
-    const int pos_lo = u.ctx - u.all + min(wrow, rows - 1) / G, pos_hi = u.ctx - u.all + min(wrow + 31, rows - 1) / G;
-    h8 q[W::QTERMS][STEPS];
-    float fq;
-    {
-        const int hq = h * G + min(row, rows - 1) - tok * G;
-        const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)hq * a.qhs + half * 8;
-        uint32_t top = 0;
+        // this lane's row of queries; the positions of its wave's rows
+        const int wrow = row0 + wave * 32, row = wrow + li;
+        const bool live = row < rows;
+        const int tok = min(row, rows - 1) / G, pos = u.ctx - u.all + tok;
+        const int pos_lo = u.ctx - u.all + min(wrow, rows - 1) / G, pos_hi = u.ctx - u.all + min(wrow + 31, rows - 1) / G;
+        h8 q[W::QTERMS][STEPS];
+        float fq;
+        {
+            const int hq = h * G + min(row, rows - 1) - tok * G;
+            const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)hq * a.qhs + half * 8;
+            uint32_t top = 0;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            if (s * 16 >= D) continue;
-            const f32x8 v = load8(src + s * 16);
+            for (int s = 0; s < STEPS; ++s) {
+                if (s * 16 >= D) continue;
+                const f32x8 v = load8(src + s * 16);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+                for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+            }
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+            const int e = top >= kInfBits ? 0 : min(14 - exponent(top), 126);
+            const float up = ldexpf(1.f, e);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const f32x8 v = (s * 16 < D ? load8(src + s * 16) : f32x8{0, 0, 0, 0, 0, 0, 0, 0}) * up;
+                q[0][s] = __builtin_convertvector(v, h8);
+                if constexpr (W::QTERMS == 2) q[1][s] = __builtin_convertvector(v - __builtin_convertvector(q[0][s], f32x8), h8);
+            }
+            fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
+            if (top >= kInfBits) fq = __uint_as_float(0x7fc00000u);
         }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-        const int e = top >= kInfBits ? 0 : min(14 - exponent(top), 126);
-        const float up = ldexpf(1.f, e);
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const f32x8 v = (s * 16 < D ? load8(src + s * 16) : f32x8{0, 0, 0, 0, 0, 0, 0, 0}) * up;
-            q[0][s] = __builtin_convertvector(v, h8);
-            if constexpr (W::QTERMS == 2) q[1][s] = __builtin_convertvector(v - __builtin_convertvector(q[0][s], f32x8), h8);
-        }
-        fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
-        if (top >= kInfBits) fq = __uint_as_float(0x7fc00000u);
-    }
 
-    // the tiles' way into LDS: 16 bytes of a key and of a value a thread and load
-    const int32_t* table = a.table + walk.c.b * a.table_stride;
-    int pg[C::LOADS], spg = 0;
-    u4 kr[C::LOADS], vr[C::LOADS];
-    float ksr = 0.f, vsr = 0.f;
-    bool hid = false;
-    // (every thread loads, tiles past the last key load that key's, and pieces
-    // past head_dim the row's start: see load_block)
-    auto lookup = [&](int k0) {
+        // the tiles' way into LDS: 16 bytes of a key and of a value a thread and load
+        const int32_t* table = a.table + walk.c.b * a.table_stride;
+        int pg[C::LOADS], spg = 0;
+        u4 kr[C::LOADS], vr[C::LOADS];
+        float ksr = 0.f, vsr = 0.f;
+        bool hid = false;
+        // (every thread loads, tiles past the last key load that key's, and pieces
+        // past head_dim the row's start: see load_block)
+        auto lookup = [&](int k0) {
 #pragma unroll
-        for (int i = 0; i < C::LOADS; ++i) pg[i] = table[sp.page(min(k0 + (tid + i * C::THREADS) / C::CH, hi - 1))];
-        spg = table[sp.page(min(k0 + tid % KT, hi - 1))];
-    };
-    auto fetch = [&](int k0) {
-#pragma unroll
-        for (int i = 0; i < C::LOADS; ++i) {
-            const int x = tid + i * C::THREADS, c = x % C::CH, key = min(k0 + x / C::CH, hi - 1);
-            const int page = (uint32_t)pg[i] < (uint32_t)a.c.pages ? pg[i] : 0;
-            const uint64_t e = (uint64_t)(uint32_t)page * (uint32_t)(H * ps * D) +
-                               (uint32_t)((h * ps + key - sp.page(key) * ps) * D + (c * 16 < D ? c * 16 : 0));
-            kr[i] = *reinterpret_cast<const u4*>(a.c.k + e);
-            vr[i] = *reinterpret_cast<const u4*>(a.c.v + e);
-        }
-        const int key = min(k0 + tid % KT, hi - 1);
-        hid = (uint32_t)spg >= (uint32_t)a.c.pages;
-        const uint64_t e = (uint64_t)(uint32_t)(hid ? 0 : spg) * (uint32_t)(H * ps) + (uint32_t)(h * ps + key - sp.page(key) * ps);
-        ksr = a.c.k_scale[e];
-        vsr = a.c.v_scale[e];
-    };
-    auto store = [&](Buffer& to) {
-#pragma unroll
-        for (int i = 0; i < C::LOADS; ++i) {
-            const int x = tid + i * C::THREADS, c = x % C::CH, key = x / C::CH;
-            if (C::CHUNKS % C::THREADS && x >= C::CHUNKS) break;
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-                h2 x0, x1, x2, x3;
-                unpack4(biased(kr[i][2 * o]), x0, x1);
-                unpack4(biased(kr[i][2 * o + 1]), x2, x3);
-                *reinterpret_cast<h8*>(to.k + key * C::KSTRIDE + ((2 * c + o) ^ C::turn(key)) * 8) = join(x0, x1, x2, x3);
-            }
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-                h2 x0, x1, x2, x3;
-                unpack4(biased(vr[i][2 * o]), x0, x1);
-                unpack4(biased(vr[i][2 * o + 1]), x2, x3);
-                *reinterpret_cast<h8*>(to.v + key * C::VSTRIDE + (2 * c + o) * 8) = join(x0, x1, x2, x3);
-            }
-        }
-        if (wave == 0) {  // (the KT scales lie in its lanes)
-            const uint32_t top = lanes_max(lane < KT && !hid ? magnitude(vsr) : 0u);
-            const unsigned long long bad = __ballot(lane < KT && hid);
-            if (lane < KT) {
-                to.ks[lane] = ksr;
-                to.vs[lane] = vsr;
-            }
-            if (lane == 0) {
-                to.hidden = bad;
-                to.top = exponent(top);
-            }
-        }
-    };
-
-    f32x16 o[DT];
-#pragma unroll
-    for (int t = 0; t < DT; ++t) o[t] = f32x16{0};
-    float m = kMinusInf, l = 0.f;  // the running maximum is of scores / fq
-    int E = kLowestE;
-
-    auto compute = [&](const Buffer& from, int k0) {
-        f32x16 s[SUB];
-        // byte address of this lane's piece 0 of key li; piece c is that xor 32 c
-        uint32_t kaddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)reinterpret_cast<const char*>(from.k) +
-                         li * (2 * C::KSTRIDE) + ((half ^ C::turn(li)) * 16);
-        asm volatile("" : "+v"(kaddr));  // (kept in one register, not in one for every c)
-#pragma unroll
-        for (int t = 0; t < SUB; ++t) s[t] = f32x16{0};
-        h8 kf[3][SUB];  // keys are read two steps ahead of their products
-        auto read = [&](int c) {
-#pragma unroll
-            for (int t = 0; t < SUB; ++t) kf[c % 3][t] = *(__attribute__((address_space(3))) const h8*)(uintptr_t)((kaddr ^ (c * 32)) + t * 32 * (2 * C::KSTRIDE));
+            for (int i = 0; i < C::LOADS; ++i) pg[i] = table[sp.page(min(k0 + (tid + i * C::THREADS) / C::CH, hi - 1))];
+            spg = table[sp.page(min(k0 + tid % KT, hi - 1))];
         };
-        read(0);
-        read(1);
+        auto fetch = [&](int k0) {
 #pragma unroll
-        for (int c = 0; c < STEPS; ++c) {
-            if (c + 2 < STEPS) read(c + 2);
-            __builtin_amdgcn_sched_barrier(0);  // (left alone, the compiler puts each read right before its use)
+            for (int i = 0; i < C::LOADS; ++i) {
+                const int x = tid + i * C::THREADS, c = x % C::CH, key = min(k0 + x / C::CH, hi - 1);
+                const int page = (uint32_t)pg[i] < (uint32_t)a.c.pages ? pg[i] : 0;
+                const uint64_t e = (uint64_t)(uint32_t)page * (uint32_t)(H * ps * D) +
+                                   (uint32_t)((h * ps + key - sp.page(key) * ps) * D + (c * 16 < D ? c * 16 : 0));
+                kr[i] = *reinterpret_cast<const u4*>(a.c.k + e);
+                vr[i] = *reinterpret_cast<const u4*>(a.c.v + e);
+            }
+            const int key = min(k0 + tid % KT, hi - 1);
+            hid = (uint32_t)spg >= (uint32_t)a.c.pages;
+            const uint64_t e = (uint64_t)(uint32_t)(hid ? 0 : spg) * (uint32_t)(H * ps) + (uint32_t)(h * ps + key - sp.page(key) * ps);
+            ksr = a.c.k_scale[e];
+            vsr = a.c.v_scale[e];
+        };
+        auto store = [&](Buffer& to) {
 #pragma unroll
-            for (int t = 0; t < SUB; ++t)
+            for (int i = 0; i < C::LOADS; ++i) {
+                const int x = tid + i * C::THREADS, c = x % C::CH, key = x / C::CH;
+                if (C::CHUNKS % C::THREADS && x >= C::CHUNKS) break;
 #pragma unroll
-                for (int i = 0; i < W::QTERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[c % 3][t], q[i][c], s[t], 0, 0, 0);
+                for (int o = 0; o < 2; ++o) {
+                    h2 x0, x1, x2, x3;
+                    unpack4(biased(kr[i][2 * o]), x0, x1);
+                    unpack4(biased(kr[i][2 * o + 1]), x2, x3);
+                    *reinterpret_cast<h8*>(to.k + key * C::KSTRIDE + ((2 * c + o) ^ C::turn(key)) * 8) = join(x0, x1, x2, x3);
+                }
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    h2 x0, x1, x2, x3;
+                    unpack4(biased(vr[i][2 * o]), x0, x1);
+                    unpack4(biased(vr[i][2 * o + 1]), x2, x3);
+                    *reinterpret_cast<h8*>(to.v + key * C::VSTRIDE + (2 * c + o) * 8) = join(x0, x1, x2, x3);
+                }
+            }
+            if (wave == 0) {  // (the KT scales lie in its lanes)
+                const uint32_t top = lanes_max(lane < KT && !hid ? magnitude(vsr) : 0u);
+                const unsigned long long bad = __ballot(lane < KT && hid);
+                if (lane < KT) {
+                    to.ks[lane] = ksr;
+                    to.vs[lane] = vsr;
+                }
+                if (lane == 0) {
+                    to.hidden = bad;
+                    to.top = exponent(top);
+                }
+            }
+        };
+
+        f32x16 o[DT];
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[t] = f32x16{0};
+        float m = kMinusInf, l = 0.f;  // the running maximum is of scores / fq
+        int E = kLowestE;
+
+        auto compute = [&](const Buffer& from, int k0) {
+            f32x16 s[SUB];
+            // byte address of this lane's piece 0 of key li; piece c is that xor 32 c
+            uint32_t kaddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)reinterpret_cast<const char*>(from.k) +
+                             li * (2 * C::KSTRIDE) + ((half ^ C::turn(li)) * 16);
+            asm volatile("" : "+v"(kaddr));  // (kept in one register, not in one for every c)
+#pragma unroll
+            for (int t = 0; t < SUB; ++t) s[t] = f32x16{0};
+            h8 kf[3][SUB];  // keys are read two steps ahead of their products
+            auto read = [&](int c) {
+#pragma unroll
+                for (int t = 0; t < SUB; ++t) kf[c % 3][t] = *(__attribute__((address_space(3))) const h8*)(uintptr_t)((kaddr ^ (c * 32)) + t * 32 * (2 * C::KSTRIDE));
+            };
+            read(0);
+            read(1);
+#pragma unroll
+            for (int c = 0; c < STEPS; ++c) {
+                if (c + 2 < STEPS) read(c + 2);
+                __builtin_amdgcn_sched_barrier(0);  // (left alone, the compiler puts each read right before its use)
+#pragma unroll
+                for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                    for (int i = 0; i < W::QTERMS; ++i) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[c % 3][t], q[i][c], s[t], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             __builtin_amdgcn_sched_barrier(0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        const uint64_t hidden = (uint64_t)uniform((int64_t)from.hidden);
-        const bool all = k0 + KT - 1 <= pos_lo && k0 + KT <= last && hidden == 0 && (!a.window || k0 > pos_hi - a.window);
-        auto scales = [&](const float* p, int t, int g) { return *reinterpret_cast<const v4f*>(p + 32 * t + 8 * g + 4 * half); };
+            const uint64_t hidden = (uint64_t)uniform((int64_t)from.hidden);
+            const bool all = k0 + KT - 1 <= pos_lo && k0 + KT <= last && hidden == 0 && (!a.window || k0 > pos_hi - a.window);
+            auto scales = [&](const float* p, int t, int g) { return *reinterpret_cast<const v4f*>(p + 32 * t + 8 * g + 4 * half); };
 #pragma unroll
-        for (int t = 0; t < SUB; ++t)
+            for (int t = 0; t < SUB; ++t)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const v4f ks = scales(from.ks, t, g);
+                for (int g = 0; g < 4; ++g) {
+                    const v4f ks = scales(from.ks, t, g);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[t][4 * g + i] *= ks[i];
+                    for (int i = 0; i < 4; ++i) s[t][4 * g + i] *= ks[i];
+                }
+            int En = max(E, __builtin_amdgcn_readfirstlane(min(from.top, 126)));
+            if (!all) {
+                // this lane's keys k0 + 4 half + x: seen from x = from_x up to to_x
+                const int j0 = k0 + 4 * half, to_x = live ? min(pos, last - 1) - j0 : -1;
+                const int from_x = a.window ? pos - a.window + 1 - j0 : 0;
+                uint32_t vtop = 0;
+#pragma unroll
+                for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const v4f vs = scales(from.vs, t, g);
+                        const uint32_t hid8 = (uint32_t)(hidden >> (32 * t + 8 * g)) >> (4 * half);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int x = 32 * t + 8 * g + i;
+                            const bool see = x <= to_x && x >= from_x && !(hid8 >> i & 1);
+                            s[t][4 * g + i] = see ? s[t][4 * g + i] : kMinusInf;
+                            vtop = max(vtop, see ? magnitude(vs[i]) : 0u);
+                        }
+                    }
+                vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 32, 64));
+                En = max(E, min(exponent(vtop), 126));
             }
-        int En = max(E, __builtin_amdgcn_readfirstlane(min(from.top, 126)));
-        if (!all) {
-            // this lane's keys k0 + 4 half + x: seen from x = from_x up to to_x
-            const int j0 = k0 + 4 * half, to_x = live ? min(pos, last - 1) - j0 : -1;
-            const int from_x = a.window ? pos - a.window + 1 - j0 : 0;
-            uint32_t vtop = 0;
+            float top = kMinusInf;
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const v4f vs = scales(from.vs, t, g);
-                    const uint32_t hid8 = (uint32_t)(hidden >> (32 * t + 8 * g)) >> (4 * half);
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float mn = fmaxf(m, top), m0 = mn == kMinusInf ? 0.f : mn;
+            if (__any(mn > m || En > E)) {
+                const float f = ldexpf(exp2_fast((m - m0) * fq), E - En);
+                l *= f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int x = 32 * t + 8 * g + i;
-                        const bool see = x <= to_x && x >= from_x && !(hid8 >> i & 1);
-                        s[t][4 * g + i] = see ? s[t][4 * g + i] : kMinusInf;
-                        vtop = max(vtop, see ? magnitude(vs[i]) : 0u);
+                for (int t = 0; t < DT; ++t) o[t] *= f;
+                m = mn;
+                E = En;
+            }
+            const float lift = m0 * fq - kLift + (float)E;  // weights and l are 2^(14 - E) times p
+            float least = 1.f;
+            auto weigh = [&](auto whole) {
+#pragma unroll
+                for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const v4f vs = scales(from.vs, t, g);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = s[t][4 * g + i];
+                            const float p = exp2_fast(x * fq - lift);
+                            l += p;
+                            // (the scale of an entry that is not seen may be a NaN)
+                            s[t][4 * g + i] = p * (whole.value || x != kMinusInf ? vs[i] : 0.f);
+                            least = fminf(least, s[t][4 * g + i]);
+                        }
                     }
-                }
-            vtop = max(vtop, (uint32_t)__shfl_xor((int)vtop, 32, 64));
-            En = max(E, min(exponent(vtop), 126));
-        }
-        float top = kMinusInf;
+            };
+            if (all)
+                weigh(std::true_type{});
+            else
+                weigh(std::false_type{});
+            auto values = [&](int t, int x, int d) {
+                // rows 32 t + 16 x + 8 {0, 1} + 4 half + 0..3, columns 32 d + 0..31, transposed
+                const _Float16* p = from.v + (32 * t + 16 * x + 4 * half + (lane & 15) / 4) * C::VSTRIDE + 32 * d + (lane & 16) + (lane & 3) * 4;
+                const h4 y0 = read_transposed(p), y1 = read_transposed(p + 8 * C::VSTRIDE);
+                return h8{y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
+            };
+            if (__any(least < W::least)) {
 #pragma unroll
-        for (int t = 0; t < SUB; ++t)
+                for (int t = 0; t < SUB; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float mn = fmaxf(m, top), m0 = mn == kMinusInf ? 0.f : mn;
-        if (__any(mn > m || En > E)) {
-            const float f = ldexpf(exp2_fast((m - m0) * fq), E - En);
-            l *= f;
+                    for (int x = 0; x < 2; ++x) {
+                        f32x8 pv;
 #pragma unroll
-            for (int t = 0; t < DT; ++t) o[t] *= f;
-            m = mn;
-            E = En;
-        }
-        const float lift = m0 * fq - kLift + (float)E;  // weights and l are 2^(14 - E) times p
-        float least = 1.f;
-        auto weigh = [&](auto whole) {
+                        for (int i = 0; i < 8; ++i) pv[i] = s[t][8 * x + i];
+                        b8 w[W::SMALL];
+                        W::take_small(pv, w);
 #pragma unroll
-            for (int t = 0; t < SUB; ++t)
+                        for (int i = 0; i < 8; ++i) s[t][8 * x + i] = pv[i];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const v4f vs = scales(from.vs, t, g);
+                        for (int d = 0; d < DT; ++d) {
+                            const b8 v = to_bf16(values(t, x, d));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float x = s[t][4 * g + i];
-                        const float p = exp2_fast(x * fq - lift);
-                        l += p;
-                        // (the scale of an entry that is not seen may be a NaN)
-                        s[t][4 * g + i] = p * (whole.value || x != kMinusInf ? vs[i] : 0.f);
-                        least = fminf(least, s[t][4 * g + i]);
+                            for (int i = 0; i < W::SMALL; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[i], o[d], 0, 0, 0);
+                            asm volatile("" ::: "memory");  // (the values are read again below: kept, they would take its registers)
+                        }
                     }
-                }
-        };
-        if (all)
-            weigh(std::true_type{});
-        else
-            weigh(std::false_type{});
-        auto values = [&](int t, int x, int d) {
-            // rows 32 t + 16 x + 8 {0, 1} + 4 half + 0..3, columns 32 d + 0..31, transposed
-            const _Float16* p = from.v + (32 * t + 16 * x + 4 * half + (lane & 15) / 4) * C::VSTRIDE + 32 * d + (lane & 16) + (lane & 3) * 4;
-            const h4 y0 = read_transposed(p), y1 = read_transposed(p + 8 * C::VSTRIDE);
-            return h8{y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
-        };
-        if (__any(least < W::least)) {
+            }
+            h8 vf[3];  // values, two products ahead
+            vf[0] = values(0, 0, 0);
+            vf[1] = values(0, 0, 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
@@ -911,89 +948,65 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
                     f32x8 pv;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) pv[i] = s[t][8 * x + i];
-                    b8 w[W::SMALL];
-                    W::take_small(pv, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) s[t][8 * x + i] = pv[i];
+                    h8 w[W::TERMS];
+                    W::terms(pv, w);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
-                        const b8 v = to_bf16(values(t, x, d));
+                        const int n = (t * 2 + x) * DT + d, n2 = n + 2;
+                        if (n2 < SUB * 2 * DT) vf[n2 % 3] = values(n2 / DT / 2, n2 / DT % 2, n2 % DT);
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int i = 0; i < W::SMALL; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[i], o[d], 0, 0, 0);
-                        asm volatile("" ::: "memory");  // (the values are read again below: kept, they would take its registers)
+                        for (int i = 0; i < W::TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n % 3], w[i], o[d], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                 }
-        }
-        h8 vf[3];  // values, two products ahead
-        vf[0] = values(0, 0, 0);
-        vf[1] = values(0, 0, 1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int t = 0; t < SUB; ++t)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                f32x8 pv;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) pv[i] = s[t][8 * x + i];
-                h8 w[W::TERMS];
-                W::terms(pv, w);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const int n = (t * 2 + x) * DT + d, n2 = n + 2;
-                    if (n2 < SUB * 2 * DT) vf[n2 % 3] = values(n2 / DT / 2, n2 / DT % 2, n2 % DT);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int i = 0; i < W::TERMS; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n % 3], w[i], o[d], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-    };
+        };
 
-    if (first < last) {
-        lookup(first);
-        fetch(first);
-        lookup(first + KT);
-        store(buf[0]);
-        fetch(first + KT);
-        __syncthreads();
-        int at_buf = 0;
-        for (int k0 = first; k0 < last; k0 += KT) {
-            lookup(k0 + 2 * KT);
-            if (wrow < rows && k0 <= pos_hi && (!a.window || k0 + KT > pos_lo + 1 - a.window)) compute(buf[at_buf], k0);
-            store(buf[at_buf ^ 1]);
-            fetch(k0 + 2 * KT);
+        if (first < last) {
+            lookup(first);
+            fetch(first);
+            lookup(first + KT);
+            store(buf[0]);
+            fetch(first + KT);
             __syncthreads();
-            at_buf ^= 1;
+            int at_buf = 0;
+            for (int k0 = first; k0 < last; k0 += KT) {
+                lookup(k0 + 2 * KT);
+                if (wrow < rows && k0 <= pos_hi && (!a.window || k0 + KT > pos_lo + 1 - a.window)) compute(buf[at_buf], k0);
+                store(buf[at_buf ^ 1]);
+                fetch(k0 + 2 * KT);
+                __syncthreads();
+                at_buf ^= 1;
+            }
         }
-    }
-    l += __shfl_xor(l, 32, 64);
-    if (live && walk.whole) {
-        const float f = l == 0.f ? 0.f : 512.f / l;
-        const int hq = h * G + row - tok * G;
-        T* out = static_cast<T*>(a.out) + (int64_t)(u.first + tok) * a.ots + (int64_t)hq * a.ohs + 4 * half;
+        l += __shfl_xor(l, 32, 64);
+        if (live && walk.whole) {
+            const float f = l == 0.f ? 0.f : 512.f / l;
+            const int hq = h * G + row - tok * G;
+            T* out = static_cast<T*>(a.out) + (int64_t)(u.first + tok) * a.ots + (int64_t)hq * a.ohs + 4 * half;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                if (32 * d + 8 * g >= D) continue;
-                store4(out + 32 * d + 8 * g, v4f{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]} * f);
-            }
-    } else if (live) {
-        const int64_t part = ((int64_t)walk.share * 2 + !walk.head) * C::ROWS + wave * 32 + li;
-        float* out = ws.o + part * D + 4 * half;
+                for (int g = 0; g < 4; ++g) {
+                    if (32 * d + 8 * g >= D) continue;
+                    store4(out + 32 * d + 8 * g, v4f{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]} * f);
+                }
+        } else if (live) {
+            const int64_t part = ((int64_t)walk.share * 2 + !walk.head) * C::ROWS + wave * 32 + li;
+            float* out = ws.o + part * D + 4 * half;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                if (32 * d + 8 * g >= D) continue;
-                v4f v;
+                for (int g = 0; g < 4; ++g) {
+                    if (32 * d + 8 * g >= D) continue;
+                    v4f v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = ldexpf(o[d][4 * g + i], E - 14 + 9);
-                *reinterpret_cast<v4f*>(out + 32 * d + 8 * g) = v;
-            }
-        if (half == 0) ws.ml[part] = make_float2(m == kMinusInf ? kMinusInf : m * fq, ldexpf(l, E - 14));
-    }
-    if (!walk.next(a, G)) break;
+                    for (int i = 0; i < 4; ++i) v[i] = ldexpf(o[d][4 * g + i], E - 14 + 9);
+                    *reinterpret_cast<v4f*>(out + 32 * d + 8 * g) = v;
+                }
+            if (half == 0) ws.ml[part] = make_float2(m == kMinusInf ? kMinusInf : m * fq, ldexpf(l, E - 14));
+        }
+        if (!walk.next(a, G)) break;
     }  // (the tiles' last barrier lies behind every read of LDS)
 }
 
@@ -1017,50 +1030,50 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Par
     static_assert(WAVES == 1 || ROUNDS == 1, "");
 #pragma unroll 1
     for (int round = 0; round < ROUNDS; ++round) {
-    const int rr = (blockIdx.y * ROUNDS + round) * (4 / WAVES) + wave / WAVES, row = at.tile * ROWS + rr;
-    if (row >= u.n * G) return;  // (with four waves a row: all of them)
-    auto part = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0)) * ROWS + rr; };
-    float M = kMinusInf, L = 0.f;
-    for (int i = lane; i < count; i += 64) M = fmaxf(M, ws.ml[part(i)].x);
+        const int rr = (blockIdx.y * ROUNDS + round) * (4 / WAVES) + wave / WAVES, row = at.tile * ROWS + rr;
+        if (row >= u.n * G) return;  // (with four waves a row: all of them)
+        auto part = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0)) * ROWS + rr; };
+        float M = kMinusInf, L = 0.f;
+        for (int i = lane; i < count; i += 64) M = fmaxf(M, ws.ml[part(i)].x);
 #pragma unroll
-    for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
-    auto factor = [&](float m) { return m == kMinusInf ? 1.f : exp2_fast(m - M); };  // (a part that saw nothing, or a NaN)
-    for (int i = lane; i < count; i += 64) L += ws.ml[part(i)].y * factor(ws.ml[part(i)].x);
-    L = lanes_sum(L);
-    float v[4] = {0, 0, 0, 0};
-    for (int i0 = 0; i0 < count; i0 += 64 * WAVES) {
-        const int mine = i0 + lane * WAVES + turn;  // this lane's part
-        const float f = mine < count ? factor(ws.ml[part(mine)].x) : 0.f;
-        const int parts = min(64, (count - i0 - turn + WAVES - 1) / WAVES);
-        for (int i = 0; i < parts; i += 4) {  // (past the last: the last, not added)
-            float w[4][4];
+        for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+        auto factor = [&](float m) { return m == kMinusInf ? 1.f : exp2_fast(m - M); };  // (a part that saw nothing, or a NaN)
+        for (int i = lane; i < count; i += 64) L += ws.ml[part(i)].y * factor(ws.ml[part(i)].x);
+        L = lanes_sum(L);
+        float v[4] = {0, 0, 0, 0};
+        for (int i0 = 0; i0 < count; i0 += 64 * WAVES) {
+            const int mine = i0 + lane * WAVES + turn;  // this lane's part
+            const float f = mine < count ? factor(ws.ml[part(mine)].x) : 0.f;
+            const int parts = min(64, (count - i0 - turn + WAVES - 1) / WAVES);
+            for (int i = 0; i < parts; i += 4) {  // (past the last: the last, not added)
+                float w[4][4];
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
+                for (int y = 0; y < 4; ++y)
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    w[y][x] = ws.o[part(i0 + min(i + y, parts - 1) * WAVES + turn) * D + min(lane + 64 * x, D - 1)];
+                    for (int x = 0; x < 4; ++x)
+                        w[y][x] = ws.o[part(i0 + min(i + y, parts - 1) * WAVES + turn) * D + min(lane + 64 * x, D - 1)];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const float fi = __shfl(f, min(i + y, 63), 64);
+                for (int y = 0; y < 4; ++y) {
+                    const float fi = __shfl(f, min(i + y, 63), 64);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) v[x] += i + y < parts ? w[y][x] * fi : 0.f;
+                    for (int x = 0; x < 4; ++x) v[x] += i + y < parts ? w[y][x] * fi : 0.f;
+                }
             }
         }
-    }
-    if constexpr (WAVES > 1) {
-        __shared__ float red[WAVES][256];
+        if constexpr (WAVES > 1) {
+            __shared__ float red[WAVES][256];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) red[turn][lane + 64 * x] = v[x];
-        __syncthreads();
-        if (turn) return;
+            for (int x = 0; x < 4; ++x) red[turn][lane + 64 * x] = v[x];
+            __syncthreads();
+            if (turn) return;
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w)
+            for (int w = 1; w < WAVES; ++w)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] += red[w][lane + 64 * x];
-    }
+                for (int x = 0; x < 4; ++x) v[x] += red[w][lane + 64 * x];
+        }
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-        if (lane + 64 * x < D) store_row<T>(a, u, at.h, G, row, lane + 64 * x, L == 0.f ? 0.f : v[x] / L);
+        for (int x = 0; x < 4; ++x)
+            if (lane + 64 * x < D) store_row<T>(a, u, at.h, G, row, lane + 64 * x, L == 0.f ? 0.f : v[x] / L);
     }
 }
 
@@ -1083,8 +1096,9 @@ Shares choose_shares(const AttnArgs& a) {
     const int tile = tile_rows(a), G = a.q_heads / a.c.kv_heads;
     int64_t range = a.max_context;
     if (a.window) range = std::min<int64_t>(range, (int64_t)a.window + (tile + G - 1) / G + 33);
+    const int64_t units = ((int64_t)a.max_chunk * G + tile - 1) / tile * a.seqs * a.c.kv_heads;
     Shares sh;
-    if (range <= (tile == 16 ? 1024 : 256))
+    if (range <= (tile == 16 ? 1024 : 256) && units <= 1 << 22)  // (2^32 threads a launch)
         sh.groups = 0;
     else if (tile == 16)
         sh.groups = a.c.head_dim <= 64 ? 768 : a.c.head_dim <= 128 ? 512 : 256;

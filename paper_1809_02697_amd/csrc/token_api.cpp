@@ -145,6 +145,7 @@ int neo_matmul_int8(const int8_t* xq, int64_t xq_stride, const float* x_scale, i
         if (c.rc != NEO_OK || M == 0) return c.rc;
         c.rows8(xq, xq_stride, in_features, "xq");
         c.ptr(x_scale, "x_scale") && c.aligned(x_scale, "x_scale", 4);
+        if (M > 1 << 30 || out_features > 1 << 26) c.bad(NEO_ERR_UNSUPPORTED, "M above 2^30 or out_features above 2^26");
         c.ptr(w_rows, "w_rows") && c.aligned(w_rows, "w_rows", 16);
         c.ptr(w_scale, "w_scale") && c.aligned(w_scale, "w_scale", 4);
         if (bias) c.aligned(bias, "bias", 4);
@@ -214,14 +215,14 @@ int neo_attention_paged_int8(const neo_kv_cache* cache, const void* q, int64_t q
         c.ptr(page_table, "page_table") && c.aligned(page_table, "page_table", 4);
         c.ptr(context_lens, "context_lens") && c.aligned(context_lens, "context_lens", 4);
         c.ptr(q_starts, "q_starts") && c.aligned(q_starts, "q_starts", 4);
-        if (c.rc == NEO_OK && (table_stride < 0 || (int64_t)cdiv(max_context, cache->page_size) > table_stride))
-            c.bad(NEO_ERR_SHAPE, "max_context does not fit table_stride pages");
         if (c.rc == NEO_OK && max_context > 0x7fff0000) c.bad(NEO_ERR_UNSUPPORTED, "max_context above 2^31 - 2^16");
+        if (c.rc == NEO_OK && (table_stride < 0 || ((int64_t)max_context + cache->page_size - 1) / cache->page_size > table_stride))
+            c.bad(NEO_ERR_SHAPE, "max_context does not fit table_stride pages");
         if (c.rc != NEO_OK) return c.rc;
         AttnArgs a{*cache, q, out, q_token_stride, q_head_stride, out_token_stride, out_head_stride, table_stride,
                    page_table, context_lens, q_starts, tokens, q_heads, seqs, std::min(max_chunk, tokens), max_context,
                    window, scale};
-        if ((int64_t)a.max_chunk * q_heads * seqs > 0x7fffffff / 8)
+        if ((int64_t)a.max_chunk * q_heads > (1 << 28) / seqs)
             return c.bad(NEO_ERR_UNSUPPORTED, "max_chunk * q_heads * seqs above 2^28"), c.rc;
         float* ws = nullptr;
         if (const size_t need = attention_workspace(dtype, a)) {

@@ -734,3 +734,46 @@ def test_attention_many_sequences(torch):
     chunks = [1 if i % 3 == 0 else 0 for i in range(n)]
     _attend(torch, "float16", chunks, contexts, 2, 1, 64, 16, seed=120)
     _attend(torch, "float16", [c * 3 for c in chunks], contexts, 16, 1, 64, 16, seed=121)
+
+
+# ---- sizes past a launch's ---------------------------------------------------------------
+
+def test_sizes_past_every_launch_are_refused():
+    def product(M, N):
+        return neo.lib().neo_matmul_int8(FAKE, 64, FAKE, M, 64, FAKE, FAKE, N, None, 0, BF16, FAKE, N, None)
+    assert product((1 << 30) + 1, 8) == -4 and product(8, (1 << 26) + 1) == -4
+
+    def attention(page=16, Hq=4, chunk=2, seqs=2, most=100, stride=8):
+        return neo.lib().neo_attention_paged_int8(_struct(page_size=page, head_dim=16), FAKE, 256, 64, 0x7fffffff, Hq, F16, FAKE, stride,
+                                                  FAKE, FAKE, seqs, chunk, most, 0.125, 0, FAKE, 256, 64, None)
+    for n in (0x7ffffffe, 1 << 29, 1 << 21):   # products of three sizes past 64 bits
+        assert attention(Hq=n, chunk=n, seqs=n) == -4
+    assert attention(page=1 << 25, most=0x7ffeffff) == -2 and "table_stride" in neo.last_error()
+
+
+@gpu
+def test_more_rows_than_a_launch_has(torch):
+    """17 million rows of one value: s = |x| / 127 (1 for zero), q = +-127, every padding byte 0."""
+    rows = 4 * (1 << 22) + 333
+    gen = torch.Generator(device="cuda").manual_seed(41)
+    x = torch.randn((rows, 1), generator=gen, device="cuda")
+    q, s = neo.quantize_tokens_int8(x)
+    top = np.abs(x[:, 0].cpu().numpy())
+    assert np.array_equal(s.cpu().numpy(), np.where(top == 0, np.float32(1), top / np.float32(127)))
+    assert torch.equal(q[:, 0], (x[:, 0].sign() * 127).to(torch.int8)) and not q[:, 1:].any()
+
+
+@gpu
+def test_product_of_more_tokens_than_a_grid_has(torch):
+    M, K, N = 64 * 65535 + 100, 1024, 5
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("not enough device memory")
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    xq = torch.randint(-127, 128, (M, K), generator=gen, device="cuda", dtype=torch.int8)
+    wq = torch.randint(-127, 128, (N, K), generator=gen, device="cuda", dtype=torch.int8)
+    xs, ws = torch.rand(M, generator=gen, device="cuda"), torch.rand(N, generator=gen, device="cuda")
+    y = neo.matmul_int8(xq, xs, K, wq, ws, N, dtype=torch.float32)
+    for at in (0, M // 2, M - 4000):
+        part = slice(at, at + 4000)
+        acc = xq[part].cpu().double() @ wq.cpu().double().T
+        assert torch.equal(y[part].cpu(), acc.float() * xs[part, None].cpu() * ws[None].cpu())
