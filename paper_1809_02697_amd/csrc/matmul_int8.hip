@@ -357,8 +357,9 @@ struct Cost {
     int resident;      // workgroups a CU holds
     float step[2];     // us a step of 128 with one workgroup a CU, with all
 };
-// (256 x 256: 2.3 us a step is 1.87 POP/s; 8192^3 587 us against 648 in tiles of
+// (256 x 256: 2.3 us a step is 1.87 POP/s; 8192^3 at the same clock 587 us against 648 in tiles of
 // 128 x 128; 1003 x 2049 -> 1001 11.2 us in 64 x 64 against 23.8 in 128 x 128;
+// 32 x 16,384 -> 4096 17.6 us in 32 x 128 against 18.3 in 64 x 64;
 // 96 x 16,384 -> 4096 24.5 us in 64 x 128 and four splits, 68.9 by matmul_rows)
 constexpr Cost kCosts[] = {{k256x256, 256, 256, 1, {2.3f, 2.3f}}, {k128x128, 128, 128, 2, {0.9f, 1.27f}},
                            {k64x128, 64, 128, 1, {0.56f, 0.56f}}, {k64x64, 64, 64, 2, {0.48f, 0.58f}},

@@ -1,8 +1,9 @@
 """Python binding of libneo (ctypes).  Argument marshalling only: every
 operation runs in the HIP kernels of ``libneo.so``; there is no fallback.
 
-Device tensors are ``torch`` float32 CUDA (HIP) tensors; torch supplies the
-memory and the current stream.  Names follow the C-ABI in ``include/neo.h``.
+Device tensors are ``torch`` CUDA (HIP) tensors, float32 for the convolutional
+path and float32, float16 or bfloat16 for the token operators; torch supplies
+the memory and the current stream.  Names follow the C-ABI in ``include/neo.h``.
 """
 from __future__ import annotations
 
