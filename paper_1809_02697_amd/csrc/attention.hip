@@ -21,6 +21,7 @@
 #include <atomic>
 #include <type_traits>
 
+#include "attention_keys.h"
 #include "token_types.h"
 
 namespace neo {
@@ -121,12 +122,6 @@ __device__ inline Unit unit_of(const AttnArgs& a, int b) {
     u.end = min(u.ctx, a.max_context);
     return u;
 }
-// The keys [lo, hi) that the chunk's tokens t0 .. t1 see.
-__device__ inline void key_range(const AttnArgs& a, const Unit& u, int t0, int t1, int& lo, int& hi) {
-    hi = min(u.end, u.ctx - u.all + t1 + 1);
-    lo = a.window ? max(0, u.ctx - u.all + t0 + 1 - a.window) : 0;
-    hi = max(hi, lo);
-}
 
 // ---- shares ---------------------------------------------------------------------------
 // A unit of work is a row tile of a sequence's key/value head; its keys are
@@ -181,7 +176,7 @@ struct Cursor {
     int skip;                     // blocks of the unit that lie before the share
 
     __device__ static int tile_blocks(const AttnArgs& a, const Unit& u, int rows, int G, int tile, int& lo, int& hi) {
-        key_range(a, u, tile * ROWS / G, (min(tile * ROWS + ROWS, rows) - 1) / G, lo, hi);
+        seen_keys(u.ctx, u.all, u.end, tile * ROWS / G, (min(tile * ROWS + ROWS, rows) - 1) / G, a.window, lo, hi);
         lo &= ~31;
         return kUnitCost + max(1, (hi - lo + BLK - 1) / BLK);
     }
@@ -469,6 +464,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
         // this lane's row of queries: values d = g * KB + ...
         const int row = min(row0 + li, rows - 1), tok = row / G, pos = u.ctx - u.all + tok;
         const int pos_lo = u.ctx - u.all + row0 / G, pos_hi = u.ctx - u.all + (min(row0 + 16, rows) - 1) / G;
+        const int from_hi = first_seen(pos_hi, a.window);
         h8 q[W::QTERMS][STEPS];
         float fq;  // what a score is multiplied with
         {
@@ -525,11 +521,11 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
                 }
             }
 
-            const bool all = kb + 32 <= last && kb + 31 <= pos_lo && (!a.window || kb > pos_hi - a.window) &&
+            const bool all = kb + 32 <= last && kb + 31 <= pos_lo && kb >= from_hi &&
                              __all(kv.there == 0xff);
             if (!all) {
                 // this lane's keys j0 + x: seen from x = from_x up to to_x
-                const int j0 = kb + 4 * g, to_x = min(pos, last - 1) - j0, from_x = a.window ? pos - a.window + 1 - j0 : 0;
+                const int j0 = kb + 4 * g, to_x = min(pos, last - 1) - j0, from_x = first_seen(pos, a.window) - j0;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -717,6 +713,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
         const bool live = row < rows;
         const int tok = min(row, rows - 1) / G, pos = u.ctx - u.all + tok;
         const int pos_lo = u.ctx - u.all + min(wrow, rows - 1) / G, pos_hi = u.ctx - u.all + min(wrow + 31, rows - 1) / G;
+        const int from_lo = first_seen(pos_lo, a.window), from_hi = first_seen(pos_hi, a.window);
         h8 q[W::QTERMS][STEPS];
         float fq;
         {
@@ -839,7 +836,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             }
             __builtin_amdgcn_sched_barrier(0);
             const uint64_t hidden = (uint64_t)uniform((int64_t)from.hidden);
-            const bool all = k0 + KT - 1 <= pos_lo && k0 + KT <= last && hidden == 0 && (!a.window || k0 > pos_hi - a.window);
+            const bool all = k0 + KT - 1 <= pos_lo && k0 + KT <= last && hidden == 0 && k0 >= from_hi;
             auto scales = [&](const float* p, int t, int g) { return *reinterpret_cast<const v4f*>(p + 32 * t + 8 * g + 4 * half); };
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
@@ -853,7 +850,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             if (!all) {
                 // this lane's keys k0 + 4 half + x: seen from x = from_x up to to_x
                 const int j0 = k0 + 4 * half, to_x = live ? min(pos, last - 1) - j0 : -1;
-                const int from_x = a.window ? pos - a.window + 1 - j0 : 0;
+                const int from_x = first_seen(pos, a.window) - j0;
                 uint32_t vtop = 0;
 #pragma unroll
                 for (int t = 0; t < SUB; ++t)
@@ -972,7 +969,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             int at_buf = 0;
             for (int k0 = first; k0 < last; k0 += KT) {
                 lookup(k0 + 2 * KT);
-                if (wrow < rows && k0 <= pos_hi && (!a.window || k0 + KT > pos_lo + 1 - a.window)) compute(buf[at_buf], k0);
+                if (wrow < rows && k0 <= pos_hi && k0 + KT > from_lo) compute(buf[at_buf], k0);
                 store(buf[at_buf ^ 1]);
                 fetch(k0 + 2 * KT);
                 __syncthreads();

@@ -777,3 +777,67 @@ def test_product_of_more_tokens_than_a_grid_has(torch):
         part = slice(at, at + 4000)
         acc = xq[part].cpu().double() @ wq.cpu().double().T
         assert torch.equal(y[part].cpu(), acc.float() * xs[part, None].cpu() * ws[None].cpu())
+
+
+# ---- windows beyond the bounds -------------------------------------------------------------
+
+def _attention64_below(q, k, v, ks, vs, table, contexts, starts, most, scale, window):
+    """_attention64 where tokens from `most` on are not computed."""
+    T, Hq, D = q.shape
+    H, page = k.shape[1], k.shape[2]
+    out, A, B = np.zeros((T, Hq, D)), np.zeros((T, Hq, D)), np.zeros((T, Hq, 1))
+    for b, c in enumerate(contexts):
+        n = int(starts[b + 1] - starts[b])
+        for i in range(n):
+            p = c - n + i
+            j = np.arange(max(0, p + 1 - window) if window else 0, min(p + 1, most))
+            if not len(j):
+                continue
+            pages = table[b, j // page]
+            for h in range(Hq):
+                kk, vv = (x[pages, h * H // Hq, j % page].astype(np.float64) * s[pages, h * H // Hq, j % page][:, None]
+                          for x, s in ((k, ks), (v, vs)))
+                row = q[starts[b] + i, h]
+                s = kk @ row * scale
+                w = np.exp(s - s.max())
+                out[starts[b] + i, h], A[starts[b] + i, h] = w @ vv / w.sum(), w @ np.abs(vv) / w.sum()
+                B[starts[b] + i, h] = (np.abs(kk) @ np.abs(row)).max() * scale
+    return out, A, B
+
+
+@gpu
+@pytest.mark.parametrize("page", [16, 10])
+@pytest.mark.parametrize("chunk", [4, 40])
+@pytest.mark.parametrize("window", [10, 100, 2 ** 31 - 1])
+def test_attention_window_beyond_the_bounds(torch, window, chunk, page):
+    """Contexts just and far above max_context under a window: what lies past
+    max_context is not there, and a window that lies there wholly sees nothing."""
+    H, D, most = 2, 64, 64
+    contexts = [65, 70, 100, 5000, 1 << 30, 2 ** 31 - 1, 64]
+    k, v, ks, vs, table = _paged(torch, [most] * len(contexts), H, D, page, 60)
+    starts = (np.arange(len(contexts) + 1) * chunk).astype(np.int32)
+    q = _rand(torch, (len(contexts) * chunk, 4, D), "float16", 61)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    got = _np(neo.attention_paged_int8((c(k), c(v), c(ks), c(vs)), q.cuda(), c(table), c(np.array(contexts, np.int32)), c(starts),
+                                       chunk, most, scale=0.125, window=window))
+    ref, A, B = _attention64_below(q.double().numpy(), k, v, ks, vs, table, contexts, starts, most, 0.125, window)
+    assert (got[ref == 0] == 0).all() and (np.abs(got - ref) <= _attention_bound(ref, A, B, D, most, "float16")).all()
+    if window <= 100:
+        assert (got[3 * chunk:6 * chunk] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("chunk", [5, 40, 300])
+def test_attention_window_past_every_length(torch, chunk):
+    """A window near 2^31 limits nothing: the bits of no window, also where a
+    chunk has more tokens than its context."""
+    H, D, page, contexts = 2, 64, 16, [0, 3, 64]
+    k, v, ks, vs, table = _paged(torch, [20, 20, 64], H, D, page, 62)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    cache, starts = (c(k), c(v), c(ks), c(vs)), c((np.arange(4) * chunk).astype(np.int32))
+    q = _rand(torch, (3 * chunk, 4, D), "bfloat16", 63).cuda()
+    run = lambda w: neo.attention_paged_int8(cache, q, c(table), c(np.array(contexts, np.int32)), starts, chunk, 64, window=w)  # noqa: E731
+    plain = run(0)
+    assert torch.isfinite(plain).all() and (plain[chunk + max(0, chunk - 3):2 * chunk] != 0).any()
+    for w in (2 ** 31 - 1, 2 ** 31 - 2, 1 << 30):
+        assert torch.equal(run(w), plain)
