@@ -523,8 +523,13 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
 
             const bool all = kb + 32 <= last && kb + 31 <= pos_lo && kb >= from_hi &&
                              __all(kv.there == 0xff);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[t][r] *= kv.ks[t][r] * fq;
             if (!all) {
-                // this lane's keys j0 + x: seen from x = from_x up to to_x
+                // this lane's keys j0 + x: seen from x = from_x up to to_x (after
+                // the scales, which may be NaN)
                 const int j0 = kb + 4 * g, to_x = min(pos, last - 1) - j0, from_x = first_seen(pos, a.window) - j0;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -533,7 +538,6 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
                         const int x = 16 * t + r;
                         const bool see = x <= to_x && x >= from_x && (kv.there >> (4 * t + r) & 1);
                         s[t][r] = see ? s[t][r] : kMinusInf;
-                        kv.ks[t][r] = see ? kv.ks[t][r] : 1.f;
                         kv.vs[t][r] = see ? kv.vs[t][r] : 0.f;
                     }
             }
@@ -543,7 +547,6 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    s[t][r] *= kv.ks[t][r] * fq;
                     top = fmaxf(top, s[t][r]);
                     vtop = max(vtop, magnitude(kv.vs[t][r]));
                 }
@@ -732,7 +735,9 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             const float up = ldexpf(1.f, e);
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                const f32x8 v = (s * 16 < D ? load8(src + s * 16) : f32x8{0, 0, 0, 0, 0, 0, 0, 0}) * up;
+                // (a query with an infinity is the factor below alone: no score of it is
+                // the minus infinity of a masked key)
+                const f32x8 v = (s * 16 < D && top < kInfBits ? load8(src + s * 16) : f32x8{0, 0, 0, 0, 0, 0, 0, 0}) * up;
                 q[0][s] = __builtin_convertvector(v, h8);
                 if constexpr (W::QTERMS == 2) q[1][s] = __builtin_convertvector(v - __builtin_convertvector(q[0][s], f32x8), h8);
             }
@@ -877,7 +882,8 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float mn = fmaxf(m, top), m0 = mn == kMinusInf ? 0.f : mn;
             if (__any(mn > m || En > E)) {
-                const float f = ldexpf(exp2_fast((m - m0) * fq), E - En);
+                // (a row that has seen nothing holds zeros, whatever its query)
+                const float f = m == kMinusInf ? 0.f : ldexpf(exp2_fast((m - m0) * fq), E - En);
                 l *= f;
 #pragma unroll
                 for (int t = 0; t < DT; ++t) o[t] *= f;
@@ -895,10 +901,11 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float x = s[t][4 * g + i];
-                            const float p = exp2_fast(x * fq - lift);
+                            // (of a key that is not seen nothing counts: its scale and the query's may be NaN)
+                            const bool there = whole.value || x != kMinusInf;
+                            const float p = there ? exp2_fast(x * fq - lift) : 0.f;
                             l += p;
-                            // (the scale of an entry that is not seen may be a NaN)
-                            s[t][4 * g + i] = p * (whole.value || x != kMinusInf ? vs[i] : 0.f);
+                            s[t][4 * g + i] = there ? p * vs[i] : 0.f;
                             least = fminf(least, s[t][4 * g + i]);
                         }
                     }

@@ -841,3 +841,37 @@ def test_attention_window_past_every_length(torch, chunk):
     assert torch.isfinite(plain).all() and (plain[chunk + max(0, chunk - 3):2 * chunk] != 0).any()
     for w in (2 ** 31 - 1, 2 ** 31 - 2, 1 << 30):
         assert torch.equal(run(w), plain)
+
+
+# ---- masked keys of queries without a finite score -----------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("chunks,contexts", [([5], [3]), ([40], [30]), ([5, 5], [3, 2000]), ([1200], [1100]), ([40, 3], [30, 900])])
+def test_attention_bad_query_that_sees_nothing(torch, chunks, contexts, dtype):
+    """Zeros for a token that sees nothing, also where its query holds an infinity
+    or a NaN and tokens of its tile see keys; those keep their bits."""
+    H, D, page = 1, 64, 16
+    k, v, ks, vs, table = _paged(torch, contexts, H, D, page, 64)
+    starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    run = lambda q: neo.attention_paged_int8((c(k), c(v), c(ks), c(vs)), q.cuda(), c(table), c(np.array(contexts, np.int32)),  # noqa: E731
+                                             c(starts), max(chunks), max(contexts)).cpu()
+    q = _rand(torch, (int(starts[-1]), 2, D), dtype, 65)
+    good = run(q)
+    unseen = chunks[0] - contexts[0]
+    q[0, 1, 3], q[unseen - 1, 0, 60] = float("inf"), float("nan")     # see nothing
+    assert (good[:unseen] == 0).all() and torch.equal(run(q), good)
+    q[unseen, 1, 0] = float("-inf")                                   # sees the first key
+    got = run(q)
+    assert torch.isnan(got[unseen, 1]).all()
+    got[unseen, 1] = good[unseen, 1]
+    assert torch.equal(got, good)
+
+
+@gpu
+@pytest.mark.parametrize("chunks,contexts,window", [([1, 33], [70, 50], 0), ([1, 4], [70, 1500], 0), ([300], [700], 90)])
+def test_attention_scores_below_float32(torch, chunks, contexts, window):
+    """Queries and a scale so small that their product is no float32: every seen
+    key weighs the same, masked ones nothing."""
+    _attend(torch, "float32", chunks, contexts, 4, 2, 64, 16, window, seed=66, scale=1e-30, spread=1e-30)
