@@ -680,6 +680,16 @@ const char* neo_last_error(void);
  * succeeds and does nothing.  Sums, norms and softmax statistics are float32
  * (int32 for integer products, exact).  Results do not depend on other work
  * on the device: the same call gives the same bits.
+ *
+ * The workspace of the stream: calls that split their work (neo_matmul_int8,
+ * neo_attention_paged_int8, and neo_conv2d_nchwxc, neo_conv2d_blocked and
+ * neo_conv2d_winograd above) keep parts in one buffer per (device, stream),
+ * which the library owns and grows outside stream capture.  A call under
+ * capture leaves the buffer's address in the graph, so that buffer is kept
+ * until the process ends, also when later calls get a larger one.  A replay
+ * uses it as a call on the captured stream would: replays of graphs captured on
+ * one stream, and that stream's own calls, must be ordered among each other (by
+ * one stream, or by events).
  * ====================================================================================== */
 enum neo_dtype { NEO_F32 = 0, NEO_F16 = 1, NEO_BF16 = 2 };
 

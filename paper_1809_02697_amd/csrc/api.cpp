@@ -4,12 +4,10 @@
 #include <cstdio>
 #include <cstdlib>
 #include <limits>
-#include <map>
-#include <mutex>
 #include <string>
-#include <utility>
 
 #include "neo_internal.h"
+#include "workspace.h"
 
 namespace neo {
 
@@ -117,19 +115,24 @@ void from_kernel_order(const float* in, const ConvShape& s, float* packed) {
 
 namespace {
 
-// Split-reduction workspace of the standalone calls, one per
-// (device, stream) so that calls on different streams never share it; calls
-// on one stream are ordered by the stream.  Grows on demand (hipFree of the
-// old buffer, hipMalloc of the new one); a call that would grow it while the
-// stream is being captured into a graph fails with NEO_ERR_STATE and launches
-// nothing (allocation is not capturable), so the first call of a given size
-// must be made outside capture.
-struct StreamWs {
-    float* ws = nullptr;
-    size_t bytes = 0;
+// The workspaces of the standalone calls (workspace.h) on this device.  A call
+// whose buffer would have to grow while its stream is being captured fails with
+// NEO_ERR_STATE and launches nothing, so the first call of a given size must be
+// made outside capture.
+struct HipDevice {
+    typedef hipStream_t stream;
+    typedef hipError_t error;
+    static hipError_t alloc(size_t bytes, float** p) { return hipMalloc(p, bytes); }
+    static hipError_t free(float* p) { return hipFree(p); }
+    static hipError_t capturing(hipStream_t st, bool* yes) {
+        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+        const hipError_t e = hipStreamIsCapturing(st, &cap);
+        if (e != hipSuccess) (void)hipGetLastError();  // (reported here; not the next launch's error)
+        *yes = cap != hipStreamCaptureStatusNone;
+        return e;
+    }
 };
-std::mutex g_ws_mu;
-std::map<std::pair<int, hipStream_t>, StreamWs> g_ws;
+Workspaces<HipDevice> g_workspaces;
 
 }  // namespace
 
@@ -137,33 +140,23 @@ int stream_workspace(const char* fn, hipStream_t st, size_t bytes, float** ws) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return hip_fail(e, (std::string(fn) + ": hipGetDevice").c_str());
-    std::lock_guard<std::mutex> lk(g_ws_mu);
-    StreamWs& w = g_ws[{dev, st}];
-    if (w.bytes < bytes) {
-        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-        e = hipStreamIsCapturing(st, &cap);
-        if (e != hipSuccess) return hip_fail(e, (std::string(fn) + ": hipStreamIsCapturing").c_str());
-        if (cap != hipStreamCaptureStatusNone)
+    switch (g_workspaces.get(dev, st, bytes, ws, &e)) {
+        case WorkspaceError::kNone:
+            return NEO_OK;
+        case WorkspaceError::kStatus:
+            return hip_fail(e, (std::string(fn) + ": hipStreamIsCapturing").c_str());
+        case WorkspaceError::kCapturing:
             return fail(NEO_ERR_STATE, std::string(fn) + ": the split-reduction workspace must "
                                        "grow to " + std::to_string(bytes) + " bytes, which "
                                        "cannot happen during stream capture; make one call of "
                                        "this size outside capture first");
-        if (w.ws) {
-            e = hipFree(w.ws);
-            w.ws = nullptr;
-            w.bytes = 0;
-            if (e != hipSuccess) return hip_fail(e, (std::string(fn) + ": hipFree of the workspace").c_str());
-        }
-        e = hipMalloc(&w.ws, bytes);
-        if (e != hipSuccess) {
-            w.ws = nullptr;
-            return fail(NEO_ERR_OOM, std::string(fn) + ": workspace allocation of " +
-                                         std::to_string(bytes) + " bytes: " + hipGetErrorString(e));
-        }
-        w.bytes = bytes;
+        case WorkspaceError::kFree:
+            return hip_fail(e, (std::string(fn) + ": hipFree of the workspace").c_str());
+        case WorkspaceError::kAlloc:
+            break;
     }
-    *ws = w.ws;
-    return NEO_OK;
+    return fail(NEO_ERR_OOM, std::string(fn) + ": workspace allocation of " + std::to_string(bytes) +
+                                 " bytes: " + hipGetErrorString(e));
 }
 
 }  // namespace neo

@@ -875,3 +875,50 @@ def test_attention_scores_below_float32(torch, chunks, contexts, window):
     """Queries and a scale so small that their product is no float32: every seen
     key weighs the same, masked ones nothing."""
     _attend(torch, "float32", chunks, contexts, 4, 2, 64, 16, window, seed=66, scale=1e-30, spread=1e-30)
+
+
+# ---- the workspace ------------------------------------------------------------------------
+
+@gpu
+def test_graphs_outlive_a_larger_workspace(torch):
+    """Graphs of calls that split their work, captured from small to large on one
+    stream: after larger calls there, and new tensors where freed memory would
+    lie, every replay gives the eager bits."""
+    H, D, page = 2, 128, 16
+    k, v, ks, vs, table = _paged(torch, [3000, 2500], H, D, page, 70)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    cache, table, ctx = (c(k), c(v), c(ks), c(vs)), c(table), c(np.array([3000, 2500], np.int32))
+    gen = torch.Generator(device="cuda").manual_seed(71)
+
+    def attention(n):
+        q = torch.randn((2 * n, 4 * H, D), generator=gen, device="cuda").bfloat16()
+        starts = torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda")
+        return lambda: neo.attention_paged_int8(cache, q, table, ctx, starts, n, 3000)
+
+    def product(M, K=16384, N=304):
+        x, w = (torch.randint(-127, 128, (r, K), generator=gen, device="cuda", dtype=torch.int8) for r in (M, N))
+        xs, ws = torch.rand(M, generator=gen, device="cuda"), torch.rand(N, generator=gen, device="cuda")
+        return lambda: neo.matmul_int8(x, xs, K, w, ws, N)
+
+    side = torch.cuda.Stream()
+    graphs = []
+    calls = product(40), attention(1), product(200), attention(20), attention(300)   # (they hold the graphs' inputs)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for call in calls:
+            eager = call().clone()
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                got = call()
+            graphs.append((g, got, eager))
+            filler = [torch.full((1 << 22,), float("nan"), device="cuda") for _ in range(8)]
+        for _ in range(3):
+            for g, got, eager in graphs:
+                got.zero_()
+                g.replay()
+                torch.cuda.synchronize()
+                assert torch.equal(got, eager)
+            calls[2]()
+            torch.cuda.synchronize()
+    assert all(torch.isnan(f).all() for f in filler)
