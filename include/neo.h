@@ -689,7 +689,8 @@ const char* neo_last_error(void);
  * until the process ends, also when later calls get a larger one.  A replay
  * uses it as a call on the captured stream would: replays of graphs captured on
  * one stream, and that stream's own calls, must be ordered among each other (by
- * one stream, or by events).
+ * one stream, or by events).  Several threads may call on one stream: a call
+ * that uses the buffer queues its launches without another's between them.
  * ====================================================================================== */
 enum neo_dtype { NEO_F32 = 0, NEO_F16 = 1, NEO_BF16 = 2 };
 

@@ -7,7 +7,6 @@
 #include <string>
 
 #include "neo_internal.h"
-#include "workspace.h"
 
 namespace neo {
 
@@ -136,7 +135,7 @@ Workspaces<HipDevice> g_workspaces;
 
 }  // namespace
 
-int stream_workspace(const char* fn, hipStream_t st, size_t bytes, float** ws) {
+int stream_workspace(const char* fn, hipStream_t st, size_t bytes, Workspace* ws) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return hip_fail(e, (std::string(fn) + ": hipGetDevice").c_str());
@@ -365,12 +364,12 @@ int neo_conv2d_nchwxc(const float* x, int x_block, int N, int C, int H, int W,
                           stride_h, stride_w, pad_h, pad_w, ep, y, y_block, y_blk_offset,
                           y_blk_total, &s, &cfg, &res);
     if (rc != NEO_OK) return rc;
-    float* ws = nullptr;
+    Workspace ws;
     if (cfg.split > 1) {
         rc = stream_workspace("neo_conv2d_blocked", (hipStream_t)stream, conv_workspace_bytes(s, cfg), &ws);
         if (rc != NEO_OK) return rc;
     }
-    hipError_t e = launch_conv2d(s, cfg, x, w_packed, false, bias, res, y, ws,
+    hipError_t e = launch_conv2d(s, cfg, x, w_packed, false, bias, res, y, ws.ptr,
                                  (hipStream_t)stream);
     return e == hipSuccess ? NEO_OK : hip_fail(e, "neo_conv2d_nchwxc launch");
 }
@@ -439,12 +438,12 @@ int neo_conv2d_winograd(const float* x, int N, int C, int H, int W, const float*
         return fail(NEO_ERR_UNSUPPORTED, "neo_conv2d_winograd: transformed filter of 2 GiB or more");
     cfg = choose_wino_config(s);
     env_wino_config(s, &cfg);
-    float* ws = nullptr;
+    Workspace ws;
     if (cfg.split > 1) {
         rc = stream_workspace("neo_conv2d_blocked", (hipStream_t)stream, conv_workspace_bytes(s, cfg), &ws);
         if (rc != NEO_OK) return rc;
     }
-    hipError_t e = launch_wino(s, cfg, x, u, bias, res, y, ws, (hipStream_t)stream);
+    hipError_t e = launch_wino(s, cfg, x, u, bias, res, y, ws.ptr, (hipStream_t)stream);
     return e == hipSuccess ? NEO_OK : hip_fail(e, "neo_conv2d_winograd launch");
 }
 

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "../../include/neo.h"
+#include "workspace.h"
 
 namespace neo {
 
@@ -20,9 +21,10 @@ void set_error(const std::string& msg);
 int fail(int code, const std::string& msg);
 int hip_fail(hipError_t e, const char* what);
 
-// The workspace of (current device, stream), at least `bytes` large; `fn`
-// leads its error messages.  Grown outside stream capture only.
-int stream_workspace(const char* fn, hipStream_t st, size_t bytes, float** ws);
+// The workspace of (current device, stream), at least `bytes` large, held until
+// *ws goes, that is past the call's last launch; `fn` leads its error messages.
+// Grown outside stream capture only.
+int stream_workspace(const char* fn, hipStream_t st, size_t bytes, Workspace* ws);
 
 inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 // log2 of a power of two

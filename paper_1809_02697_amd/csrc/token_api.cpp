@@ -152,12 +152,12 @@ int neo_matmul_int8(const int8_t* xq, int64_t xq_stride, const float* x_scale, i
         c.data(y, y_stride, out_features, dtype, "y");
         if (c.rc != NEO_OK) return c.rc;
         MatmulArgs a{xq, w_rows, x_scale, w_scale, bias, y, xq_stride, y_stride, M, out_features, cdiv(in_features, 16) * 16, act, dtype};
-        float* ws = nullptr;
+        Workspace ws;
         if (const size_t need = matmul_int8_workspace(a)) {
             const int rc = stream_workspace(c.fn, (hipStream_t)stream, need, &ws);
             if (rc != NEO_OK) return rc;
         }
-        return c.launched(launch_matmul_int8(a, ws, (hipStream_t)stream));
+        return c.launched(launch_matmul_int8(a, ws.ptr, (hipStream_t)stream));
     });
 }
 
@@ -224,11 +224,11 @@ int neo_attention_paged_int8(const neo_kv_cache* cache, const void* q, int64_t q
                    window, scale};
         if ((int64_t)a.max_chunk * q_heads > (1 << 28) / seqs)
             return c.bad(NEO_ERR_UNSUPPORTED, "max_chunk * q_heads * seqs above 2^28"), c.rc;
-        float* ws = nullptr;
+        Workspace ws;
         if (const size_t need = attention_workspace(dtype, a)) {
             const int rc = stream_workspace(c.fn, (hipStream_t)stream, need, &ws);
             if (rc != NEO_OK) return rc;
         }
-        return c.launched(launch_attention(dtype, a, ws, (hipStream_t)stream));
+        return c.launched(launch_attention(dtype, a, ws.ptr, (hipStream_t)stream));
     });
 }

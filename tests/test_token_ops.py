@@ -922,3 +922,39 @@ def test_graphs_outlive_a_larger_workspace(torch):
             calls[2]()
             torch.cuda.synchronize()
     assert all(torch.isnan(f).all() for f in filler)
+
+
+@gpu
+def test_threads_on_one_stream(torch):
+    """Threads whose calls split their work on one stream, of different needs: each gets its own results."""
+    import threading
+    H, D, page = 2, 128, 16
+    k, v, ks, vs, table = _paged(torch, [3000], H, D, page, 72)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    cache, table, ctx = (c(k), c(v), c(ks), c(vs)), c(table), c(np.array([3000], np.int32))
+
+    def attention(n):
+        q = _rand(torch, (n, 4 * H, D), "bfloat16", 73 + n).cuda()
+        starts = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        return lambda: neo.attention_paged_int8(cache, q, table, ctx, starts, n, 3000)
+
+    def product(M, K=16384, N=304):
+        x, w = (torch.randint(-127, 128, (r, K), device="cuda", dtype=torch.int8) for r in (M, N))
+        xs, ws = torch.rand(M, device="cuda"), torch.rand(N, device="cuda")
+        return lambda: neo.matmul_int8(x, xs, K, w, ws, N)
+
+    calls = [attention(1), attention(40), product(40), product(200)]
+    right = [f() for f in calls]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(f, expect):
+        for _ in range(5):
+            got = [f() for _ in range(40)]
+            wrong.extend(1 for g in got if not torch.equal(g, expect))
+    threads = [threading.Thread(target=run, args=a) for a in zip(calls, right)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(100)
+    assert not any(t.is_alive() for t in threads) and not wrong

@@ -3,6 +3,7 @@ device of pretence: what is kept, freed, refused and shared."""
 import ctypes
 import os
 import subprocess
+import threading
 
 import pytest
 
@@ -41,11 +42,18 @@ neo::Workspaces<Pretence> table;
 extern "C" {
 // the buffer, or minus the error
 long get(int dev, long st, long bytes) {
-    float* ws = nullptr;
+    neo::Workspace ws;
     int e = 0;
     const neo::WorkspaceError r = table.get(dev, st, bytes, &ws, &e);
-    return r == neo::WorkspaceError::kNone ? (long)ws : -(long)r;
+    return r == neo::WorkspaceError::kNone ? (long)ws.ptr : -(long)r;
 }
+// the same, held until let_go on the same thread
+static thread_local neo::Workspace mine;
+long hold(int dev, long st, long bytes) {
+    int e = 0;
+    return table.get(dev, st, bytes, &mine, &e) == neo::WorkspaceError::kNone ? (long)mine.ptr : 0;
+}
+void let_go() { mine = neo::Workspace(); }
 void capture(long st, int on) {
     if (on) Pretence::under_capture.insert(st);
     else Pretence::under_capture.erase(st);
@@ -64,6 +72,7 @@ def host(tmp_path):
                     str(tmp_path / "shim.cpp")], check=True, timeout=100)
     L = ctypes.CDLL(str(tmp_path / "shim.so"))
     L.get.restype, L.get.argtypes = ctypes.c_long, [ctypes.c_int, ctypes.c_long, ctypes.c_long]
+    L.hold.restype, L.hold.argtypes = L.get.restype, L.get.argtypes
     L.is_freed.argtypes = [ctypes.c_long]
     return L
 
@@ -112,3 +121,35 @@ def test_errors(host):
     assert host.get(0, 7, 40) > 0                                       # the next call that fits
     host.set_room(1 << 30)
     assert host.get(0, 7, 101) > 0
+
+
+def test_a_call_holds_its_buffer_until_its_launches_are_queued(host):
+    """Calls of two threads on one stream come one after the other, and the second,
+    larger one does not free what the first still launches with; other streams go on."""
+    queue, taken, go = [], threading.Event(), threading.Event()
+
+    def first():
+        p = host.hold(0, 7, 100)
+        queue.append("first main")
+        taken.set()
+        go.wait(20)
+        queue.append("first join" if not host.is_freed(p) else "freed")
+        host.let_go()
+
+    def second():
+        taken.wait(20)
+        p = host.hold(0, 7, 200)
+        queue.extend(["second main", "second join"])
+        host.let_go()
+        assert p > 0
+
+    threads = [threading.Thread(target=f) for f in (first, second)]
+    for t in threads:
+        t.start()
+    assert taken.wait(20)
+    threads[1].join(0.3)
+    assert threads[1].is_alive() and host.get(0, 8, 100) > 0 and host.get(1, 7, 100) > 0
+    go.set()
+    for t in threads:
+        t.join(20)
+    assert queue == ["first main", "first join", "second main", "second join"]
