@@ -670,7 +670,7 @@ const char* neo_last_error(void);
  * Quantization of a row of values v: s = max|v| / 127 in float32 (1 for a row
  * of zeros; at least the smallest normal float), q = clamp(round_half_even(v /
  * s), -127, 127), the division in float32.  A row with an infinity or a NaN
- * gets s = NaN and q = 0, so whatever is computed from it is NaN.
+ * gets s = NaN and q = 0, so whatever is computed from it is NaN, past a ReLU too.
  * int8 rows are padded with zero bytes to INp = ceil(cols / 16) * 16, their
  * pointers 16-byte aligned and their strides multiples of 16 (NEO_ERR_ALIGN).
  * Pointers to float data (float32, float16, bfloat16: enum neo_dtype) need

@@ -21,7 +21,7 @@ __device__ inline float epilogue(int acc, float xs, float ws, const float* bias,
 #pragma clang fp contract(off)
     float v = (float)acc * xs * ws;
     if (bias) v += bias[n];
-    return act == NEO_ACT_RELU ? fmaxf(v, 0.f) : v;
+    return act == NEO_ACT_RELU && v < 0.f ? 0.f : v;  // (a NaN stays one)
 }
 
 // Four neighbouring channels of a token, n < N the first; the callers' branch on

@@ -958,3 +958,23 @@ def test_threads_on_one_stream(torch):
     for t in threads:
         t.join(100)
     assert not any(t.is_alive() for t in threads) and not wrong
+
+
+# ---- NaN past an activation ------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("M,K,N", [(3, 2, 2), (5, 4096, 30), (30, 500, 70), (70, 16384, 304), (150, 300, 270), (600, 2000, 700)])
+def test_matmul_of_a_bad_row_with_an_activation(torch, M, K, N, act):
+    """A token with a NaN scale is NaN past a ReLU too, in the product of few tokens,
+    in tiles and where in_features are split; the other tokens keep their values."""
+    x = _rand(torch, (M, K), "float32", 80)
+    w, ws = neo.pack_dense_int8(_rand(torch, (N, K), "float32", 81).cuda())
+    bias = _rand(torch, (N,), "float32", 82).cuda()
+    good = neo.matmul_int8(*neo.quantize_tokens_int8(x.cuda()), K, w, ws, N, bias=bias, act=act, dtype=torch.float32)
+    x[M // 2, K // 2], x[M - 1, 0] = float("nan"), float("-inf")
+    got = neo.matmul_int8(*neo.quantize_tokens_int8(x.cuda()), K, w, ws, N, bias=bias, act=act, dtype=torch.float32)
+    bad = [M // 2, M - 1]
+    assert torch.isnan(got[bad]).all()
+    got[bad] = good[bad]
+    assert torch.equal(got, good) and torch.isfinite(good).all() and (act == "none" or (good >= 0).all())
