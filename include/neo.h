@@ -697,7 +697,9 @@ enum neo_dtype { NEO_F32 = 0, NEO_F16 = 1, NEO_BF16 = 2 };
 /*
  * Residual addition, root-mean-square norm, quantization:
  *   h = x + residual,  y = h / sqrt(mean(h^2) + eps) * gamma,  (yq, y_scale) = quantized y
- * evaluated in float32 from the unrounded h; h and y rounded once.
+ * evaluated in float32 from the unrounded h, without its squares leaving the
+ * range of normal floats; h and y rounded once.  A row of zeros gives zeros,
+ * with eps = 0 too.
  *   x         device [rows][cols] of `dtype`
  *   residual  device, the same shape and type, or NULL (h = x)
  *   gamma     device float32 [cols], or NULL (ones)

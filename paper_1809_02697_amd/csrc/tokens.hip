@@ -96,17 +96,20 @@ __global__ __launch_bounds__((WAVES > 4 ? WAVES : 4) * 64) void row_int8(RowsArg
             return ss;
         };
         float ss = sum_squares(0), eps = a.eps;
-        if (!(ss < __uint_as_float(kInfBits))) {
-            // Squares past float32's range (or an infinity, a NaN): the same
-            // norm of the row times 2^-80, whose squares stay in range.
-            const float down = 0x1p-80f;
+        const bool over = !(ss < __uint_as_float(kInfBits)), under = ss / (float)a.cols + eps < 0x1p-100f;
+        if (over || under) {
+            // Squares past float32's range (or an infinity, a NaN), or so small that
+            // they lose bits below it: the same norm of the row times 2^-80, or 2^100,
+            // whose squares stay in range.
+            const float by = over ? 0x1p-80f : 0x1p100f;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) v[c] *= down;
-            eps *= down;
-            eps *= down;
+            for (int c = 0; c < CH; ++c) v[c] *= by;
+            eps *= by;
+            eps *= by;
             ss = sum_squares(1);
         }
-        const float inv = 1.f / sqrtf(ss / (float)a.cols + eps);
+        const float mean = ss / (float)a.cols + eps;
+        const float inv = mean == 0.f ? 0.f : 1.f / sqrtf(mean);  // (a row of zeros with eps 0 is zeros)
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int j = (c * THREADS + tid) * 8, n = a.cols - j;

@@ -978,3 +978,32 @@ def test_matmul_of_a_bad_row_with_an_activation(torch, M, K, N, act):
     assert torch.isnan(got[bad]).all()
     got[bad] = good[bad]
     assert torch.equal(got, good) and torch.isfinite(good).all() and (act == "none" or (good >= 0).all())
+
+
+# ---- norms of small rows -----------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("eps", [0.0, 1e-42, 1e-36])
+@pytest.mark.parametrize("rows,cols", [(7, 40), (7, 1500), (7, 5000), (7, 12000), (700, 4000)])
+def test_norm_of_small_rows(torch, rows, cols, eps, dtype):
+    """Rows whose squares lie below float32's normal numbers, eps 0 and next to it;
+    a row of zeros is zeros (the bounds are test_norm's)."""
+    x = _rand(torch, (rows, cols), "float32", 90)
+    for i, m in enumerate([1e-18, 1e-20, 1e-23, 1e-30, 1e-38, 1e-42]):
+        x[i] *= m
+    x[6] = 0
+    x = x.to(getattr(torch, dtype))
+    x64 = x.double().numpy()
+    with np.errstate(invalid="ignore"):
+        y64 = x64 / np.sqrt((x64 ** 2).mean(1, keepdims=True) + float(np.float32(eps)))
+    y64[~x64.any(1)] = 0     # (1e-42 is 0 in bfloat16)
+    slack = (cols / 64 + 16) * U["float32"] / 2 + 4 * U["float32"]
+    y = torch.full((rows, cols), float("nan"), dtype=x.dtype, device="cuda")
+    q, s, h = neo.rmsnorm_int8(x.cuda(), None, eps, h=torch.empty_like(x, device="cuda"), y=y)
+    assert torch.equal(h.cpu(), x)
+    assert (np.abs(_np(y) - y64) <= (slack + U[dtype] * (1 + slack)) * np.abs(y64) + TINY[dtype]).all()
+    q, s = q.cpu().numpy().astype(np.float64), _np(s)
+    far = np.abs(y64).max(1) / 127 >= 2.0 ** -126      # (smaller scales are held at the least normal float)
+    _step_check(q[far, :cols], s[far], y64[far], slack)
+    assert s[6] == 1 and not q[6].any() and not q[:, cols:].any()
