@@ -23,11 +23,17 @@ enum { kNorm, kPlain, kGate };
 // instructions instead of the 40 of expf and a division, which bound the rows
 // of few tokens.
 __device__ inline float silu(float g) {
-    constexpr float kLog2eHi = 1.44269502f, kLog2eLo = 1.92596299e-8f;
+    constexpr float kLog2eHi = 1.44269502f, kLog2eLo = 1.92596299e-8f, kLn2 = 0.693147181f;
     const float hi = -g * kLog2eHi, lo = fmaf(-g, kLog2eHi, -hi) - g * kLog2eLo;
+    if (hi >= 125.f) {
+        // The reciprocal of such a sum lies below the normal numbers, which the
+        // instruction makes 0: g exp(g), 2^64 times as large until it is rounded.
+        // (Far past float32's range lo is noise, and the result -0.)
+        const float e = __builtin_amdgcn_exp2f(64.f - hi);
+        return g * (hi < 256.f ? fmaf(e, lo * -kLn2, e) : e) * 0x1p-64f;
+    }
     float e = __builtin_amdgcn_exp2f(hi);
-    // (past float32's range lo is noise: exp is 0 or infinite there)
-    if (fabsf(hi) < 126.f) e = fmaf(e, lo * 0.693147181f, e);
+    if (hi > -126.f) e = fmaf(e, lo * kLn2, e);
     return g * __builtin_amdgcn_rcpf(1.f + e);
 }
 

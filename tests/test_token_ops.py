@@ -1007,3 +1007,26 @@ def test_norm_of_small_rows(torch, rows, cols, eps, dtype):
     far = np.abs(y64).max(1) / 127 >= 2.0 ** -126      # (smaller scales are held at the least normal float)
     _step_check(q[far, :cols], s[far], y64[far], slack)
     assert s[6] == 1 and not q[6].any() and not q[:, cols:].any()
+
+
+# ---- nearly closed gates -----------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [50, 5000])
+def test_quantize_with_nearly_closed_gates(torch, cols, dtype):
+    """Gates of -84 to -91, where exp(-g) nears and passes float32's largest number
+    and g / (1 + exp(-g)) is a normal one still; then closed ones (the bounds are
+    test_quantize_tokens')."""
+    g = torch.rand(8, cols, generator=torch.Generator().manual_seed(100)) - 84 - torch.arange(8)[:, None]
+    g = g.clamp(min=-91).to(getattr(torch, dtype))
+    x = _rand(torch, (8, cols), dtype, 101, 1e4)
+    q, s = neo.quantize_tokens_int8(x.cuda(), gate=g.cuda())
+    g64 = g.double().numpy()
+    y64 = x.double().numpy() * g64 / (1 + np.exp(-g64))
+    _step_check(q.cpu().numpy()[:, :cols].astype(np.float64), _np(s), y64, 6 * U["float32"])
+    for closed in (-250.0, -6e4, -3e38 if dtype != "float16" else -6.5e4):
+        q, s = neo.quantize_tokens_int8(x.cuda(), gate=torch.full_like(x, closed, device="cuda"))
+        assert (q == 0).all() and (s == 1).all()
+    q, s = neo.quantize_tokens_int8(x.cuda(), gate=torch.full_like(x, float("-inf"), device="cuda"))
+    assert torch.isnan(s).all()          # (infinity over infinity)
