@@ -185,6 +185,19 @@ def _stream(stream=None):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _new(x, shape, dtype, stream, fill="new_empty"):
+    """A call's own output on x's device, from the memory pool of the stream that
+    the call runs on: a block of the current stream's pool may still be in use
+    there while the kernel writes it on another."""
+    if stream is None:
+        return getattr(x, fill)(shape, dtype=dtype)
+    import torch
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        return getattr(x, fill)(shape, dtype=dtype)
+
+
 def _dptr(t, name="tensor"):
     if t is None:
         return None
@@ -242,8 +255,7 @@ def _conv_common(fn, x, xb, C, w_packed, K, R, S, bias, stride, pad, act, residu
     OH, OW = out_size(H, R, sh, ph), out_size(W, S, sw, pw)
     tot = cblocks(K, y_block) if y_tot is None else y_tot
     if out is None:
-        out = torch.empty((N, tot, max(OH, 0), max(OW, 0), y_block), device=x.device,
-                          dtype=torch.float32)
+        out = _new(x, (N, tot, max(OH, 0), max(OW, 0), y_block), torch.float32, stream)
     if OH > 0 and OW > 0:
         _need(out, N * tot * OH * OW * y_block, "out")
         _need(residual, N * cblocks(K, y_block) * OH * OW * y_block, "residual")
@@ -291,7 +303,7 @@ def layout_transform(src, src_block, dst_block, N, C, H, W, out=None, stream=Non
     import torch
     if out is None:
         shape = (N, C, H, W) if dst_block == 0 else (N, cblocks(C, dst_block), H, W, dst_block)
-        out = torch.empty(shape, device=src.device, dtype=torch.float32)
+        out = _new(src, shape, torch.float32, stream)
     _check(lib().neo_layout_transform(_dptr(src, "src"), src_block, _dptr(out, "out"), dst_block,
                                       N, C, H, W, _stream(stream)))
     return out
@@ -312,8 +324,7 @@ def pack_filter(w, ic_bn=BLOCK, oc_bn=BLOCK, out=None, stream=None):
     import torch
     K, C, R, S = w.shape
     if out is None:
-        out = torch.empty((cblocks(K, oc_bn), cblocks(C, ic_bn), R, S, ic_bn, oc_bn),
-                          device=w.device, dtype=torch.float32)
+        out = _new(w, (cblocks(K, oc_bn), cblocks(C, ic_bn), R, S, ic_bn, oc_bn), torch.float32, stream)
     _check(lib().neo_pack_filter(_dptr(w, "w"), K, C, R, S, ic_bn, oc_bn, _dptr(out, "out"),
                                  _stream(stream)))
     return out
@@ -331,7 +342,7 @@ def winograd_filter(w, out=None, stream=None):
     if (R, S) != (3, 3):
         raise ValueError("the Winograd filter transform takes 3x3 filters")
     if out is None:
-        out = torch.empty((cblocks(K), cblocks(C), 16, 256), device=w.device, dtype=torch.float32)
+        out = _new(w, (cblocks(K), cblocks(C), 16, 256), torch.float32, stream)
     _need(out, winograd_filter_floats(K, C), "out")
     _check(lib().neo_winograd_filter(_dptr(w, "w"), K, C, _dptr(out, "out"), _stream(stream)))
     return out
@@ -349,8 +360,7 @@ def conv2d_winograd(x, C, u, K, bias=None, pad=1, act="none", residual=None, out
     OH, OW = out_size(H, 3, 1, ph), out_size(W, 3, 1, pw)
     tot = cblocks(K) if y_cblk_total is None else y_cblk_total
     if out is None:
-        out = torch.empty((N, tot, max(OH, 0), max(OW, 0), BLOCK), device=x.device,
-                          dtype=torch.float32)
+        out = _new(x, (N, tot, max(OH, 0), max(OW, 0), BLOCK), torch.float32, stream)
     if OH > 0 and OW > 0:
         _need(out, N * tot * OH * OW * BLOCK, "out")
         _need(residual, N * cblocks(K) * OH * OW * BLOCK, "residual")
@@ -381,7 +391,7 @@ def quantize_int8(x, C, x_scale, pad=0, out=None, stream=None):
         raise ValueError(f"x shape {tuple(x.shape)} is not NCHW16c of {C} channels")
     shape = (N, XB, H + 2 * ph, W + 2 * pw, BLOCK)
     if out is None:
-        out = torch.empty(shape, device=x.device, dtype=torch.int8)
+        out = _new(x, shape, torch.int8, stream)
     if out.numel() < int(np.prod(shape)):
         raise ValueError(f"out holds {out.numel()} bytes, the call needs {int(np.prod(shape))}")
     _check(lib().neo_quantize_int8(_dptr(x, "x"), N, C, H, W, float(x_scale), ph, pw,
@@ -396,9 +406,9 @@ def pack_filter_int8(w, out=None, scale=None, stream=None):
     K, C, R, S = w.shape
     nb = int8_filter_bytes(K, C, R, S)
     if out is None:
-        out = torch.empty(nb, device=w.device, dtype=torch.int8)
+        out = _new(w, nb, torch.int8, stream)
     if scale is None:
-        scale = torch.empty(cblocks(K) * BLOCK, device=w.device, dtype=torch.float32)
+        scale = _new(w, cblocks(K) * BLOCK, torch.float32, stream)
     if out.numel() < nb:
         raise ValueError(f"out holds {out.numel()} bytes, the call needs {nb}")
     _need(scale, cblocks(K) * BLOCK, "scale")
@@ -420,9 +430,9 @@ def pack_dense_int8(w, out=None, scale=None, stream=None):
     OUT, IN = w.shape
     shape = (OUT, dense_row_bytes(IN))
     if out is None:
-        out = torch.empty(shape, device=w.device, dtype=torch.int8)
+        out = _new(w, shape, torch.int8, stream)
     if scale is None:
-        scale = torch.empty(OUT, device=w.device, dtype=torch.float32)
+        scale = _new(w, OUT, torch.float32, stream)
     if out.numel() < OUT * shape[1]:
         raise ValueError(f"out holds {out.numel()} bytes, the call needs {OUT * shape[1]}")
     _need(scale, OUT, "scale")
@@ -438,7 +448,7 @@ def quantize_rows_int8(x, x_scale, out=None, stream=None):
     N, IN = x.shape
     shape = (N, dense_row_bytes(IN))
     if out is None:
-        out = torch.empty(shape, device=x.device, dtype=torch.int8)
+        out = _new(x, shape, torch.int8, stream)
     if out.numel() < N * shape[1]:
         raise ValueError(f"out holds {out.numel()} bytes, the call needs {N * shape[1]}")
     _check(lib().neo_quantize_rows_int8(_dptr(x, "x"), N, IN, float(x_scale),
@@ -460,11 +470,11 @@ def dense_int8(xq, IN, w_rows, w_scale, OUT, x_scale, bias=None, act="none", out
     _need(w_scale, OUT, "w_scale")
     _need(bias, OUT, "bias")
     if out is None:
-        out = torch.empty((N, OUT), device=xq.device, dtype=torch.float32)
+        out = _new(xq, (N, OUT), torch.float32, stream)
     if out is not False:
         _need(out, N * OUT, "out")
     if y_scale is not None and out_q is None:
-        out_q = torch.zeros((N, dense_row_bytes(OUT)), device=xq.device, dtype=torch.int8)
+        out_q = _new(xq, (N, dense_row_bytes(OUT)), torch.int8, stream, "new_zeros")
     if out_q is not None and out_q.numel() < N * dense_row_bytes(OUT):
         raise ValueError(f"out_q holds {out_q.numel()} bytes, the call needs {N * dense_row_bytes(OUT)}")
     yp = None if out is False else _dptr(out, "out")
@@ -570,7 +580,7 @@ def rmsnorm_int8(x, gamma, eps=1e-5, residual=None, h=None, y=None, out=None, sc
     if residual is not None:
         rp, rs = _rows(residual, rows, cols, t, "residual")
         if h is None:
-            h = x.new_empty((rows, cols))
+            h = _new(x, (rows, cols), t, stream)
     if h is not None and h is not False:
         hp, hs = _rows(h, rows, cols, t, "h")
     if y is not None:
@@ -578,12 +588,12 @@ def rmsnorm_int8(x, gamma, eps=1e-5, residual=None, h=None, y=None, out=None, sc
     if quantize:
         if out is None:
             qs = dense_row_bytes(cols)
-            out = x.new_empty((rows, qs), dtype=_DTYPES["i8"])
+            out = _new(x, (rows, qs), _DTYPES["i8"], stream)
             qp = out.data_ptr()
         else:
             qp, qs = _rows8(out, rows, cols, "out")
         if scale is None:
-            scale = x.new_empty(rows, dtype=f32)
+            scale = _new(x, rows, f32, stream)
         sp = _vec(scale, rows, f32, "scale")
     _check(lib().neo_rmsnorm_int8(xp, xs, rp, rs, _vec(gamma, cols, f32, "gamma"), eps, rows, cols, code, hp, hs, yp, ys, qp, qs,
                                   sp, _stream(stream)))
@@ -601,12 +611,12 @@ def quantize_tokens_int8(x, gate=None, out=None, scale=None, stream=None):
     gp, gs = (None, 0) if gate is None else _rows(gate, rows, cols, t, "gate")
     if out is None:
         qs = dense_row_bytes(cols)
-        out = x.new_empty((rows, qs), dtype=_DTYPES["i8"])
+        out = _new(x, (rows, qs), _DTYPES["i8"], stream)
         qp = out.data_ptr()
     else:
         qp, qs = _rows8(out, rows, cols, "out")
     if scale is None:
-        scale = x.new_empty(rows, dtype=f32)
+        scale = _new(x, rows, f32, stream)
     _check(lib().neo_quantize_tokens_int8(xp, xs, gp, gs, rows, cols, code, qp, qs, _vec(scale, rows, f32, "scale"),
                                           _stream(stream)))
     return out, scale
@@ -618,7 +628,7 @@ def dequantize_tokens_int8(xq, x_scale, cols, dtype, out=None, stream=None):
     rows = xq.shape[0]
     qp, qs = _rows8(xq, rows, cols, "xq")
     if out is None:
-        out, ys = xq.new_empty((rows, cols), dtype=dtype), cols
+        out, ys = _new(xq, (rows, cols), dtype, stream), cols
         yp = out.data_ptr()
     else:
         yp, ys = _rows(out, rows, cols, dtype, "out")
@@ -641,7 +651,7 @@ def matmul_int8(xq, x_scale, IN, w_rows, w_scale, OUT, bias=None, act="none", dt
     M = xq.shape[0]
     qp, qs = _rows8(xq, M, IN, "xq")
     if out is None:
-        out, ys = xq.new_empty((M, OUT), dtype=dtype), OUT
+        out, ys = _new(xq, (M, OUT), dtype, stream), OUT
         yp = out.data_ptr()
     else:
         yp, ys = _rows(out, M, OUT, dtype, "out")
@@ -698,7 +708,7 @@ def kv_read_int8(cache, slots, dtype, k_out=None, v_out=None, stream=None):
     outs = []
     for o in (k_out, v_out):
         if o is None:
-            o = slots.new_empty(shape, dtype=dtype)
+            o = _new(slots, shape, dtype, stream)
         elif o.dtype != dtype or o.shape != shape:
             raise ValueError(f"an output is {tuple(o.shape)} of {o.dtype}, not {shape} of {dtype}")
         outs.append(o)
@@ -725,7 +735,7 @@ def attention_paged_int8(cache, q, page_table, context_lens, q_starts, max_chunk
     if max_context > most * c.page_size:
         raise ValueError(f"max_context {max_context} exceeds the {most} pages a sequence has")
     if out is None:
-        out, ot, oh = q.new_empty((T, Hq, D)), Hq * D, D
+        out, ot, oh = _new(q, (T, Hq, D), t, stream), Hq * D, D
         op = out.data_ptr()
     else:
         if out.dtype != t or out.shape != q.shape:
@@ -769,8 +779,7 @@ def conv2d_int8(xq, C, w_packed, w_scale, K, R, S, x_scale, bias=None, stride=1,
     N, H, W, sh, sw, ph, pw, OH, OW = _int8_args(xq, C, w_packed, K, R, S, stride, pad)
     tot = cblocks(K) if y_cblk_total is None else y_cblk_total
     if out is None:
-        out = torch.empty((N, tot, max(OH, 0), max(OW, 0), BLOCK), device=xq.device,
-                          dtype=torch.float32)
+        out = _new(xq, (N, tot, max(OH, 0), max(OW, 0), BLOCK), torch.float32, stream)
     if OH > 0 and OW > 0:
         _need(out, N * tot * OH * OW * BLOCK, "out")
         _need(residual, N * cblocks(K) * OH * OW * BLOCK, "residual")
@@ -801,7 +810,7 @@ def conv2d_int8_q(xq, C, w_packed, w_scale, K, R, S, x_scale, y_scale, bias=None
     tot = cblocks(K) if y_cblk_total is None else y_cblk_total
     shape = (N, tot, max(OH, 0) + 2 * qph, max(OW, 0) + 2 * qpw, BLOCK)
     if out is None:
-        out = torch.zeros(shape, device=xq.device, dtype=torch.int8)
+        out = _new(xq, shape, torch.int8, stream, "new_zeros")
     if OH > 0 and OW > 0:
         if out.numel() < int(np.prod(shape)):
             raise ValueError(f"out holds {out.numel()} bytes, the call needs {int(np.prod(shape))}")
@@ -827,8 +836,7 @@ def conv2d_int8_acc(xq, C, w_packed, K, R, S, stride=1, pad=0, out=None, stream=
     import torch
     N, H, W, sh, sw, ph, pw, OH, OW = _int8_args(xq, C, w_packed, K, R, S, stride, pad)
     if out is None:
-        out = torch.empty((N, cblocks(K), max(OH, 0), max(OW, 0), BLOCK), device=xq.device,
-                          dtype=torch.int32)
+        out = _new(xq, (N, cblocks(K), max(OH, 0), max(OW, 0), BLOCK), torch.int32, stream)
     if OH > 0 and OW > 0 and out.numel() < N * cblocks(K) * OH * OW * BLOCK:
         raise ValueError(f"out holds {out.numel()} values, the call needs "
                          f"{N * cblocks(K) * OH * OW * BLOCK}")
@@ -862,8 +870,7 @@ def _pool(fn, x, C, R, S, stride, pad, out, y_cblk_offset, y_cblk_total, stream,
     OH, OW = out_size(H, R, sh, ph), out_size(W, S, sw, pw)
     tot = CB if y_cblk_total is None else y_cblk_total
     if out is None:
-        out = torch.empty((N, tot, max(OH, 0), max(OW, 0), blk), device=x.device,
-                          dtype=torch.float32)
+        out = _new(x, (N, tot, max(OH, 0), max(OW, 0), blk), torch.float32, stream)
     if CB != cblocks(C, blk):
         raise ValueError(f"x shape {tuple(x.shape)} is not NCHW[{blk}]c of {C} channels")
     if OH > 0 and OW > 0:
@@ -891,7 +898,7 @@ def global_avgpool_nchwxc(x, C, out=None, stream=None):
     import torch
     N, CB, H, W, blk = x.shape
     if out is None:
-        out = torch.empty((N, CB, 1, 1, blk), device=x.device, dtype=torch.float32)
+        out = _new(x, (N, CB, 1, 1, blk), torch.float32, stream)
     _need(out, N * CB * blk, "out")
     _check(lib().neo_global_avgpool_nchwxc(_dptr(x, "x"), blk, N, C, H, W, _dptr(out, "out"),
                                            _stream(stream)))
@@ -914,7 +921,7 @@ def global_avgpool_blocked(x, C, out=None, stream=None):
     import torch
     N, CB, H, W, _ = x.shape
     if out is None:
-        out = torch.empty((N, CB, 1, 1, BLOCK), device=x.device, dtype=torch.float32)
+        out = _new(x, (N, CB, 1, 1, BLOCK), torch.float32, stream)
     _need(out, N * CB * BLOCK, "out")
     _check(lib().neo_global_avgpool_blocked(_dptr(x, "x"), N, C, H, W, _dptr(out, "out"),
                                             _stream(stream)))
@@ -927,7 +934,7 @@ def dense(x, w, bias=None, act="none", out=None, stream=None):
     N, IN = x.shape
     OUT = w.shape[0]
     if out is None:
-        out = torch.empty((N, OUT), device=x.device, dtype=torch.float32)
+        out = _new(x, (N, OUT), torch.float32, stream)
     if w.numel() != OUT * IN:
         raise ValueError(f"w holds {w.numel()} floats, not {OUT} x {IN}")
     _need(out, N * OUT, "out")
@@ -1059,7 +1066,7 @@ class Plan:
         if out is None:
             N, C, H, W = self.output_shape
             shape = (N, C) if (H, W) == (1, 1) else (N, C, H, W)
-            out = torch.empty(shape, device=x.device, dtype=torch.float32)
+            out = _new(x, shape, torch.float32, stream)
         _need(out, int(np.prod(self.output_shape)), "out")
         _check(lib().neo_run_graph(self.handle, _dptr(x, "x"), _dptr(out, "out"),
                                    _stream(stream)))
@@ -1074,7 +1081,7 @@ class Plan:
         if out is None:
             N, C, H, W = self.output_shape
             shape = (N, C) if (H, W) == (1, 1) else (N, C, H, W)
-            out = torch.empty(shape, device=x.device, dtype=torch.float32)
+            out = _new(x, shape, torch.float32, stream)
         _need(out, int(np.prod(self.output_shape)), "out")
         _check(lib().neo_plan_calibrate_int8(self.handle, _dptr(x, "x"), _dptr(out, "out"),
                                              _stream(stream)))

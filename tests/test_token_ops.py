@@ -1030,3 +1030,24 @@ def test_quantize_with_nearly_closed_gates(torch, cols, dtype):
         assert (q == 0).all() and (s == 1).all()
     q, s = neo.quantize_tokens_int8(x.cuda(), gate=torch.full_like(x, float("-inf"), device="cuda"))
     assert torch.isnan(s).all()          # (infinity over infinity)
+
+
+# ---- a given stream ------------------------------------------------------------------------------
+
+@gpu
+def test_a_given_stream_has_its_own_outputs(torch):
+    """stream=: outputs do not lie in memory that the current stream has just given
+    back, and hold what the current stream's call gives."""
+    x = _rand(torch, (512, 1024), "float32", 110).cuda()
+    q, s = neo.quantize_tokens_int8(x)
+    want = neo.dequantize_tokens_int8(q, s, 1024, torch.float32)
+    freed = torch.empty_like(want)
+    at = freed.data_ptr()
+    del freed
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = neo.dequantize_tokens_int8(q, s, 1024, torch.float32, stream=side)
+    again = torch.empty_like(want)
+    assert got.data_ptr() != at and again.data_ptr() == at
+    side.synchronize()
+    assert torch.equal(got, want)
