@@ -101,10 +101,13 @@ class Decoder:
 
     def step(self, tokens):
         """tokens: for every sequence the list of its new tokens (maybe empty).  Returns the
-        logits [sequences with new tokens][vocab] (float32) after the last of each."""
+        logits [sequences with new tokens][vocab] (float32) after the last of each.  A call that is
+        refused leaves the decoder as it was."""
         new = [len(t) for t in tokens]
         if len(tokens) != len(self.pages) or not any(new):
             raise ValueError("one list of tokens a sequence, and at least one token")
+        if not all(0 <= t < len(self.embed) for s in tokens for t in s):  # (looked up on the device it ends the process)
+            raise ValueError(f"a token outside the vocabulary of {len(self.embed)}")
         need = [-(-(n + m) // self.page_size) - len(p) for p, n, m in zip(self.pages, self.lengths, new)]
         if sum(need) > len(self.free):
             raise RuntimeError("the cache has no page left")
