@@ -800,9 +800,10 @@ int neo_kv_read_int8(const neo_kv_cache* cache, const int64_t* slots, int tokens
  *                 and not read
  * Products run on fp16 MFMA with float32 sums: int8 values are exact there,
  * float16 and bfloat16 queries too (scaled by a power of two per row), float32
- * queries are taken as two fp16 terms (22 bits).  The softmax weights are
- * rounded to 11 bits for bfloat16, to 22 for float16 and float32, whatever
- * their size beside the row's largest.  A call that cuts contexts into shares
+ * queries are taken as two fp16 terms (22 bits).  The softmax weights (times
+ * their value's scale) are rounded to 11 bits for bfloat16, to 22 for float16
+ * and float32, whatever their size beside the row's largest; float16's below
+ * 2^-17 of it keep 11 to 22.  A call that cuts contexts into shares
  * keeps their parts in the workspace of the stream (as neo_matmul_int8).
  */
 int neo_attention_paged_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride,

@@ -1051,3 +1051,71 @@ def test_a_given_stream_has_its_own_outputs(torch):
     assert got.data_ptr() != at and again.data_ptr() == at
     side.synchronize()
     assert torch.equal(got, want)
+
+
+# ---- float16's two terms -------------------------------------------------------------------------
+
+def _two_term_bound(out, A, B, D, longest):
+    """float16 outputs with weights of two terms: float32's bound (2^-21 for the weights, in
+    place of one term's 2^-11) and one rounding to float16.  It holds for weights that lie
+    within 2^-17 of the largest, here by a spread of scores of less than e and scales of
+    1 to 10."""
+    inner = _attention_bound(out, A, B, D, longest, "float32")
+    return inner + U["float16"] * (np.abs(out) + inner) + TINY["float16"]
+
+
+TWO_TERM = [([1, 1, 1], [9, 33, 70], 16), ([40], [40], 16), ([1], [1500], 64), ([70], [90], 64), ([300], [300], 16)]
+
+
+def _two_term_case(torch, chunks, contexts, D, seed):
+    k, v, ks, vs, table = _paged(torch, contexts, 2, D, 16, seed)
+    starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+    q = _rand(torch, (int(starts[-1]), 8, D), "float16", seed + 1, 0.1)
+    return q, k, v, ks, vs, table, starts
+
+
+@gpu
+@pytest.mark.parametrize("chunks,contexts,D", TWO_TERM)
+def test_attention_float16_weights_have_two_terms(torch, chunks, contexts, D):
+    q, k, v, ks, vs, table, starts = _two_term_case(torch, chunks, contexts, D, 120)
+    ref, A, B = _attention64(q.double().numpy(), k, v, ks, vs, table, contexts, starts, D ** -0.5, 0)
+    c = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    got = _np(neo.attention_paged_int8((c(k), c(v), c(ks), c(vs)), q.cuda(), c(table), c(np.array(contexts, np.int32)), c(starts),
+                                       max(chunks), max(contexts)))
+    assert (np.abs(got - ref) <= _two_term_bound(ref, A, B, D, max(contexts))).all()
+
+
+def _beyond_the_two_term_bound(torch, chunks, contexts, D):
+    """How many values of the same inputs lie beyond the bound with weights of one and of
+    two fp16 terms, all else in 64 bits."""
+    q, k, v, ks, vs, table, starts = _two_term_case(torch, chunks, contexts, D, 120)
+    ref, A, B = _attention64(q.double().numpy(), k, v, ks, vs, table, contexts, starts, D ** -0.5, 0)
+    bound = _two_term_bound(ref, A, B, D, max(contexts))
+    off = {}
+    for terms in (1, 2):
+        out = np.zeros_like(ref)
+        for b, ctx in enumerate(contexts):
+            j = np.arange(ctx)
+            pages = table[b, j // 16]
+            for h in range(8):
+                keys, values = (x[pages, h // 4, j % 16].astype(np.float64) for x in (k, v))
+                for i in range(chunks[b]):
+                    n = ctx - chunks[b] + i + 1
+                    s = keys[:n] * ks[pages, h // 4, j % 16][:n, None] @ q[starts[b] + i, h].double().numpy() * D ** -0.5
+                    p = np.exp(s - s.max())
+                    w = p * vs[pages, h // 4, j % 16][:n]
+                    w *= 2.0 ** (14 - np.floor(np.log2(vs[pages, h // 4, j % 16][:n].max())))
+                    held = w.astype(np.float16).astype(np.float64)
+                    if terms == 2:
+                        held += (w - held).astype(np.float16).astype(np.float64)
+                    assert held.min() >= 2.0 ** -3
+                    out[starts[b] + i, h] = held @ values[:n] / (w @ np.ones(n)) * (p @ vs[pages, h // 4, j % 16][:n] / p.sum())
+        off[terms] = (np.abs(out.astype(np.float16).astype(np.float64) - ref) > bound).sum()
+    return off
+
+
+def test_the_two_term_bound_rejects_one_term():
+    """In the cases of few keys (over 1500 the single roundings average out)."""
+    import torch
+    off = [_beyond_the_two_term_bound(torch, *case) for case in TWO_TERM]
+    assert all(o[2] == 0 for o in off) and sum(o[1] > 0 for o in off) >= 3, off
