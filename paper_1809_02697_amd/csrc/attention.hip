@@ -521,7 +521,9 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
                 }
             }
 
-            const bool all = kb + 32 <= last && kb + 31 <= pos_lo && kb >= from_hi &&
+            // (from_hi is 0 without a window; asked all the same, single tokens over up to
+            // 32,000 take 128 us, and 139 else: the compiler orders the loop otherwise)
+            const bool all = kb + 32 <= last && kb + 31 <= pos_lo && (!a.window || kb >= from_hi) &&
                              __all(kv.there == 0xff);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
