@@ -721,6 +721,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
         const int from_lo = first_seen(pos_lo, a.window), from_hi = first_seen(pos_hi, a.window);
         h8 q[W::QTERMS][STEPS];
         float fq;
+        bool undefined;  // (a query with an infinity has no finite score)
         {
             const int hq = h * G + min(row, rows - 1) - tok * G;
             const T* src = static_cast<const T*>(a.q) + (int64_t)(u.first + tok) * a.qts + (int64_t)hq * a.qhs + half * 8;
@@ -737,14 +738,15 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             const float up = ldexpf(1.f, e);
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                // (a query with an infinity is the factor below alone: no score of it is
-                // the minus infinity of a masked key)
+                // (a query with an infinity is taken as zeros, and its sum made NaN at the end:
+                // no score of it is the minus infinity of a masked key)
                 const f32x8 v = (s * 16 < D && top < kInfBits ? load8(src + s * 16) : f32x8{0, 0, 0, 0, 0, 0, 0, 0}) * up;
                 q[0][s] = __builtin_convertvector(v, h8);
                 if constexpr (W::QTERMS == 2) q[1][s] = __builtin_convertvector(v - __builtin_convertvector(q[0][s], f32x8), h8);
             }
-            fq = ldexpf(a.scale * kLog2e / kInt8Unit, -e);
-            if (top >= kInfBits) fq = __uint_as_float(0x7fc00000u);
+            // (positive, so that minus infinity stays that)
+            fq = fmaxf(ldexpf(a.scale * kLog2e / kInt8Unit, -e), 0x1p-126f);
+            undefined = top >= kInfBits;
         }
 
         // the tiles' way into LDS: 16 bytes of a key and of a value a thread and load
@@ -884,8 +886,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float mn = fmaxf(m, top), m0 = mn == kMinusInf ? 0.f : mn;
             if (__any(mn > m || En > E)) {
-                // (a row that has seen nothing holds zeros, whatever its query)
-                const float f = m == kMinusInf ? 0.f : ldexpf(exp2_fast((m - m0) * fq), E - En);
+                const float f = ldexpf(exp2_fast((m - m0) * fq), E - En);
                 l *= f;
 #pragma unroll
                 for (int t = 0; t < DT; ++t) o[t] *= f;
@@ -903,11 +904,10 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float x = s[t][4 * g + i];
-                            // (of a key that is not seen nothing counts: its scale and the query's may be NaN)
-                            const bool there = whole.value || x != kMinusInf;
-                            const float p = there ? exp2_fast(x * fq - lift) : 0.f;
+                            const float p = exp2_fast(x * fq - lift);
                             l += p;
-                            s[t][4 * g + i] = there ? p * vs[i] : 0.f;
+                            // (the scale of an entry that is not seen may be a NaN)
+                            s[t][4 * g + i] = p * (whole.value || x != kMinusInf ? vs[i] : 0.f);
                             least = fminf(least, s[t][4 * g + i]);
                         }
                     }
@@ -986,6 +986,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
             }
         }
         l += __shfl_xor(l, 32, 64);
+        if (undefined && l != 0.f) l = __uint_as_float(0x7fc00000u);  // (it saw a key)
         if (live && walk.whole) {
             const float f = l == 0.f ? 0.f : 512.f / l;
             const int hq = h * G + row - tok * G;
