@@ -11,7 +11,8 @@
 // fp16 MFMA with float32 sums.  int8 values are exact in fp16.  A query row is
 // scaled by a power of two that puts its largest value in [2^14, 2^15), so
 // float16 and bfloat16 queries are exact too (values 2^-28 of the largest and
-// less lose bits); a float32 query is the sum of two fp16 terms.  The weights
+// less lose bits); a float32 query is the sum of two fp16 terms.  A query with an
+// infinity or a NaN gives NaN where it sees a key, and no other row.  The weights
 // w_ij are scaled by 2^(14 - E), E the exponent of the largest vs that the row
 // has seen so far, and rounded to fp16 (float16 and float32: two terms; Weights below).
 //
@@ -669,10 +670,11 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
 // lie in LDS as they came and are read transposed.
 //
 // The softmax's arithmetic and the products bound it, one after the other more
-// than side by side: of the cycles the vector unit works 57 %, the matrix unit
-// 36 % and LDS 37 %.  2048 tokens at 32,768, 32 query heads on 8 of 128 in
-// bfloat16 take 1.29 ms, 823 TFLOP/s (float16 17 % more, whose weights are two
-// terms).  32 rows a wave rather than
+// than side by side: of the cycles the vector unit works 58 %, the matrix unit
+// 37 % and LDS 38 %.  2048 tokens at 32,768, 32 query heads on 8 of 128 in
+// bfloat16 take 1.29 ms, 823 TFLOP/s (float16, whose weights are two terms, 28 %
+// more; float32, whose queries are too, 57 %).  Scores ten times as far apart, so
+// that most tiles hold small weights, take 2.24 ms.  32 rows a wave rather than
 // 16 halve the reads of keys and values (16 rows: 1.63 ms); eight waves share a
 // tile because each then converts an eighth of it (two workgroups of four
 // waves a CU: 1.54 ms).
@@ -1086,7 +1088,9 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Par
 
 // Rows a workgroup takes.  Up to two tiles of 16 go to the kernel for few rows
 // (8 tokens of 4 heads a unit, 8 sequences of 8192: 61 us against 79 in tiles of
-// 64); the tiles grow with the rows a unit has.
+// 64); the tiles grow with the rows that the longest chunk has.  (A sequence of one
+// token beside a chunk takes a whole such tile: 512 tokens and 31 single ones over
+// 8192 take 407 us in one call, 125 and 112 in two.)
 int tile_rows(const AttnArgs& a) {
     const int64_t rows = (int64_t)a.max_chunk * (a.q_heads / a.c.kv_heads);
     if (rows <= 32) return 16;
@@ -1097,8 +1101,10 @@ int tile_rows(const AttnArgs& a) {
 
 // As many shares as the chip holds workgroups at a time.  Short units are not
 // worth cutting, as a join is a launch of its own: seven float32 tokens of 3
-// heads a unit over 700 tokens take 14 us whole and 20 us cut; 40 tokens over
-// 600 in the tile kernel 29 us cut and 42 whole.
+// heads a unit over 700 tokens take 14 us whole and 20 us cut; one token of one
+// head over 300 keys 12 and 17, over 1000 (eight blocks in one workgroup) 16.0 and
+// 16.8; 4 tokens of 8 heads over 1000 16.1 and 15.9, 32 of them 20 and 29; 40
+// tokens over 600 in the tile kernel 29 us cut and 42 whole.
 Shares choose_shares(const AttnArgs& a) {
     const int tile = tile_rows(a), G = a.q_heads / a.c.kv_heads;
     int64_t range = a.max_context;

@@ -5,7 +5,7 @@
 // take a row, eight values each, so a wave holds 64 / LANES rows and a row's
 // maximum is a few lane exchanges.  Both directions move each value once, and
 // memory bounds them: 16,000 tokens x 8 heads of 128 written from float16 in
-// 32 us (3.1 TB/s: a launch of some 10 us at the front and end of its loads),
+// 29 us (3.4 TB/s: a launch of some 10 us at the front and end of its loads),
 // 60,000 read back in 75 us (4.9 TB/s); 32 tokens 4 us either way, the launch
 // and the trips slot -> value -> entry.
 #include "token_types.h"

@@ -57,7 +57,7 @@ __device__ inline void by_dtype(int dtype, F&& f) {
 // their sums in LDS.  The weights, each read once, bound it: they go straight
 // into registers, as no wave shares them, and 16 channels a workgroup with
 // eight waves along the reduction put 512 workgroups on 8192 channels.  A token
-// times 4096 -> 8192 8.4 us (4.0 TB/s, a launch's 3 us included).
+// times 4096 -> 8192 7.7 us (4.4 TB/s, a launch's 3 us included).
 constexpr int kRowWaves = 8;
 template <int FM, int U>
 __global__ __launch_bounds__(kRowWaves * 64) void matmul_rows(MatmulArgs a) {
@@ -358,7 +358,8 @@ struct Cost {
     float step[2];     // us a step of 128 with one workgroup a CU, with all
 };
 // (256 x 256: 2.3 us a step is 1.87 POP/s; 8192^3 at the same clock 587 us against 648 in tiles of
-// 128 x 128; 1003 x 2049 -> 1001 11.2 us in 64 x 64 against 23.8 in 128 x 128;
+// 128 x 128; 1003 x 2049 -> 1001 12.2 us in 64 x 64 and 12.5 in 32 x 128, which the
+// costs prefer by half a microsecond, against 17.4 in 64 x 128 and 24.7 in 128 x 128;
 // 32 x 16,384 -> 4096 17.6 us in 32 x 128 against 18.3 in 64 x 64;
 // 96 x 16,384 -> 4096 24.5 us in 64 x 128 and four splits, 68.9 by matmul_rows)
 constexpr Cost kCosts[] = {{k256x256, 256, 256, 1, {2.3f, 2.3f}}, {k128x128, 128, 128, 2, {0.9f, 1.27f}},
