@@ -212,7 +212,6 @@ def prepare(case, seed):
             starts.append(starts[-1] + len(k))
         st.update(bases=ints(bases), keep=ints([i for k in keep for i in k]), starts=ints(starts), most=max(len(k) for k in keep))
     if kind in ("copy", "compact"):
-        st["caches"] = [tuple(c[layer] for c in st["all"]) for layer in range(case["layers"])]
         return st
     sizes, prefix, new, fresh = _lens(case)
     B, H, D = case["seqs"], case["kv_heads"], case["dim"]
@@ -274,10 +273,10 @@ def _own(st):
                                      layout=st["layout"], amplitude=st["amplitude"])
         return (q, *neo.kv_read_int8(st["cache"], st["slots"], TYPES[st["out"]]))
     if st["kind"] == "copy":
-        neo.kv_copy_pages(st["caches"], st["src"], st["dst"], entries=st["entries"])
+        neo.kv_copy_pages(st["all"], st["src"], st["dst"], entries=st["entries"])
         return st["all"]
     if st["kind"] == "compact":
-        neo.kv_compact(st["caches"], st["table"], st["bases"], st["keep"], st["starts"], st["most"])
+        neo.kv_compact(st["all"], st["table"], st["bases"], st["keep"], st["starts"], st["most"])
         return st["all"]
     return neo.attention_shared_int8(st["cache"], st["q"], st["table"], st["contexts"], st["starts"], st["group_starts"],
                                      st["prefix_lens"], st["max_chunk"], st["max_group"], st["max_context"], st["max_own"],
