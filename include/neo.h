@@ -682,7 +682,7 @@ const char* neo_last_error(void);
  * on the device: the same call gives the same bits.
  *
  * The workspace of the stream: calls that split their work (neo_matmul_int8,
- * neo_attention_paged_int8, and neo_conv2d_nchwxc, neo_conv2d_blocked and
+ * neo_attention_paged_int8, neo_attention_shared_int8, and neo_conv2d_nchwxc, neo_conv2d_blocked and
  * neo_conv2d_winograd above) keep parts in one buffer per (device, stream),
  * which the library owns and grows outside stream capture.  A call under
  * capture leaves the buffer's address in the graph, so that buffer is kept
@@ -813,6 +813,120 @@ int neo_attention_paged_int8(const neo_kv_cache* cache, const void* q, int64_t q
                              int max_chunk, int max_context, float scale, int window, void* out,
                              int64_t out_token_stride, int64_t out_head_stride,
                              neo_stream_t stream);
+
+/*
+ * Rotary positions.  Pair i (0 <= i < rot_dim / 2) of a head's first rot_dim
+ * values is (x[i], x[i + rot_dim / 2]) in the layout HALF, (x[2 i], x[2 i + 1])
+ * in INTERLEAVED; at position p it becomes
+ *   amplitude * (a cos t - b sin t, b cos t + a sin t),  t = p * freqs[i]
+ * the product and the angle in 64 bits (right for |t| up to 2^45), sine and
+ * cosine rounded to float32, the rest in float32, rounded once to `dtype`.
+ * Values from rot_dim on stay as they are.
+ */
+enum neo_rotary_layout { NEO_ROTARY_HALF = 0, NEO_ROTARY_INTERLEAVED = 1 };
+/*
+ * neo_rotary_frequencies: freqs (host, [rot_dim / 2]) of f_i = base^(-2 i / rot_dim),
+ * scaled for contexts longer than the first by `factor`:
+ *   NONE    as they are
+ *   LINEAR  f_i / factor
+ *   BASE    base * factor^(rot_dim / (rot_dim - 2)) in place of base (the lowest
+ *           frequency divided by factor, the highest as it is; rot_dim 2 as NONE)
+ *   TURNS   by the turns that a pair makes in `context` tokens, r = context f_i / (2 pi):
+ *           f_i from r = high on, f_i / factor up to r = low, between them
+ *           f_i (w + (1 - w) / factor), w = (r - low) / (high - low)
+ * Host only, synchronous.  rot_dim even and positive, base and factor finite and >= 1,
+ * for TURNS context > 0 and 0 <= low < high, finite (NEO_ERR_INVALID_ARG).
+ */
+enum neo_rotary_scaling {
+    NEO_ROTARY_NONE = 0,
+    NEO_ROTARY_LINEAR = 1,
+    NEO_ROTARY_BASE = 2,
+    NEO_ROTARY_TURNS = 3
+};
+int neo_rotary_frequencies(int rot_dim, double base, int scaling, double factor, double context,
+                           double low, double high, double* freqs);
+
+/*
+ * neo_rotary: x and y device [tokens][heads][head_dim] of `dtype`, strides per
+ *   token and head; positions device int64 [tokens], freqs device float64
+ *   [rot_dim / 2].  y may be x itself (same strides); they must not overlap
+ *   otherwise.  rot_dim even, 2 .. head_dim; any head_dim up to 65,536.
+ * neo_rotary_kv_write_int8: the same for the queries (q to q_out; q_out may be q),
+ *   and the keys, turned in float32 and not rounded between, and values quantized
+ *   into the entries slots[t] as neo_kv_write_int8 does.  Tokens whose slot lies
+ *   outside the cache have their queries turned all the same.
+ * amplitude finite.
+ */
+int neo_rotary(const void* x, int64_t x_token_stride, int64_t x_head_stride, int tokens, int heads,
+               int head_dim, int rot_dim, int layout, int dtype, const int64_t* positions,
+               const double* freqs, float amplitude, void* y, int64_t y_token_stride,
+               int64_t y_head_stride, neo_stream_t stream);
+int neo_rotary_kv_write_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride,
+                             int64_t q_head_stride, int q_heads, const void* k,
+                             int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                             int64_t v_token_stride, int64_t v_head_stride, int tokens, int rot_dim,
+                             int layout, int dtype, const int64_t* positions, const double* freqs,
+                             float amplitude, const int64_t* slots, void* q_out,
+                             int64_t out_token_stride, int64_t out_head_stride, neo_stream_t stream);
+
+/*
+ * Pages of the cache in all layers at once.  `cache` is the first of `layers`
+ * caches of one shape that lie layer_stride entries apart (keys and values
+ * layer_stride * head_dim bytes, scales layer_stride floats): at least
+ * pages * kv_heads * page_size, ignored for one layer.  Bytes and scales move as
+ * they are.
+ * neo_kv_copy_pages: page dst[i] becomes what page src[i] is (a sequence forks,
+ *   or pages move together); with `entries` its first entries[i] tokens of every
+ *   head only (clamped to 0 .. page_size), the others left as they were.  src, dst
+ *   and entries device int32 [pairs].  A pair with a page outside [0, pages), or
+ *   with src = dst, is skipped.  No page may be the destination of two pairs, or
+ *   the source of one and the destination of another: which of their values it
+ *   then holds is not said.  One page may be the source of many.
+ * neo_kv_compact: of sequence b, token bases[b] + i becomes what token
+ *   keep[keep_starts[b] + i] was before the call (tokens are dropped, and those
+ *   that are kept close up).  keep device int32 [kept], keep_starts device int32
+ *   [seqs + 1], ascending from 0 to kept, bases device int32 [seqs]; page_table as
+ *   in neo_attention_paged_int8.  An entry keep < bases[b] + i, or a token past
+ *   the table's end or in a page outside the cache, moves nothing; entries need not
+ *   ascend, and may repeat.  max_keep (host) bounds a sequence's entries: those past
+ *   it move nothing.  A page that a token moves to must belong to one sequence.
+ */
+int neo_kv_copy_pages(const neo_kv_cache* cache, int layers, int64_t layer_stride, const int32_t* src,
+                      const int32_t* dst, const int32_t* entries, int pairs, neo_stream_t stream);
+int neo_kv_compact(const neo_kv_cache* cache, int layers, int64_t layer_stride,
+                   const int32_t* page_table, int64_t table_stride, const int32_t* bases,
+                   const int32_t* keep, const int32_t* keep_starts, int kept, int seqs, int max_keep,
+                   neo_stream_t stream);
+
+/*
+ * neo_attention_paged_int8 for sequences of which groups share their first
+ * tokens: the sequences group_starts[g] .. group_starts[g + 1] - 1 hold the same
+ * prefix_lens[g] first tokens, which are read once for all queries of the group,
+ * through the page table of its first sequence.  Its values differ from that call's
+ * by the order of their sums only.
+ *   group_starts  device int32 [groups + 1], ascending from 0 to seqs; every
+ *                 sequence is in one group (of one sequence, maybe, or with a
+ *                 prefix of 0)
+ *   prefix_lens   device int32 [groups]
+ *   max_group     host: how many new tokens a group has at most; the sequences
+ *                 of one that has more read the prefix each
+ *   max_own       host: how many cached tokens a sequence has behind its prefix at
+ *                 most.  The work is laid out for it; where one has more, its
+ *                 tokens take longer and are the same
+ * and the rest as there; every group's prefix has a page in its first
+ * sequence's table.  A window hides shared tokens too, but they are read: for
+ * windows much shorter than the prefix the other call reads less.  The parts of
+ * the shared tokens are kept in the workspace of the stream,
+ * tokens * q_heads * (head_dim + 2) floats beside those of the shares.
+ */
+int neo_attention_shared_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride,
+                              int64_t q_head_stride, int tokens, int q_heads, int dtype,
+                              const int32_t* page_table, int64_t table_stride,
+                              const int32_t* context_lens, const int32_t* q_starts, int seqs,
+                              const int32_t* group_starts, const int32_t* prefix_lens, int groups,
+                              int max_chunk, int max_group, int max_context, int max_own, float scale,
+                              int window, void* out, int64_t out_token_stride,
+                              int64_t out_head_stride, neo_stream_t stream);
 
 #ifdef __cplusplus
 }

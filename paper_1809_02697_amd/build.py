@@ -16,7 +16,8 @@ OUT = os.path.join(HERE, "libneo.so")
 ARCH = "gfx950"
 SOURCES = ["conv.hip", "conv_xy.hip", "conv_h2.hip", "conv_h2_raw.hip", "conv_h2_xy.hip", "conv_h2_raw_xy.hip", "conv_group.hip", "conv_pair.hip", "layout.hip", "pool.hip", "dense.hip", "api.cpp", "plan.cpp", "tune.cpp",
            "search.cpp", "noalloc.hip", "conv_pool.hip", "conv_stream.hip", "winograd.hip", "conv_int8.hip",
-           "token_api.cpp", "tokens.hip", "matmul_int8.hip", "kv_cache.hip", "attention.hip"]
+           "token_api.cpp", "tokens.hip", "matmul_int8.hip", "kv_cache.hip", "attention.hip",
+           "attention_shared.hip", "attention_own.hip", "rotary.hip", "kv_pages.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Wno-unused-command-line-argument"]

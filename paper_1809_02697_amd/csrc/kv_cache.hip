@@ -13,15 +13,6 @@
 namespace neo {
 namespace {
 
-// Entry `slot` of head h, in entries from the cache's start; -1 outside.
-__device__ inline int64_t entry_of(const neo_kv_cache& c, int64_t slot, int h) {
-    const int64_t total = (int64_t)c.pages * c.page_size;
-    if (slot < 0 || slot >= total) return -1;
-    // (a 64-bit division takes some hundred instructions)
-    const int64_t page = total <= 0x7fffffff ? (int64_t)((uint32_t)slot / (uint32_t)c.page_size) : slot / c.page_size;
-    return (page * c.kv_heads + h) * c.page_size + (slot - page * c.page_size);
-}
-
 // A group takes a token's key and value of a head: one lookup of the slot, and
 // two rows' loads under way at once (16,000 tokens x 8 heads of 128 in float16
 // 32 us, 41 with a row a group and a division a value).

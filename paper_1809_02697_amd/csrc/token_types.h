@@ -129,6 +129,15 @@ __device__ inline float lanes_sum(float v) {
     return v;
 }
 
+// Entry `slot` of head h, in entries from the cache's start; -1 outside.
+__device__ inline int64_t entry_of(const neo_kv_cache& c, int64_t slot, int h) {
+    const int64_t total = (int64_t)c.pages * c.page_size;
+    if (slot < 0 || slot >= total) return -1;
+    // (a 64-bit division takes some hundred instructions)
+    const int64_t page = total <= 0x7fffffff ? (int64_t)((uint32_t)slot / (uint32_t)c.page_size) : slot / c.page_size;
+    return (page * c.kv_heads + h) * c.page_size + (slot - page * c.page_size);
+}
+
 // ---- launchers: arguments are valid (token_api.cpp checks them) ------------------------
 
 struct RowsArgs {
@@ -177,8 +186,51 @@ struct AttnArgs {
     const int32_t *table, *contexts, *starts;
     int tokens, q_heads, seqs, max_chunk, max_context, window;
     float scale;
+    // Attention over a shared prefix.  In the launch over the shared tokens `seqs`
+    // counts the groups and `max_chunk` bounds a group's tokens.
+    const int32_t *group_starts = nullptr, *prefix_lens = nullptr;
+    int all_seqs = 0, max_own = 0;
+    float* part_o = nullptr;    // [tokens][q_heads][head_dim], of the shared tokens
+    float2* part_ml = nullptr;  // [tokens][q_heads]
+    int32_t* shared = nullptr;  // [sequences]: tokens that its group shares
 };
-size_t attention_workspace(int dtype, const AttnArgs& a);
+size_t attention_workspace(const AttnArgs& a);
 hipError_t launch_attention(int dtype, const AttnArgs& a, float* ws, hipStream_t st);
+// Floats of the parts, and the launches: over the shared tokens, then over the others.
+size_t attention_shared_floats(const AttnArgs& a);
+size_t attention_own_floats(const AttnArgs& a);
+hipError_t launch_attention_shared(int dtype, const AttnArgs& a, float* ws, hipStream_t st);
+hipError_t launch_attention_own(int dtype, const AttnArgs& a, float* ws, hipStream_t st);
+
+struct RotaryArgs {
+    const void* x;  // rows that are turned
+    void* y;
+    int64_t xts, xhs, yts, yhs;
+    int heads;
+    const int64_t* positions;
+    const double* freqs;
+    float amplitude;
+    int tokens, dim, rot, layout;
+    KvArgs kv;  // with the cache's write: keys (turned too) and values
+};
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, bool write, hipStream_t st);
+
+struct CopyArgs {
+    neo_kv_cache c;  // of the first layer
+    int64_t layer_stride;
+    int layers;
+    const int32_t *src, *dst, *entries;
+    int pairs;
+};
+hipError_t launch_kv_copy(const CopyArgs& a, hipStream_t st);
+struct CompactArgs {
+    neo_kv_cache c;
+    int64_t layer_stride;
+    int layers;
+    const int32_t *table, *bases, *keep, *starts;
+    int64_t table_stride;
+    int kept, seqs, max_keep;
+};
+hipError_t launch_kv_compact(const CompactArgs& a, hipStream_t st);
 
 }  // namespace neo

@@ -23,6 +23,8 @@ OK = 0
 ERR_NAMES = {-1: "NEO_ERR_INVALID_ARG", -2: "NEO_ERR_SHAPE", -3: "NEO_ERR_ALIGN",
              -4: "NEO_ERR_UNSUPPORTED", -5: "NEO_ERR_HIP", -6: "NEO_ERR_OOM", -7: "NEO_ERR_STATE"}
 ACT = {"none": 0, "relu": 1}
+ROTARY_LAYOUT = {"half": 0, "interleaved": 1}
+ROTARY_SCALING = {"none": 0, "linear": 1, "base": 2, "turns": 3}
 OPS = {"input": 0, "conv": 1, "maxpool": 2, "avgpool": 3, "gap": 4, "concat": 5, "flatten": 6,
        "dense": 7, "output": 8}
 PLAN_HOST_ONLY = 1
@@ -89,7 +91,7 @@ def lib():
     import torch  # noqa: F401
     L = ctypes.CDLL(LIB_PATH)
     P, I, F, S = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
-    L64, KV = ctypes.c_int64, ctypes.POINTER(KvCacheStruct)
+    L64, KV, D = ctypes.c_int64, ctypes.POINTER(KvCacheStruct), ctypes.c_double
     sig = {
         "neo_conv2d_blocked": [P, I, I, I, I, P, I, I, I, P, I, I, I, I,
                                ctypes.POINTER(Epilogue), P, I, I, P],
@@ -137,6 +139,12 @@ def lib():
         "neo_kv_read_int8": [KV, P, I, I, P, P, P],
         "neo_attention_paged_int8": [KV, P, L64, L64, I, I, I, P, L64, P, P, I, I, I, F, I, P, L64,
                                      L64, P],
+        "neo_rotary_frequencies": [I, D, I, D, D, D, D, P],
+        "neo_rotary": [P, L64, L64, I, I, I, I, I, I, P, P, F, P, L64, L64, P],
+        "neo_rotary_kv_write_int8": [KV, P, L64, L64, I, P, L64, L64, P, L64, L64, I, I, I, I, P, P, F, P, P, L64, L64, P],
+        "neo_kv_copy_pages": [KV, I, L64, P, P, P, I, P],
+        "neo_kv_compact": [KV, I, L64, P, L64, P, P, P, I, I, I, P],
+        "neo_attention_shared_int8": [KV, P, L64, L64, I, I, I, P, L64, P, P, I, P, P, I, I, I, I, I, F, I, P, L64, L64, P],
         "neo_tune_db_save": [ctypes.c_char_p],
         "neo_tune_db_load": [ctypes.c_char_p],
         "neo_tune_db_clear": [],
@@ -492,19 +500,26 @@ def dense_int8(xq, IN, w_rows, w_scale, OUT, x_scale, bias=None, act="none", out
 class KVCache(NamedTuple):
     """A paged int8 cache: k and v int8 [pages][kv_heads][page_size][head_dim],
     their scales float32 [pages][kv_heads][page_size].  Any tuple of the four
-    tensors in this order serves as well."""
+    tensors in this order serves as well.  The caches of all layers may be one,
+    with the layers in front (kv_cache with layers=); kv_layer gives one of them."""
     k: "torch.Tensor"
     v: "torch.Tensor"
     k_scale: "torch.Tensor"
     v_scale: "torch.Tensor"
 
 
-def kv_cache(pages, kv_heads, page_size, head_dim, device="cuda"):
-    """A new, zeroed cache."""
+def kv_cache(pages, kv_heads, page_size, head_dim, device="cuda", layers=None):
+    """A new, zeroed cache; with layers, those of so many layers as one."""
     import torch
-    q = [torch.zeros((pages, kv_heads, page_size, head_dim), device=device, dtype=torch.int8) for _ in range(2)]
-    s = [torch.zeros((pages, kv_heads, page_size), device=device, dtype=torch.float32) for _ in range(2)]
+    shape = (pages, kv_heads, page_size) if layers is None else (layers, pages, kv_heads, page_size)
+    q = [torch.zeros((*shape, head_dim), device=device, dtype=torch.int8) for _ in range(2)]
+    s = [torch.zeros(shape, device=device, dtype=torch.float32) for _ in range(2)]
     return KVCache(*q, *s)
+
+
+def kv_layer(cache, layer):
+    """One layer's cache of those of all layers (the same memory)."""
+    return KVCache(*(t[layer] for t in cache))
 
 
 # These calls are a few microseconds of GPU work for a token, so what the
@@ -514,12 +529,16 @@ def kv_cache(pages, kv_heads, page_size, head_dim, device="cuda"):
 _DTYPES = {}   # torch dtype -> enum neo_dtype, and the types by name; filled on first use
 
 
+def _fill_dtypes():
+    import torch
+    _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, "f32": torch.float32, "i8": torch.int8, "i32": torch.int32,
+                    "i64": torch.int64, "bf16": torch.bfloat16, "f64": torch.float64})
+
+
 def _dtype(t):
     code = _DTYPES.get(t)
     if code is None:
-        import torch
-        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, "f32": torch.float32, "i8": torch.int8,
-                        "i32": torch.int32, "i64": torch.int64, "bf16": torch.bfloat16})
+        _fill_dtypes()
         code = _DTYPES.get(t)
         if code is None:
             raise TypeError(f"{t} is not float32, float16 or bfloat16")
@@ -688,6 +707,29 @@ def _heads(t, heads, dim, name):
     return t.data_ptr(), s[0], s[1]
 
 
+def _heads_like(t, x, name):
+    """_heads of an output given by the caller for an input x."""
+    if t.dtype != x.dtype or t.shape != x.shape:
+        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, not {tuple(x.shape)} of {x.dtype}")
+    return _heads(t, t.shape[1], t.shape[2], name)
+
+
+def _layers(cache):
+    """A cache of one layer or of several as (C struct of the first, layers, entries from one to the next)."""
+    if not _DTYPES:
+        _fill_dtypes()
+    k, v, ks, vs = cache
+    if k.dim() == 4:
+        return _cache(cache), 1, 0
+    shape = k.shape
+    if len(shape) != 5 or v.shape != shape or ks.shape != shape[:4] or vs.shape != shape[:4]:
+        raise ValueError("the caches of several layers are k and v [layers][pages][kv_heads][page_size][head_dim] and their scales "
+                         "[layers][pages][kv_heads][page_size]")
+    i8, f32 = _DTYPES["i8"], _DTYPES["f32"]
+    c = KvCacheStruct(_vec(k, 0, i8, "k"), _vec(v, 0, i8, "v"), _vec(ks, 0, f32, "k_scale"), _vec(vs, 0, f32, "v_scale"), *shape[1:])
+    return c, shape[0], shape[1] * shape[2] * shape[3]
+
+
 def kv_write_int8(cache, k, v, slots, stream=None):
     """Quantizes k and v [tokens][kv_heads][head_dim] into the cache entries
     slots [tokens] (int64: page * page_size + entry; a slot outside the cache,
@@ -749,6 +791,122 @@ def attention_paged_int8(cache, q, page_table, context_lens, q_starts, max_chunk
                                           _vec(context_lens, B, i32, "context_lens"), _vec(q_starts, B + 1, i32, "q_starts"), B,
                                           max_chunk, max_context, D ** -0.5 if scale is None else scale, window, op, ot, oh,
                                           _stream(stream)))
+    return out
+
+
+def rotary_frequencies(rot_dim, base=10000.0, scaling="none", factor=1.0, context=0, low=1.0, high=32.0, device="cuda"):
+    """The frequencies of rotary positions, float64 [rot_dim / 2] on the device: base^(-2 i / rot_dim)
+    radians a position, as they are ("none") or scaled for contexts `factor` times as long: all divided
+    ("linear"), the base raised so that the lowest is ("base"), or by the turns that a pair makes in
+    `context` tokens, divided up to `low`, kept from `high` on, blended between ("turns")."""
+    import torch
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError(f"rot_dim must be even and positive, is {rot_dim}")
+    f = np.empty(rot_dim // 2)
+    _check(lib().neo_rotary_frequencies(rot_dim, base, ROTARY_SCALING[scaling], factor, context, low, high, _hp(f)))
+    return torch.from_numpy(f).to(device)
+
+
+def rotary(x, positions, freqs, layout="half", amplitude=1.0, out=None, stream=None):
+    """x [tokens][heads][dim] with each head's first 2 * len(freqs) values turned by
+    positions [tokens] (int64) times freqs (float64): pairs (i, i + half) in the layout
+    "half", neighbours in "interleaved", times amplitude.  out=x works in place."""
+    t = x.dtype
+    code = _dtype(t)
+    if x.dim() != 3:
+        raise ValueError(f"x must be [tokens][heads][dim], is {tuple(x.shape)}")
+    T, H, D = x.shape
+    xp, xt, xh = _heads(x, H, D, "x")
+    if out is None:
+        out = x.new_empty((T, H, D)) if stream is None else _new(x, (T, H, D), t, stream)
+        op, ot, oh = out.data_ptr(), H * D, D
+    else:
+        op, ot, oh = _heads_like(out, x, "out")
+    rot = 2 * freqs.numel()
+    _check(lib().neo_rotary(xp, xt, xh, T, H, D, rot, ROTARY_LAYOUT[layout], code, _vec(positions, T, _DTYPES["i64"], "positions"),
+                            _vec(freqs, 0, _DTYPES["f64"], "freqs"), amplitude, op, ot, oh, _stream(stream)))
+    return out
+
+
+def rotary_kv_write_int8(cache, q, k, v, slots, positions, freqs, layout="half", amplitude=1.0, q_out=None, stream=None):
+    """rotary of q [tokens][q_heads][head_dim], and of k [tokens][kv_heads][head_dim] on its way with v
+    into the cache entries slots (kv_write_int8).  Returns the turned queries (q_out, which may be q)."""
+    t = q.dtype
+    code = _dtype(t)
+    c = _cache(cache)
+    if k.dtype != t or v.dtype != t or k.shape != v.shape or k.shape[0] != q.shape[0]:
+        raise ValueError("q, k and v differ in type or tokens, or k and v in shape")
+    D = c.head_dim
+    qp, qt, qh = _heads(q, None, D, "q")
+    T, Hq, _ = q.shape
+    if q_out is None:
+        q_out = q.new_empty((T, Hq, D)) if stream is None else _new(q, (T, Hq, D), t, stream)
+        op, ot, oh = q_out.data_ptr(), Hq * D, D
+    else:
+        op, ot, oh = _heads_like(q_out, q, "q_out")
+    i64 = _DTYPES["i64"]
+    _check(lib().neo_rotary_kv_write_int8(ctypes.byref(c), qp, qt, qh, Hq, *_heads(k, c.kv_heads, D, "k"),
+                                          *_heads(v, c.kv_heads, D, "v"), T, 2 * freqs.numel(), ROTARY_LAYOUT[layout], code,
+                                          _vec(positions, T, i64, "positions"), _vec(freqs, 0, _DTYPES["f64"], "freqs"), amplitude,
+                                          _vec(slots, T, i64, "slots"), op, ot, oh, _stream(stream)))
+    return q_out
+
+
+def kv_copy_pages(cache, src, dst, entries=None, stream=None):
+    """Pages dst [pairs] become what the pages src [pairs] are (int32), in every layer of the
+    cache; with entries (int32 [pairs]) their first so many tokens only.  No page may be the
+    destination of two pairs, or the source of one and the destination of another."""
+    c, layers, stride = _layers(cache)
+    i32 = _DTYPES["i32"]
+    n = src.numel()
+    if dst.numel() != n or (entries is not None and entries.numel() != n):
+        raise ValueError("src, dst and entries differ in length")
+    _check(lib().neo_kv_copy_pages(ctypes.byref(c), layers, stride, _vec(src, n, i32, "src"), _vec(dst, n, i32, "dst"),
+                                   _vec(entries, n, i32, "entries"), n, _stream(stream)))
+
+
+def kv_compact(cache, page_table, bases, keep, keep_starts, max_keep, stream=None):
+    """Tokens close up in every layer of the cache: token bases[b] + i of sequence b becomes what
+    its token keep[keep_starts[b] + i] >= bases[b] + i was.  page_table int32 [seqs][pages of a
+    sequence], bases int32 [seqs], keep int32, keep_starts int32 [seqs + 1]; max_keep bounds a
+    sequence's entries.  A page that a token moves to must belong to one sequence."""
+    c, layers, stride = _layers(cache)
+    i32 = _DTYPES["i32"]
+    B, most = _shape2(page_table, "page_table")
+    tp, ts = _rows(page_table, B, most, i32, "page_table")
+    n = keep.numel()
+    _check(lib().neo_kv_compact(ctypes.byref(c), layers, stride, tp, ts, _vec(bases, B, i32, "bases"), _vec(keep, n, i32, "keep"),
+                                _vec(keep_starts, B + 1, i32, "keep_starts"), n, B, max_keep, _stream(stream)))
+
+
+def attention_shared_int8(cache, q, page_table, context_lens, q_starts, group_starts, prefix_lens, max_chunk, max_group,
+                          max_context, max_own=None, scale=None, window=0, out=None, stream=None):
+    """attention_paged_int8 for sequences of which groups share their first tokens, which are then read
+    once a group: sequences group_starts[g] .. group_starts[g + 1] - 1 (int32 [groups + 1]) share the
+    first prefix_lens[g] (int32 [groups]), found in the first one's page table.  max_group: a group's
+    new tokens at most (one with more is not taken together); max_own: a sequence's cached tokens behind
+    the shared ones at most (max_context unless given), which the work is laid out for."""
+    t = q.dtype
+    code = _dtype(t)
+    i32 = _DTYPES["i32"]
+    c = _cache(cache)
+    qp, qt, qh = _heads(q, None, c.head_dim, "q")
+    T, Hq, D = q.shape
+    B, most = _shape2(page_table, "page_table")
+    tp, ts = _rows(page_table, B, most, i32, "page_table")
+    groups = prefix_lens.numel()
+    if max_context > most * c.page_size:
+        raise ValueError(f"max_context {max_context} exceeds the {most} pages a sequence has")
+    if out is None:
+        out = q.new_empty((T, Hq, D)) if stream is None else _new(q, (T, Hq, D), t, stream)
+        op, ot, oh = out.data_ptr(), Hq * D, D
+    else:
+        op, ot, oh = _heads_like(out, q, "out")
+    _check(lib().neo_attention_shared_int8(ctypes.byref(c), qp, qt, qh, T, Hq, code, tp, ts,
+                                           _vec(context_lens, B, i32, "context_lens"), _vec(q_starts, B + 1, i32, "q_starts"), B,
+                                           _vec(group_starts, groups + 1, i32, "group_starts"), _vec(prefix_lens, groups, i32, "prefix_lens"),
+                                           groups, max_chunk, max_group, max_context, max_context if max_own is None else max_own,
+                                           D ** -0.5 if scale is None else scale, window, op, ot, oh, _stream(stream)))
     return out
 
 

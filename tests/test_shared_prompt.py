@@ -1,0 +1,789 @@
+"""The operators of requests that share a prompt (neo_rotary_frequencies,
+neo_rotary, neo_rotary_kv_write_int8, neo_kv_copy_pages, neo_kv_compact,
+neo_attention_shared_int8): refusals on the host; on the GPU against plain
+implementations in 64 bits.
+
+Tolerances, derived from the formats (u = 2^-24):
+
+* rotation: cosine and sine are within 2^-31 of the angle's, rounded to float32
+  and times the amplitude A (2 u), each product and the difference within u, so
+  a value is within 5 u (|a c| + |b s|) + 2^-30 A (|a| + |b|) of a c - b s, plus
+  the output's rounding.  The angle is the float64 product of position and
+  frequency on both sides;
+* a key on its way into the cache: |a c| + |b s| is at most twice the larger of
+  the pair's turned values, so at most twice the row's largest, and a value
+  is within (10 u + 2^-29) of it before it is quantized: half a step, and that;
+* pages: bytes and scales move as they are, bit for bit;
+* attention: the bound of neo_attention_paged_int8 (test_token_ops), and 16 u
+  for the join with the shared part: two exponentials' factors, two products and
+  a sum for the values and for the weights' sum, and the quotient.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from paper_1809_02697_amd import neo
+
+from gpu_util import torch_cuda
+from test_token_ops import (BAD_CACHES, BF16, F16, F32, FAKE, MIS, ODD, TINY, TYPES, U, _attention64, _attention_bound, _np, _rand,
+                            _step_check, _struct)
+
+gpu = pytest.mark.gpu
+u = U["float32"]
+
+
+@pytest.fixture(scope="module")
+def torch():
+    t = torch_cuda()
+    neo.lib()
+    return t
+
+
+def cuda(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+# ---- host ------------------------------------------------------------------------------
+
+def test_frequencies():
+    f = lambda *a, **k: neo.rotary_frequencies(*a, device="cpu", **k).numpy()  # noqa: E731
+    i = np.arange(64)
+    plain = 10000.0 ** (-i / 64)
+    np.testing.assert_allclose(f(128), plain, rtol=1e-14)
+    np.testing.assert_allclose(f(128, scaling="linear", factor=4.0), plain / 4, rtol=1e-14)
+    raised = f(128, scaling="base", factor=8.0)
+    assert raised[0] == 1 and abs(raised[-1] * 8 / plain[-1] - 1) < 1e-12
+    np.testing.assert_allclose(raised, (10000 * 8 ** (128 / 126)) ** (-i / 64), rtol=1e-13)
+    turns = f(128, scaling="turns", factor=16.0, context=4096, low=1.0, high=32.0)
+    r = 4096 * plain / (2 * math.pi)
+    assert (turns[r >= 32] == f(128)[r >= 32]).all()
+    np.testing.assert_allclose(turns[r <= 1], plain[r <= 1] / 16, rtol=1e-14)
+    w = np.clip((r - 1) / 31, 0, 1)
+    np.testing.assert_allclose(turns, plain * (w + (1 - w) / 16), rtol=1e-13)
+    assert f(2, scaling="base", factor=8.0).tolist() == [1.0]
+    with pytest.raises(ValueError):
+        neo.rotary_frequencies(7, device="cpu")
+
+
+def test_frequencies_refusals():
+    out = (ctypes.c_double * 4)()
+
+    def call(rot=8, base=1e4, scaling=0, factor=2.0, context=100.0, low=1.0, high=4.0, freqs=out):
+        return neo.lib().neo_rotary_frequencies(rot, base, scaling, factor, context, low, high, freqs)
+    assert call() == 0
+    for bad in (dict(rot=0), dict(rot=-2), dict(rot=7), dict(base=0.5), dict(base=math.nan), dict(base=math.inf), dict(scaling=-1),
+                dict(scaling=4), dict(freqs=None), dict(scaling=1, factor=0.5), dict(scaling=2, factor=math.inf),
+                dict(scaling=3, factor=math.nan), dict(scaling=3, context=0.0), dict(scaling=3, low=-1.0), dict(scaling=3, low=4.0),
+                dict(scaling=3, high=math.inf), dict(scaling=3, context=math.nan)):
+        assert call(**bad) == -1 and "neo_rotary_frequencies" in neo.last_error(), bad
+    assert call(factor=0.0, context=0.0) == 0      # (not asked for without a scaling)
+
+
+OTHER = ctypes.c_void_p(1 << 24)
+ROTARY_BAD = [(dict(rot=0), -2), (dict(rot=3), -2), (dict(rot=66), -2), (dict(layout=2), -1), (dict(layout=-1), -1), (dict(dtype=3), -1),
+              (dict(amp=math.nan), -1), (dict(amp=math.inf), -1), (dict(T=-1), -1), (dict(H=0), -1), (dict(x=None), -1),
+              (dict(y=None), -1), (dict(pos=None), -1), (dict(freqs=None), -1), (dict(x=ODD), -3), (dict(y=ODD), -3),
+              (dict(pos=ctypes.c_void_p((1 << 20) + 4)), -3), (dict(freqs=ctypes.c_void_p((1 << 20) + 4)), -3), (dict(xt=-1), -1),
+              (dict(xh=-64), -1), (dict(yt=63), -2), (dict(yh=63), -2), (dict(yt=64, yh=64), -2), (dict(yt=100, yh=100), -2)]
+
+
+def test_rotary_refusals():
+    def call(x=FAKE, xt=256, xh=64, T=3, H=4, D=64, rot=64, layout=0, dtype=F16, pos=FAKE, freqs=FAKE, amp=1.0, y=OTHER, yt=256, yh=64):
+        return neo.lib().neo_rotary(x, xt, xh, T, H, D, rot, layout, dtype, pos, freqs, amp, y, yt, yh, None)
+    for over, code in ROTARY_BAD + [(dict(D=0), -1), (dict(D=65537, yh=65537, yt=1 << 20), -4), (dict(H=1 << 23), -4)]:
+        assert call(**over) == code and "neo_rotary" in neo.last_error(), over
+    assert call(y=FAKE, yt=512) == -2 and "in place" in neo.last_error()
+    assert call(y=FAKE, xh=0) == -2 and "in place" in neo.last_error()     # heads read from one place, written in place
+    assert call(T=0, x=None, y=None) == 0
+
+
+def test_rotary_write_refusals():
+    def call(c=None, x=FAKE, xt=256, xh=64, H=4, k=FAKE, kt=64, v=FAKE, vt=64, T=3, rot=64, layout=0, dtype=F16, pos=FAKE, freqs=FAKE,
+             amp=1.0, slots=FAKE, y=OTHER, yt=256, yh=64):
+        return neo.lib().neo_rotary_kv_write_int8(_struct() if c is None else c, x, xt, xh, H, k, kt, 64, v, vt, 64, T, rot, layout,
+                                                  dtype, pos, freqs, amp, slots, y, yt, yh, None)
+    for over, code in BAD_CACHES:
+        assert call(_struct(**over)) == code and "neo_rotary_kv_write_int8: cache" in neo.last_error(), over
+    for over, code in ROTARY_BAD:
+        assert call(**over) == code and "neo_rotary_kv_write_int8" in neo.last_error(), over
+    assert call(k=None) == -1 and call(v=None) == -1 and call(slots=None) == -1 and call(kt=-1) == -1 and call(vt=-1) == -1
+    assert call(k=ODD) == -3 and call(v=ODD) == -3 and call(slots=ctypes.c_void_p((1 << 20) + 4)) == -3
+    assert call(y=FAKE, yt=512) == -2
+    assert call(T=0, x=None, k=None, slots=None) == 0
+
+
+def test_page_refusals():
+    big = 4 * 2 * 16
+
+    def copy(c=None, layers=2, stride=big, src=FAKE, dst=FAKE, n=None, pairs=3):
+        return neo.lib().neo_kv_copy_pages(_struct() if c is None else c, layers, stride, src, dst, n, pairs, None)
+
+    def compact(c=None, layers=2, stride=big, table=FAKE, ts=8, bases=FAKE, keep=FAKE, starts=FAKE, kept=5, seqs=2, most=4):
+        return neo.lib().neo_kv_compact(_struct() if c is None else c, layers, stride, table, ts, bases, keep, starts, kept, seqs, most, None)
+    for call, name in ((copy, "neo_kv_copy_pages"), (compact, "neo_kv_compact")):
+        for over, code in BAD_CACHES:
+            assert call(_struct(**over)) == code and f"{name}: cache" in neo.last_error(), over
+        assert call(layers=-1) == -1 and call(stride=big - 1) == -2 and call(stride=-big) == -2 and call(stride=0) == -2
+        assert call(layers=1 << 17) == -4 and call(stride=1 << 39) == -4 and name in neo.last_error()
+        assert call(layers=0) == 0
+    for over in (dict(src=None), dict(dst=None), dict(pairs=-1)):
+        assert copy(**over) == -1, over
+    for over in (dict(src=ODD), dict(dst=ODD), dict(n=ODD)):
+        assert copy(**over) == -3, over
+    assert copy(pairs=0, src=None) == 0
+    for over in (dict(table=None), dict(bases=None), dict(keep=None), dict(starts=None), dict(kept=-1), dict(seqs=-1), dict(most=-1)):
+        assert compact(**over) == -1, over
+    for over in (dict(table=ODD), dict(bases=ODD), dict(keep=ODD), dict(starts=ODD)):
+        assert compact(**over) == -3, over
+    assert compact(ts=-1) == -2 and compact(ts=1 << 31) == -4
+    assert compact(kept=0, keep=None) == 0 and compact(seqs=0, table=None) == 0 and compact(most=0) == 0 and compact(ts=0) == 0
+
+
+def test_shared_attention_refusals():
+    def call(c=None, q=FAKE, qt=256, qh=64, T=3, Hq=4, dtype=F16, table=FAKE, ts=8, ctx=FAKE, st=FAKE, B=2, gs=FAKE, pl=FAKE, groups=1,
+             n=2, group=3, most=100, own=50, scale=0.125, window=0, out=FAKE, ot=256, oh=64):
+        return neo.lib().neo_attention_shared_int8(_struct() if c is None else c, q, qt, qh, T, Hq, dtype, table, ts, ctx, st, B, gs, pl,
+                                                   groups, n, group, most, own, scale, window, out, ot, oh, None)
+    for over, code in BAD_CACHES:
+        assert call(_struct(**over)) == code and "neo_attention_shared_int8: cache" in neo.last_error(), over
+    for name in ("q", "table", "ctx", "st", "out", "gs", "pl"):
+        assert call(**{name: None}) == -1, name
+        assert call(**{name: ODD}) == -3, name
+    for name in ("T", "B", "n", "most", "window", "groups", "group", "own"):
+        assert call(**{name: -1}) == -1, name
+    assert call(Hq=0) == -1 and call(dtype=5) == -1
+    assert call(Hq=3) == -2 and call(qt=-1) == -1 and call(oh=63) == -2 and call(ot=1) == -2
+    assert call(most=129) == -2 and call(groups=0) == -2 and call(groups=3) == -2
+    for s in (0.0, -1.0, math.nan, math.inf):
+        assert call(scale=s) == -1
+    assert call(T=1 << 29, n=1 << 29) == -4 and call(T=1 << 27, group=1 << 27) == -4
+    assert call(T=0, q=None) == 0 and call(B=0, q=None) == 0 and call(n=0, q=None) == 0
+
+
+# ---- rotation ----------------------------------------------------------------------------
+
+def _pairs(rot, layout):
+    i = np.arange(rot // 2)
+    return (i, i + rot // 2) if layout == "half" else (2 * i, 2 * i + 1)
+
+
+def _turned(x, pos, f, layout, amp):
+    """The turned rows [T][H][D] in 64 bits, and |a c| + |b s| and |a| + |b| of each value."""
+    x, rot = x.astype(np.float64), 2 * len(f)
+    a, b = _pairs(rot, layout)
+    t = pos.astype(np.float64)[:, None] * f
+    c, s = amp * np.cos(t)[:, None], amp * np.sin(t)[:, None]
+    y, big, sums = x.copy(), np.abs(x) * 0, np.abs(x) * 0
+    y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., b] * c + x[..., a] * s
+    big[..., a] = np.abs(x[..., a] * c) + np.abs(x[..., b] * s)
+    big[..., b] = np.abs(x[..., b] * c) + np.abs(x[..., a] * s)
+    sums[..., a] = sums[..., b] = np.abs(x[..., a]) + np.abs(x[..., b])
+    return y, big, sums
+
+
+def _turn_check(got, x, pos, f, layout, amp, dtype):
+    y, big, sums = _turned(x, pos, f, layout, amp)
+    bound = 5 * u * big + 2.0 ** -30 * abs(amp) * sums
+    bound += U[dtype] * (np.abs(y) + bound) * (big > 0) + TINY[dtype]
+    bound[..., 2 * len(f):] = 0
+    err = np.abs(got - y)
+    assert (err <= bound).all(), f"{(err > bound).sum()} of {err.size} beyond the bound, worst {(err / np.maximum(bound, 1e-300)).max():.2f} times"
+
+
+ROTARY = [  # tokens, heads, dim, rot
+    (1, 1, 2, 2), (1, 40, 128, 128), (3, 5, 64, 32), (7, 3, 90, 50), (2, 2, 17, 16), (33, 7, 80, 80), (5, 1, 256, 6), (4, 3, 96, 34),
+    (129, 6, 200, 200), (2000, 12, 128, 64), (1, 2, 1000, 998),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("T,H,D,rot", ROTARY)
+def test_rotary(torch, T, H, D, rot, layout, dtype):
+    """Out of place from a strided input into a strided output, and in place: the same bits."""
+    rng = np.random.default_rng(T + H + D)
+    both = _rand(torch, (T, H + 2, D + 3), dtype, 1).cuda()
+    x = both[:, 1:H + 1, 1:D + 1]
+    pos = np.concatenate([[0], rng.integers(-5, 1 << 30, T)])[-T:]
+    pos[0] = 0
+    f = rng.uniform(0, 1, rot // 2) ** 4
+    amp = 1.25
+    spare = torch.full((T, H, D + 5), 7.0, device="cuda", dtype=x.dtype)
+    got = neo.rotary(x, cuda(pos), cuda(f), layout=layout, amplitude=amp, out=spare[..., 2:D + 2])
+    assert (spare[..., :2] == 7).all() and (spare[..., D + 2:] == 7).all()
+    _turn_check(_np(got), _np(x), pos, f, layout, amp, dtype)
+    assert torch.equal(neo.rotary(x, cuda(pos), cuda(f), layout=layout, amplitude=amp), got)
+    was = both.clone()
+    assert neo.rotary(x, cuda(pos), cuda(f), layout=layout, amplitude=amp, out=x) is x
+    assert torch.equal(x, got)
+    x.copy_(was[:, 1:H + 1, 1:D + 1])
+    assert torch.equal(both, was)          # nothing beside the rows is touched
+
+
+@gpu
+def test_rotary_back(torch):
+    """Positions of the other sign turn back; position 0 and an amplitude of 1 change nothing."""
+    x = _rand(torch, (50, 4, 64), "float32", 3).cuda()
+    f = neo.rotary_frequencies(64, scaling="turns", factor=4, context=100, low=1, high=8)
+    pos = torch.arange(50, device="cuda") * 1000
+    y = neo.rotary(neo.rotary(x, pos, f), -pos, f)
+    # |a c| + |b s| is at most the pair's norm, sqrt(2) of the largest: 5 u of that, and sqrt(2) 5 u turned back
+    assert (y - x).abs().max() <= (5 + 5 * 2 ** 0.5) * 2 ** 0.5 * (1 + 2.0 ** -6) * u * x.abs().max()
+    assert torch.equal(neo.rotary(x, pos * 0, f), x)
+
+
+@gpu
+def test_rotary_bad_values_stay_in_their_pair(torch):
+    x = _rand(torch, (3, 2, 32), "float32", 4).cuda()
+    pos = torch.tensor([5, 6, 7], device="cuda")
+    f = neo.rotary_frequencies(32)
+    good = neo.rotary(x, pos, f)
+    x[1, 0, 3] = math.inf
+    x[2, 1, 20] = math.nan
+    got = neo.rotary(x, pos, f)
+    same = torch.ones_like(x, dtype=torch.bool)
+    same[1, 0, [3, 19]] = False
+    same[2, 1, [4, 20]] = False
+    assert torch.equal(got[same], good[same]) and not torch.isfinite(got[~same]).any()
+
+
+WRITES = [  # tokens, group, kv heads, dim, page, rot
+    (1, 1, 1, 16, 1, 2), (5, 4, 2, 128, 16, 128), (3, 3, 1, 80, 10, 24), (64, 4, 8, 128, 64, 64), (9, 1, 3, 96, 7, 50), (2, 2, 2, 256, 16, 256),
+    (40, 2, 2, 240, 5, 6), (700, 5, 4, 64, 16, 64), (900, 1, 8, 128, 32, 100),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("T,G,H,D,page,rot", WRITES)
+def test_rotary_write(torch, T, G, H, D, page, rot, layout, dtype):
+    """Queries as neo_rotary turns them; keys within the bound; values, skipped tokens and other
+    entries as neo_kv_write_int8 leaves them."""
+    rng = np.random.default_rng(T + D + rot)
+    P = -(-T // page) + 3
+    qkv = _rand(torch, (T, (G + 2) * H, D), dtype, 5).cuda()
+    q, k, v = qkv.split([G * H, H, H], 1)
+    slots = rng.permutation(P * page)[:T]
+    if T > 2:
+        slots[1], slots[T - 1] = -1, P * page
+    pos, f, amp = rng.integers(0, 1 << 20, T), rng.uniform(0, 1, rot // 2) ** 3, 0.75
+    fresh = lambda: tuple(torch.full(s, 5, device="cuda", dtype=t) for s, t in  # noqa: E731
+                          (((P, H, page, D), torch.int8), ((P, H, page, D), torch.int8), ((P, H, page), torch.float32), ((P, H, page), torch.float32)))
+    cache, other = fresh(), fresh()
+    args = cuda(slots), cuda(pos), cuda(f)
+    got = neo.rotary_kv_write_int8(cache, q, k, v, *args, layout=layout, amplitude=amp)
+    assert torch.equal(got, neo.rotary(q, *args[1:], layout=layout, amplitude=amp))
+    neo.kv_write_int8(other, v, v, args[0])
+    assert torch.equal(cache[1], other[1]) and torch.equal(cache[3], other[3])
+    real = (slots >= 0) & (slots < P * page)
+    p, o = slots[real] // page, slots[real] % page
+    y, _, _ = _turned(_np(k)[real], pos[real], f, layout, amp)
+    kq, ks = _np(cache[0]), _np(cache[2])
+    _step_check(kq[p, :, o].reshape(-1, D), ks[p, :, o].reshape(-1), y.reshape(-1, D), 10 * u + 2.0 ** -29)
+    left = np.ones((P, page), bool)
+    left[p, o] = False
+    assert (kq.transpose(0, 2, 1, 3)[left] == 5).all() and (ks.transpose(0, 2, 1)[left] == 5).all()
+    again = fresh()
+    assert neo.rotary_kv_write_int8(again, q, k, v, *args, layout=layout, amplitude=amp, q_out=q) is q
+    assert torch.equal(q, got) and all(torch.equal(a, b) for a, b in zip(again, cache))
+
+
+@gpu
+def test_rotary_write_bad_values(torch):
+    """A key with an infinity is a NaN scale and zeros; a row of zeros has scale 1."""
+    q = _rand(torch, (3, 2, 32), "bfloat16", 6).cuda()
+    k, v = q.clone(), q.clone()
+    k[0, 0, 30], k[1, 1], v[2, 0] = math.inf, 0, math.nan
+    cache = neo.kv_cache(1, 2, 4, 32)
+    neo.rotary_kv_write_int8(cache, q, k, v, torch.arange(3, device="cuda"), torch.arange(3, device="cuda") + 9, neo.rotary_frequencies(16))
+    ks, vs = cache.k_scale[0, :, :3], cache.v_scale[0, :, :3]
+    assert torch.isnan(ks).tolist() == [[True, False, False], [False, False, False]] and torch.isnan(vs).tolist() == [[False, False, True], [False] * 3]
+    assert (cache.k[0, 0, 0] == 0).all() and (cache.k[0, 1, 1] == 0).all() and ks[1, 1] == 1
+
+
+# ---- pages -------------------------------------------------------------------------------
+
+def _layers(torch, layers, P, H, page, D, seed):
+    """Caches of all layers, some scales NaN of several bit patterns."""
+    rng = np.random.default_rng(seed)
+    q = [rng.integers(-128, 128, (layers, P, H, page, D)).astype(np.int8) for _ in "kv"]
+    s = [rng.integers(-2 ** 31, 2 ** 31, (layers, P, H, page)).astype(np.int32).view(np.float32) for _ in "kv"]
+    return q + s
+
+
+def _bits(t):
+    a = t.cpu().numpy() if hasattr(t, "cpu") else t
+    return a.view(np.int32) if a.dtype == np.float32 else a
+
+
+COPIES = [  # layers, pages, heads, page size, dim, pairs
+    (1, 4, 1, 1, 16, 2), (3, 20, 2, 16, 64, 9), (2, 9, 3, 10, 80, 4), (5, 12, 8, 64, 128, 5), (1, 70, 1, 128, 256, 30), (40, 8, 2, 7, 48, 3),
+]
+
+
+@gpu
+@pytest.mark.parametrize("partly", [False, True])
+@pytest.mark.parametrize("layers,P,H,page,D,n", COPIES)
+def test_copy_pages(torch, layers, P, H, page, D, n, partly):
+    rng = np.random.default_rng(P)
+    have = _layers(torch, layers, P, H, page, D, P)
+    order = rng.permutation(P)
+    dst, src = order[:n].astype(np.int32), order[n:][rng.integers(0, P - n, n)].astype(np.int32)    # (a source may serve many)
+    count = rng.integers(-1, page + 3, n).astype(np.int32) if partly else np.full(n, page, np.int32)
+    if n > 2:
+        src[0], dst[1] = -1, P              # outside the cache: skipped
+    if n > 3:
+        src[2] = dst[2]
+    want = [a.copy() for a in have]
+    for s, d, e in zip(src, dst, count):
+        if 0 <= s < P and 0 <= d < P:
+            for a in want:
+                a[:, d, :, :max(e, 0)] = a[:, s, :, :max(e, 0)]
+    dev = tuple(cuda(a) for a in have)
+    neo.kv_copy_pages(dev, cuda(src), cuda(dst), entries=cuda(count) if partly else None)
+    assert all((_bits(a) == _bits(b)).all() for a, b in zip(dev, want))
+    one = tuple(cuda(a[0]) for a in have)   # a single layer's cache, without a layer in front
+    neo.kv_copy_pages(one, cuda(src), cuda(dst), entries=cuda(count) if partly else None)
+    assert all((_bits(a) == _bits(b[0])).all() for a, b in zip(one, want))
+
+
+def _tables(rng, need, P):
+    table = np.full((len(need), max(need) + 1), -1, np.int32)
+    order, at = rng.permutation(P).astype(np.int32), 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table
+
+
+def _compacted(have, table, bases, keep):
+    """The definition, token by token, from a copy of what was there."""
+    want, P, page = [a.copy() for a in have], have[0].shape[1], have[0].shape[3]
+    for b, (base, ks) in enumerate(zip(bases, keep)):
+        for i, k in enumerate(ks):
+            t = base + i
+            if base < 0 or k <= t or k >= table.shape[1] * page:
+                continue
+            p, d = table[b, k // page], table[b, t // page]
+            if 0 <= p < P and 0 <= d < P:
+                for a, h in zip(want, have):
+                    a[:, d, :, t % page] = h[:, p, :, k % page]
+    return want
+
+
+COMPACTS = [  # layers, heads, page size, dim, (base, tokens, share kept) of every sequence
+    (1, 1, 1, 16, [(0, 5, 0.5)]), (2, 8, 16, 128, [(100, 8, 0.5), (0, 8, 0.2), (37, 3, 1.0), (5, 6, 0.0)]), (3, 2, 10, 80, [(0, 400, 0.9), (13, 300, 0.3)]),
+    (1, 3, 64, 64, [(3, 5000, 0.5), (0, 100, 0.5)]), (1, 1, 128, 256, [(70, 700, 0.98)]), (17, 2, 7, 48, [(9, 20, 0.5)] * 5),
+]
+
+
+@gpu
+@pytest.mark.parametrize("case", range(len(COMPACTS)))
+def test_compact(torch, case):
+    layers, H, page, D, seqs = COMPACTS[case]
+    rng = np.random.default_rng(case)
+    need = [-(-(b + t) // page) for b, t, _ in seqs]
+    P = sum(need) + 2
+    table = _tables(rng, need, P)
+    have = _layers(torch, layers, P, H, page, D, case)
+    bases = [b for b, _, _ in seqs]
+    keep = [[b + i for i in range(t) if rng.random() < share] for b, t, share in seqs]
+    want = _compacted(have, table, bases, keep)
+    starts = np.concatenate([[0], np.cumsum([len(k) for k in keep])]).astype(np.int32)
+    flat = np.array([x for k in keep for x in k], np.int32)
+    for _ in range(2):                      # (from the start again: the same bits)
+        dev = tuple(cuda(a) for a in have)
+        neo.kv_compact(dev, cuda(table), cuda(np.array(bases, np.int32)), cuda(flat), cuda(starts), max(len(k) for k in keep))
+        assert all((_bits(a) == _bits(b)).all() for a, b in zip(dev, want))
+
+
+@gpu
+def test_compact_entries_of_any_kind(torch):
+    """Entries that repeat, do not ascend, lie below their place, past the table or in pages that do
+    not exist; a bound below a sequence's entries, a base that is negative."""
+    layers, H, page, D, P = 2, 2, 4, 32, 40
+    rng = np.random.default_rng(3)
+    table = _tables(rng, [12, 12, 12], P)
+    table[1, 3], table[1, 6] = -1, P        # (tokens 12 .. 15 and 24 .. 27 are nowhere)
+    have = _layers(torch, layers, P, H, page, D, 9)
+    bases = [2, 0, -3]
+    keep = [[47, 9, 9, 3, 30, 6, 8, 60, 2 ** 31 - 1, 45, -7, 40], [13, 5, 25, 20, 4, 5, 6, 31, 30, 29, 28, 40, 41, 42, 43, 44], [5, 6, 7]]
+    most = 14
+    want = _compacted(have, table, bases, [k[:most] for k in keep])
+    starts = np.concatenate([[0], np.cumsum([len(k) for k in keep])]).astype(np.int32)
+    dev = tuple(cuda(a) for a in have)
+    neo.kv_compact(dev, cuda(table), cuda(np.array(bases, np.int32)), cuda(np.array([x for k in keep for x in k], np.int32)), cuda(starts), most)
+    assert all((_bits(a) == _bits(b)).all() for a, b in zip(dev, want))
+
+
+@gpu
+def test_pages_past_32_bits(torch):
+    """Pages whose bytes lie past 2^32 from the cache's start."""
+    P, H, page, D = 40000, 8, 64, 128       # 2.6 GB of keys
+    cache = neo.kv_cache(P, H, page, D)
+    k = _rand(torch, (2 * page, H, D), "float16", 1).cuda()
+    far = (P - 2) * page + torch.arange(2 * page, device="cuda")
+    neo.kv_write_int8(cache, k, k, far)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    neo.kv_copy_pages(cache, i32([P - 2, P - 1]), i32([P - 4, 0]))
+    assert torch.equal(cache.k[P - 4], cache.k[P - 2]) and torch.equal(cache.k[0], cache.k[P - 1]) and torch.equal(cache.v_scale[0], cache.v_scale[P - 1])
+    want = cache.k[P - 2].clone(), cache.v_scale[P - 1].clone()
+    neo.kv_compact(cache, i32([[P - 4, P - 2, P - 1]]), i32([0]), i32(list(range(page, 3 * page))), i32([0, 2 * page]), 2 * page)
+    assert torch.equal(cache.k[P - 4], want[0]) and torch.equal(cache.v_scale[P - 2], want[1])
+
+
+# ---- attention ----------------------------------------------------------------------------
+
+def _shared(groups, H, D, page, seed, spare=2):
+    """groups: (prefix, [(new, own), ...]); own may be negative (a sequence inside its prefix).  A
+    cache whose unused entries hold NaN scales and extreme bytes, tables whose sequences share
+    the whole pages of their group's prefix and hold copies of the rest of it."""
+    rng = np.random.default_rng(seed)
+    seqs = [(p, n, own, i == 0) for p, s in groups for i, (n, own) in enumerate(s)]
+    need = [-(-max(p + own, p if first else 0) // page) for p, _, own, first in seqs]
+    P = sum(need) + spare
+    k, v = (np.clip(np.rint(rng.normal(size=(P, H, page, D)) * 40), -127, 127).astype(np.int8) for _ in "kv")
+    ks, vs = (rng.uniform(0.005, 0.05, (P, H, page)).astype(np.float32) for _ in "kv")
+    table = np.full((len(seqs), max(need) + 1), 1 << 30, np.int32)
+    order, at, used, lead = rng.permutation(P), 0, np.zeros((P, page), bool), 0
+    for b, (p, _, own, first) in enumerate(seqs):
+        lead = b if first else lead
+        whole = 0 if first else min(p // page, need[b])
+        table[b, :whole] = table[lead, :whole]
+        table[b, whole:need[b]] = order[at:at + need[b] - whole]
+        at += need[b] - whole
+        if not first and p % page and need[b] > p // page:
+            for a in (k, v, ks, vs):
+                a[table[b, p // page], :, :p % page] = a[table[lead, p // page], :, :p % page]
+        for t in range(max(p + own, p if first else 0)):
+            used[table[b, t // page], t % page] = True
+    for s, x in ((ks, k), (vs, v)):
+        s.transpose(0, 2, 1)[~used] = np.nan
+        x.transpose(0, 2, 1, 3)[~used] = -128
+    chunks, contexts = [n for _, n, _, _ in seqs], [p + own for p, _, own, _ in seqs]
+    first = np.concatenate([[0], np.cumsum([len(s) for _, s in groups])]).astype(np.int32)
+    return k, v, ks, vs, table, chunks, contexts, first, np.array([p for p, _ in groups], np.int32)
+
+
+def _most(groups):
+    return max(sum(n for n, _ in s) for _, s in groups)
+
+
+def _attend(torch, dtype, groups, Hq, H, D, page, window=0, seed=0, spread=1.0, max_group=None, max_own=None):
+    k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, H, D, page, seed)
+    starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+    q = _rand(torch, (int(starts[-1]), Hq, D), dtype, seed + 1, spread)
+    scale = D ** -0.5
+    ref, A, B = _attention64(q.double().numpy(), k, v, ks, vs, table, contexts, starts, scale, window)
+    run = lambda: neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q.cuda(), cuda(table), cuda(np.array(contexts, np.int32)),  # noqa: E731
+                                            cuda(starts), cuda(first), cuda(prefix), max(chunks), _most(groups) if max_group is None else max_group,
+                                            max(contexts), max_own, scale=scale, window=window)
+    got = run()
+    err = np.abs(_np(got) - ref)
+    bound = _attention_bound(ref, A, B, D, max(contexts), dtype) + 16 * u * A
+    assert np.isfinite(_np(got)).all()
+    assert (err <= bound).all(), f"{(err > bound).sum()} of {err.size} beyond the bound, worst {(err / bound).max():.2f} times"
+    assert torch.equal(run(), got)
+    return got
+
+
+SHARED = [  # groups, q heads, kv heads, head dim, page size, window
+    ([(1, [(1, 1), (1, 1)])], 1, 1, 16, 1, 0),
+    ([(33, [(1, 1), (1, 3)])], 4, 1, 64, 16, 0),
+    ([(300, [(1, 1), (1, 40), (1, 17)]), (64, [(1, 9), (1, 1)])], 8, 2, 128, 64, 0),
+    ([(45, [(3, 5), (0, 2), (2, 30)]), (0, [(1, 70), (2, 3)]), (90, [(4, 4)])], 6, 2, 64, 10, 0),
+    ([(1500, [(1, 700)] * 5)], 16, 1, 80, 16, 0),
+    ([(1111, [(1, 20)] * 9)], 24, 3, 256, 32, 0),
+    ([(200, [(1, 9)] * 9), (31, [(1, 50)] * 2)], 32, 4, 128, 16, 0),
+    ([(97, [(40, 90), (1, 3), (9, 9)])], 8, 2, 96, 7, 0),
+    ([(500, [(7, 60)] * 12), (129, [(30, 30), (2, 200)])], 10, 2, 128, 64, 0),
+    ([(2500, [(1, 100)] * 70)], 8, 1, 64, 128, 0),
+    ([(600, [(60, 300), (100, 100), (3, 900)])], 4, 1, 240, 48, 0),
+    ([(300, [(1, 40), (5, 90), (1, 1)]), (80, [(1, 10), (1, 200)])], 8, 4, 64, 16, 60),
+    ([(300, [(30, 40), (70, 90), (1, 1)])], 4, 1, 128, 16, 350),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(SHARED)))
+def test_shared_attention(torch, case, dtype):
+    groups, Hq, H, D, page, window = SHARED[case]
+    _attend(torch, dtype, groups, Hq, H, D, page, window, seed=case)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("spread", [1e-4, 30.0])
+def test_shared_attention_flat_and_sharp(torch, dtype, spread):
+    _attend(torch, dtype, [(700, [(1, 40), (30, 60), (2, 500)])], 4, 2, 64, 16, seed=50, spread=spread)
+
+
+@gpu
+@pytest.mark.parametrize("max_group", [0, 1, 2, 5])
+def test_groups_beyond_the_bound_read_for_themselves(torch, max_group):
+    """A group of two tokens within it, one of five beyond it below 5."""
+    _attend(torch, "bfloat16", [(150, [(1, 30), (1, 2)]), (220, [(1, 30), (3, 40), (1, 5)])], 4, 2, 64, 16, seed=60, max_group=max_group)
+
+
+@gpu
+@pytest.mark.parametrize("max_own", [0, 40, 1300])
+def test_the_layout_of_the_work_changes_no_more_than_rounding(torch, max_own):
+    """max_own below what the sequences have, as tight as it may be, and above."""
+    _attend(torch, "float16", [(150, [(1, 30), (5, 40)]), (0, [(4, 1200)]), (90, [(2, 7)])], 4, 2, 64, 16, seed=61, max_own=max_own)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("new", [1, 20])
+def test_sequences_inside_their_prefix(torch, new, dtype):
+    """Contexts that end before the prefix does: their tokens see a part of it and nothing else."""
+    _attend(torch, dtype, [(400, [(new, 30), (new, -100), (new, -380), (new, 0)])], 4, 2, 64, 16, seed=63)
+
+
+@gpu
+@pytest.mark.parametrize("new", [5, 40])
+def test_shared_rows_that_see_nothing(torch, new):
+    """More new tokens than context, in a group and out of one; pages of the prefix outside the cache."""
+    groups = [(30, [(new, 20), (new, new - 30 - 3)]), (8, [(new, new - 8 - 2)])]
+    k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, 2, 64, 4, 64)
+    table[0, 2] = table[1, 2] = -1          # tokens 8 .. 11 of both
+    starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+    q = _rand(torch, (int(starts[-1]), 4, 64), "float16", 65)
+    q[new, 1, 5] = math.inf                 # (a query that sees nothing is zeros whatever it holds)
+    got = _np(neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q.cuda(), cuda(table), cuda(np.array(contexts, np.int32)),
+                                        cuda(starts), cuda(first), cuda(prefix), new, 2 * new, max(contexts), scale=0.125))
+    assert (got[new:new + 3] == 0).all() and (got[2 * new:2 * new + 2] == 0).all()
+    q[new, 1, 5] = 0
+    for b in range(3):
+        n, c = chunks[b], contexts[b]
+        for i in range(n):
+            p = c - n + i
+            seen = [j for j in range(p + 1) if 0 <= table[b, j // 4] < k.shape[0]]
+            for h in range(4):
+                if not seen:
+                    assert (got[starts[b] + i, h] == 0).all()
+                    continue
+                pg, o = table[b, np.array(seen) // 4], np.array(seen) % 4
+                keys = k[pg, h // 2, o].astype(np.float64) * ks[pg, h // 2, o][:, None]
+                vals = v[pg, h // 2, o].astype(np.float64) * vs[pg, h // 2, o][:, None]
+                row = q[starts[b] + i, h].double().numpy()
+                s = keys @ row * 0.125
+                w = np.exp(s - s.max())
+                ref, A, B = w @ vals / w.sum(), w @ np.abs(vals) / w.sum(), (np.abs(keys) @ np.abs(row)).max() * 0.125
+                assert (np.abs(got[starts[b] + i, h] - ref) <= _attention_bound(ref, A, B, 64, max(contexts), "float16") + 16 * u * A).all()
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 30])
+def test_shared_bad_entries_and_queries(torch, new):
+    """A NaN among one sequence's own keys, and an infinity in one query, reach that sequence, that
+    query alone; one among the shared values reaches all of its group and no other."""
+    groups = [(100, [(new, 30 + new), (new, 40 + new)]), (60, [(new, 50), (new, 30)])]
+    k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, 1, 64, 16, 66)
+    starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+    q = _rand(torch, (int(starts[-1]), 2, 64), "bfloat16", 67).cuda()
+    run = lambda q: neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q, cuda(table), cuda(np.array(contexts, np.int32)),  # noqa: E731
+                                              cuda(starts), cuda(first), cuda(prefix), new, 2 * new, max(contexts))
+    good = run(q)
+    at = table[1, 110 // 16], 0, 110 % 16
+    for s in (ks, vs):
+        was, s[at] = s[at], np.nan
+        got = run(q)
+        s[at] = was
+        assert torch.equal(got[:new], good[:new]) and torch.equal(got[2 * new:], good[2 * new:])
+        assert torch.isnan(got[new:2 * new]).any(-1).all()
+    at = table[0, 3], 0, 5
+    was, vs[at] = vs[at], np.nan
+    got = run(q)
+    vs[at] = was
+    assert torch.equal(got[2 * new:], good[2 * new:]) and torch.isnan(got[:2 * new]).any(-1).all()
+    bad = q.clone()
+    bad[0, 1, 3] = math.inf
+    got = run(bad)
+    assert torch.isnan(got[0, 1]).all() and torch.equal(got[0, 0], good[0, 0]) and torch.equal(got[1:], good[1:])
+
+
+@gpu
+def test_shared_attention_strides(torch):
+    groups = [(90, [(3, 30), (2, 40)])]
+    k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, 2, 64, 16, 68)
+    q = _rand(torch, (5, 9, 80), "float16", 69).cuda()
+    rest = (cuda(np.array(contexts, np.int32)), cuda(np.array([0, 3, 5], np.int32)), cuda(first), cuda(prefix), 3, 5, max(contexts))
+    cache = cuda(k), cuda(v), cuda(ks), cuda(vs)
+    want = neo.attention_shared_int8(cache, q[:, 3:7, 8:72].contiguous(), cuda(table), *rest)
+    out = torch.full((5, 6, 70), 3.0, device="cuda", dtype=torch.float16)
+    wide = torch.cat([cuda(table), cuda(table)], 1)
+    got = neo.attention_shared_int8(cache, q[:, 3:7, 8:72], wide[:, :table.shape[1]], *rest, out=out[:, 1:5, 3:67])
+    assert torch.equal(got, want) and (out[:, 0] == 3).all() and (out[:, 5] == 3).all() and (out[..., :3] == 3).all() and (out[..., 67:] == 3).all()
+
+
+@gpu
+def test_many_sequences_in_groups(torch):
+    """More sequences than a workgroup has threads, groups of one to nine."""
+    rng = np.random.default_rng(70)
+    groups = [(int(rng.integers(0, 60)), [(1, int(rng.integers(1, 30))) for _ in range(rng.integers(1, 10))]) for _ in range(150)]
+    _attend(torch, "float16", groups, 2, 1, 32, 16, seed=70)
+
+
+# ---- as they are used together -----------------------------------------------------------
+
+def _i32(torch, v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+@gpu
+def test_a_forked_prompt(torch):
+    """A prompt is written, forks, its copies go on for some tokens, drop some of them, and attend: the
+    same as sequences that were written apart."""
+    H, G, D, page, L, T = 2, 3, 64, 16, 2, 41
+    f = neo.rotary_frequencies(D)
+    mine, apart = (neo.kv_cache(40, H, page, D, layers=L) for _ in range(2))
+    pages = [[0, 1, 2, 9], [0, 1, 3, 10], [0, 1, 4, 11]]
+    alone = [[10 * b + i for i in range(4)] for b in range(3)]
+    slot = lambda p, t: torch.tensor([p[i // page] * page + i % page for i in t], device="cuda")  # noqa: E731
+    qkv = lambda n, seed: _rand(torch, (n, (G + 2) * H, D), "bfloat16", seed).cuda().split([G * H, H, H], 1)  # noqa: E731
+    for layer in range(L):
+        q, k, v = qkv(T, 80 + layer)
+        at = torch.arange(T, device="cuda")
+        neo.rotary_kv_write_int8(neo.kv_layer(mine, layer), q, k, v, slot(pages[0], range(T)), at, f)
+        for p in alone:
+            neo.rotary_kv_write_int8(neo.kv_layer(apart, layer), q, k, v, slot(p, range(T)), at, f)
+    neo.kv_copy_pages(mine, _i32(torch, [2, 2]), _i32(torch, [3, 4]), entries=_i32(torch, [T % page] * 2))
+    for layer in range(L):                  # ten tokens more each; of those the odd ones stay
+        for b in range(3):
+            q, k, v = qkv(10, 90 + 10 * layer + b)
+            at = T + torch.arange(10, device="cuda")
+            neo.rotary_kv_write_int8(neo.kv_layer(mine, layer), q, k, v, slot(pages[b], range(T, T + 10)), at, f)
+            odd = torch.arange(1, 10, 2, device="cuda")
+            neo.rotary_kv_write_int8(neo.kv_layer(apart, layer), q[odd], k[odd], v[odd], slot(alone[b], range(T, T + 5)), at[odd], f)
+    kept = [T + i for i in range(1, 10, 2)]
+    neo.kv_compact(mine, _i32(torch, pages), _i32(torch, [T] * 3), _i32(torch, kept * 3), _i32(torch, [0, 5, 10, 15]), 5)
+    q = _rand(torch, (3, G * H, D), "bfloat16", 99).cuda()
+    ctx, starts = _i32(torch, [T + 5] * 3), _i32(torch, [0, 1, 2, 3])
+    for layer in range(L):
+        one = neo.attention_shared_int8(neo.kv_layer(mine, layer), q, _i32(torch, pages), ctx, starts, _i32(torch, [0, 3]), _i32(torch, [T]), 1, 3, T + 5, 5)
+        two = neo.attention_paged_int8(neo.kv_layer(apart, layer), q, _i32(torch, alone), ctx, starts, 1, T + 5)
+        # both round the output (2^-8) and the weights (2^-11, and less than 2^-12 for what float32 does, of values up to top)
+        top = max(t.abs().max() for t in neo.kv_read_int8(neo.kv_layer(apart, layer), torch.arange(40 * page, device="cuda"), torch.float32)[1:])
+        assert ((one.float() - two.float()).abs() <= 2 * (2.0 ** -8 * (1 + 2.0 ** -7) * two.float().abs() + (2.0 ** -11 + 2.0 ** -12) * top)).all()
+        for a, b in zip(neo.kv_layer(mine, layer), neo.kv_layer(apart, layer)):
+            for p, r in zip(pages, alone):
+                x, y = (t[s].transpose(0, 1).reshape(H, 4 * page, -1)[:, :T + 5] for t, s in ((a, p), (b, r)))
+                assert torch.equal(x, y)
+
+
+@gpu
+def test_graph_of_all(torch):
+    """A step captured into a graph (rotation and write, a copy, closing up, attention) and replayed
+    several times with eager work between gives the eager call's bits each time."""
+    groups = [(1200, [(1, 30)] * 6), (300, [(1, 500)] * 2)]
+    k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, 2, 128, 16, 71, spare=4)
+    base = tuple(cuda(np.nan_to_num(a)) for a in (k, v, ks, vs))
+    cache = tuple(t.clone() for t in base)
+    P, T = k.shape[0], 8
+    qkv = _rand(torch, (T, 12, 128), "bfloat16", 72).cuda()
+    q, kn, vn = qkv.split([8, 2, 2], 1)
+    tab, ctx, starts, fs, pl = (cuda(a) for a in (table, np.array(contexts, np.int32), np.arange(T + 1, dtype=np.int32), first, prefix))
+    slots = torch.tensor([int(table[b, (c - 1) // 16]) * 16 + (c - 1) % 16 for b, c in enumerate(contexts)], device="cuda")
+    pos, f = (ctx - 1).long(), neo.rotary_frequencies(128)
+    free = [p for p in range(P) if p not in set(table.flatten().tolist())][:2]
+    src, dst = _i32(torch, [int(table[0, 0]), int(table[6, 0])]), _i32(torch, free)
+    bases, keep, ksts = _i32(torch, [c - 3 for c in contexts]), _i32(torch, [x for c in contexts for x in (c - 2, c - 1)]), _i32(torch, list(range(0, 17, 2)))
+    q_out, out = torch.empty(T, 8, 128, device="cuda", dtype=torch.bfloat16), torch.empty(T, 8, 128, device="cuda", dtype=torch.bfloat16)
+
+    def step():
+        neo.rotary_kv_write_int8(cache, q, kn, vn, slots, pos, f, q_out=q_out)
+        neo.attention_shared_int8(cache, q_out, tab, ctx, starts, fs, pl, 1, 6, max(contexts), out=out)
+        neo.kv_copy_pages(cache, src, dst)
+        neo.kv_compact(cache, tab, bases, keep, ksts, 2)
+
+    def back():
+        for a, b in zip(cache, base):
+            a.copy_(b)
+        out.zero_()
+        torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        back()
+        step()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in cache] + [out.clone(), q_out.clone()]
+        back()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step()
+        for i in range(4):
+            back()
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip([*cache, out, q_out], want)), i
+            if i == 1:                      # a larger call of the stream, and what it computes, between
+                neo.attention_shared_int8(cache, q_out.repeat(4, 1, 1), tab, ctx, starts * 4, fs, pl, 4, 24, max(contexts))
+                torch.cuda.synchronize()
+
+
+@gpu
+def test_two_streams(torch):
+    """Calls of different sizes under way on two streams at once, each with its own workspace."""
+    calls = []
+    for i, groups in enumerate(([(2000, [(1, 60)] * 9)], [(900, [(20, 90)] * 4)])):
+        k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, 2, 128, 16, 73 + i)
+        starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+        q = _rand(torch, (int(starts[-1]), 8, 128), "bfloat16", 75 + i).cuda()
+        args = ((cuda(k), cuda(v), cuda(ks), cuda(vs)), q, cuda(table), cuda(np.array(contexts, np.int32)), cuda(starts), cuda(first), cuda(prefix),
+                max(chunks), _most(groups), max(contexts))
+        calls.append(lambda args=args, **kw: neo.attention_shared_int8(*args, **kw))
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    got = [[c(stream=s) for _ in range(20)] for c, s in zip(calls, streams)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, w) for xs, w in zip(got, want) for x in xs)
+
+
+@gpu
+def test_no_work(torch):
+    """No tokens, no pairs, nothing kept: nothing happens."""
+    cache = neo.kv_cache(2, 1, 4, 16, layers=2)
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    f = neo.rotary_frequencies(16)
+    x = torch.empty(0, 2, 16, device="cuda")
+    long = torch.empty(0, dtype=torch.int64, device="cuda")
+    assert neo.rotary(x, long, f).shape == (0, 2, 16)
+    assert neo.rotary_kv_write_int8(neo.kv_layer(cache, 0), x, x[:, :1], x[:, :1], long, long, f).shape == (0, 2, 16)
+    neo.kv_copy_pages(cache, none, none)
+    neo.kv_compact(cache, _i32(torch, [[0, 1]]), _i32(torch, [0]), none, _i32(torch, [0, 0]), 3)
+    assert neo.attention_shared_int8(neo.kv_layer(cache, 0), x, _i32(torch, [[0]]), _i32(torch, [0]), _i32(torch, [0, 0]), _i32(torch, [0, 1]),
+                                     _i32(torch, [0]), 1, 1, 4).shape == (0, 2, 16)
+    assert all((t == 0).all() for t in cache)
+
+
+@gpu
+def test_wrong_tensors_are_refused(torch):
+    cache = neo.kv_cache(2, 1, 4, 16, layers=2)
+    one = neo.kv_layer(cache, 0)
+    z = _i32(torch, [0, 0])
+    x = torch.ones(1, 1, 16, device="cuda")
+    f = neo.rotary_frequencies(16)
+    pos = torch.zeros(1, dtype=torch.int64, device="cuda")
+    t = z[:1].view(1, 1)
+    for bad in (lambda: neo.rotary(x[0], pos, f), lambda: neo.rotary(x, pos.int(), f), lambda: neo.rotary(x, pos[:0], f),
+                lambda: neo.rotary(x, pos, f.float()), lambda: neo.rotary(x.double(), pos, f), lambda: neo.rotary(x.cpu(), pos, f),
+                lambda: neo.rotary(x, pos, f, out=x.half()), lambda: neo.rotary(x, pos, f, out=x[:, :, :8]),
+                lambda: neo.rotary_kv_write_int8(cache, x, x, x, pos, pos, f), lambda: neo.rotary_kv_write_int8(one, x, x.half(), x, pos, pos, f),
+                lambda: neo.rotary_kv_write_int8(one, x, x[:0], x[:0], pos, pos, f), lambda: neo.rotary_kv_write_int8(one, x, x, x, pos.int(), pos, f),
+                lambda: neo.kv_copy_pages(cache, z, z[:1]), lambda: neo.kv_copy_pages(cache, z.long(), z), lambda: neo.kv_copy_pages(cache, z, z, entries=z[:1]),
+                lambda: neo.kv_copy_pages(cache[:3] + (cache[3][:1],), z, z), lambda: neo.kv_copy_pages(tuple(c.transpose(0, 1) for c in cache), z, z),
+                lambda: neo.kv_compact(cache, t, z[:0], z, z, 1), lambda: neo.kv_compact(cache, t, z, z, z[:1], 1), lambda: neo.kv_compact(cache, z, z, z, z, 1),
+                lambda: neo.attention_shared_int8(one, x, t, z, z, z[:1], z[:1], 1, 1, 4), lambda: neo.attention_shared_int8(one, x, t, z, z, z, z[:1], 1, 1, 5),
+                lambda: neo.attention_shared_int8(cache, x, t, z, z, z, z[:1], 1, 1, 4)):
+        with pytest.raises((TypeError, ValueError)):
+            bad()
+    with pytest.raises(neo.NeoError):
+        neo.rotary(x, pos, neo.rotary_frequencies(18))
