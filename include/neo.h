@@ -850,7 +850,7 @@ int neo_rotary_frequencies(int rot_dim, double base, int scaling, double factor,
  * neo_rotary: x and y device [tokens][heads][head_dim] of `dtype`, strides per
  *   token and head; positions device int64 [tokens], freqs device float64
  *   [rot_dim / 2].  y may be x itself (same strides); they must not overlap
- *   otherwise.  rot_dim even, 2 .. head_dim; any head_dim up to 65,536.
+ *   otherwise.  rot_dim even, 2 .. head_dim; any head_dim up to 1024.
  * neo_rotary_kv_write_int8: the same for the queries (q to q_out; q_out may be q),
  *   and the keys, turned in float32 and not rounded between, and values quantized
  *   into the entries slots[t] as neo_kv_write_int8 does.  Tokens whose slot lies
@@ -902,8 +902,9 @@ int neo_kv_compact(const neo_kv_cache* cache, int layers, int64_t layer_stride,
  * neo_attention_paged_int8 for sequences of which groups share their first
  * tokens: the sequences group_starts[g] .. group_starts[g + 1] - 1 hold the same
  * prefix_lens[g] first tokens, which are read once for all queries of the group,
- * through the page table of its first sequence.  Its values differ from that call's
- * by the order of their sums only.
+ * through the page table of its first sequence, or, where that would save too
+ * little, through each one's own (which must have them too).  Its values differ from
+ * that call's by the order of their sums only.
  *   group_starts  device int32 [groups + 1], ascending from 0 to seqs; every
  *                 sequence is in one group (of one sequence, maybe, or with a
  *                 prefix of 0)
@@ -911,10 +912,9 @@ int neo_kv_compact(const neo_kv_cache* cache, int layers, int64_t layer_stride,
  *   max_group     host: how many new tokens a group has at most; the sequences
  *                 of one that has more read the prefix each
  *   max_own       host: how many cached tokens a sequence has behind its prefix at
- *                 most.  The work is laid out for it; where one has more, its
- *                 tokens take longer and are the same
- * and the rest as there; every group's prefix has a page in its first
- * sequence's table.  A window hides shared tokens too, but they are read: for
+ *                 most (0: not known).  The work is laid out for it; where one has
+ *                 more, its tokens take longer and are the same
+ * and the rest as there.  A window hides shared tokens too, but they are read: for
  * windows much shorter than the prefix the other call reads less.  The parts of
  * the shared tokens are kept in the workspace of the stream,
  * tokens * q_heads * (head_dim + 2) floats beside those of the shares.

@@ -227,10 +227,11 @@ __device__ inline int64_t share_start(int64_t W, int used, int i) { return W * i
 // Parts in the workspace: part 2 i of share i is the unit it starts in, 2 i + 1
 // the one it ends in; o[part][row of the tile][head_dim] in true units relative
 // to the part's maximum, ml[part][row] (maximum, sum).  starts[i]: where share i
-// starts, for the join (W = 0: no such share).
+// starts, for the join (W = 0: no such share), and of how many parts the unit
+// there consists if it is the first share to start in the middle of it (else 0).
 struct Start {
     int64_t W;
-    int b, h, tile, skip, blocks, unused;
+    int b, h, tile, skip, blocks, count;
 };
 struct Parts {
     float* o;
@@ -404,12 +405,18 @@ struct Walk {
             return share_start(W, used, share);
         });
         if ((int)blockIdx.x >= used || W == 0) {
-            if (threadIdx.x == 0) ws.starts[blockIdx.x].W = 0;
+            if (threadIdx.x == 0) ws.starts[blockIdx.x] = Start{0, 0, 0, 0, 0, 0, 0};
             return false;
         }
         x = uniform(share_start(W, used, share));
         end = uniform(share_start(W, used, share + 1));
-        if (threadIdx.x == 0) ws.starts[share] = Start{W, c.b, c.h, c.tile, c.skip, c.blocks, 0};
+        if (threadIdx.x == 0) {
+            int count = 0;
+            const int64_t x0 = x - c.skip;  // of the unit
+            if (MODE != kAll && c.skip > 0 && x0 >= share_start(W, used, share - 1))
+                count = (int)(((x0 + c.blocks) * used + W - 1) / W) - share + 1;  // (share i starts before y if i < y used / W)
+            ws.starts[share] = Start{W, c.b, c.h, c.tile, c.skip, c.blocks, count};
+        }
         return x < end;
     }
 };
@@ -548,18 +555,18 @@ __device__ inline void load_block(const AttnArgs& a, const Shares& sp, const Key
     }
 }
 
-constexpr int kRowsBlock = kRowsWaves * 32;  // keys the workgroup takes at a time
-
-template <typename T, int DP, bool TILED, int MODE>
-__global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void attention_rows(AttnArgs a, Shares sp, Parts ws) {
+// WAVES: kRowsWaves, or two where there are units enough without (see launch_rows).
+template <typename T, int DP, bool TILED, int MODE, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void attention_rows(AttnArgs a, Shares sp, Parts ws) {
     typedef Weights<T> W;
     constexpr int KB = DP / 4, STEPS = DP / 32, VB = DP / 16;
-    __shared__ float red_m[kRowsWaves][16], red_l[kRowsWaves][16], red_o[kRowsWaves][16][DP + 4];
+    constexpr int kRowsBlock = WAVES * 32;  // keys the workgroup takes at a time
+    __shared__ float red_m[WAVES][16], red_l[WAVES][16], red_o[WAVES][16][DP + 4];
     __shared__ typename Cursor<16, kRowsBlock, MODE>::Scratch scratch;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, g = lane >> 4;
     const int H = a.c.kv_heads, G = a.q_heads / H, D = a.c.head_dim;
     if constexpr (MODE == kShared) write_shared(a);
-    Walk<16, kRowsBlock, kRowsWaves * 64, MODE> walk;
+    Walk<16, kRowsBlock, WAVES * 64, MODE> walk;
     if (!walk.begin(a, sp, G, ws, scratch)) return;
     for (;;) {
         const Unit u = walk.c.u;
@@ -750,7 +757,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
         if (row0 + li < rows) {
             float M = kMinusInf;
 #pragma unroll
-            for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][li]);
+            for (int w = 0; w < WAVES; ++w) M = fmaxf(M, red_m[w][li]);
             const float f = m == kMinusInf ? 0.f : ldexpf(exp2_fast(m - M), E - 14 + 9);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
@@ -760,14 +767,14 @@ __global__ __launch_bounds__(kRowsWaves * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) 
         }
         __syncthreads();
         const int live = min(16, rows - row0);
-        for (int x = threadIdx.x; x < live * DP; x += kRowsWaves * 64) {
+        for (int x = threadIdx.x; x < live * DP; x += WAVES * 64) {
             const int rr = x / DP, d = x - rr * DP, rw = row0 + rr;
             if (d >= D) continue;
             float M = kMinusInf, L = 0.f, v = 0.f;
 #pragma unroll
-            for (int w = 0; w < kRowsWaves; ++w) M = fmaxf(M, red_m[w][rr]);
+            for (int w = 0; w < WAVES; ++w) M = fmaxf(M, red_m[w][rr]);
 #pragma unroll
-            for (int w = 0; w < kRowsWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 L += red_m[w][rr] == kMinusInf ? red_l[w][rr] : red_l[w][rr] * exp2_fast(red_m[w][rr] - M);
                 v += red_o[w][rr][d];
             }
@@ -1180,7 +1187,7 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
 // The parts of the unit in which share j starts, if it is the first to start in
 // it: workgroup (j - 1, y) joins ROUNDS times four rows of the tile, a wave a
 // row, or with WAVES = 4 row y, its waves taking the parts in turn.
-template <typename T, int ROWS, int WAVES, int ROUNDS, int MODE>
+template <typename T, int ROWS, int WAVES, int ROUNDS>
 __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Parts ws) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turn = wave % WAVES;
     const int G = a.q_heads / a.c.kv_heads, D = a.c.head_dim, j = blockIdx.x + 1;
@@ -1193,7 +1200,7 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Par
     // parts: the end of share j - 1, the starts of shares j .. j + count - 2
     int count = 2;
     while (j + count - 1 < used && share_start(W, used, j + count - 1) < x0 + at.blocks) ++count;
-    const Unit u = unit_of<MODE>(a, at.b);
+    const Unit u = unit_of<kAll>(a, at.b);
     static_assert(WAVES == 1 || ROUNDS == 1, "");
 #pragma unroll 1
     for (int round = 0; round < ROUNDS; ++round) {
@@ -1240,7 +1247,69 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Par
         }
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-            if (lane + 64 * x < D) finish<T, MODE>(a, u, at.h, G, row, lane + 64 * x, v[x], M, L);
+            if (lane + 64 * x < D) finish<T, kAll>(a, u, at.h, G, row, lane + 64 * x, v[x], M, L);
+    }
+}
+
+// The same for the other modes: DP / 4 lanes take a row, four columns each, and
+// SPLIT such groups its parts in turn.  What attention_join works out from the
+// shares' starts (64-bit divisions, which bound it where units have few parts)
+// stands in them.
+template <typename T, int DP, int ROWS, int SPLIT, int MODE>
+__global__ __launch_bounds__(256) void attention_join_parts(AttnArgs a, Parts ws) {
+    constexpr int LW = DP / 4, GROUPS = 256 / LW, EACH = GROUPS / SPLIT;
+    const int lane = threadIdx.x % LW, group = threadIdx.x / LW, turn = group % SPLIT;
+    const int G = a.q_heads / a.c.kv_heads, D = a.c.head_dim, j = blockIdx.x + 1;
+    const Start at = ws.starts[j];
+    if (at.count == 0) return;
+    const Unit u = unit_of<MODE>(a, at.b);
+    const int rr = blockIdx.y * EACH + group / SPLIT, row = at.tile * ROWS + rr, count = at.count;
+    if (SPLIT == 1 && row >= u.n * G) return;
+    // (rows past the last have parts that nothing wrote, and are not stored)
+    auto part = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0)) * ROWS + rr; };
+    float M = kMinusInf, L = 0.f;
+    for (int i = lane; i < count; i += LW) M = fmaxf(M, ws.ml[part(i)].x);
+#pragma unroll
+    for (int x = LW / 2; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+    for (int i = lane; i < count; i += LW) L += ws.ml[part(i)].y * part_factor(ws.ml[part(i)].x, M);
+    L = lanes_sum<LW>(L);
+    v4f v = {0, 0, 0, 0};
+    for (int i = turn; i < count; i += 4 * SPLIT) {
+        v4f w[4];
+        float f[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const int64_t at_part = part(min(i + y * SPLIT, count - 1));
+            w[y] = *reinterpret_cast<const v4f*>(ws.o + at_part * D + min(lane * 4, D - 4));
+            f[y] = ws.ml[at_part].x;
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+            if (i + y * SPLIT < count) v += w[y] * part_factor(f[y], M);
+    }
+    if constexpr (SPLIT > 1) {
+        __shared__ v4f red[GROUPS][LW];
+        red[group][lane] = v;
+        __syncthreads();
+        if (turn || row >= u.n * G) return;
+#pragma unroll
+        for (int x = 1; x < SPLIT; ++x) v += red[group + x][lane];
+    }
+    if (lane * 4 >= D) return;
+    const int t = row / G, hq = at.h * G + row - t * G;
+    const int64_t to = (int64_t)(u.first + t) * a.q_heads + hq;
+    v4f* shared = reinterpret_cast<v4f*>(a.part_o + to * D + lane * 4);
+    if constexpr (MODE == kShared) {
+        *shared = v;
+        if (lane == 0) a.part_ml[to] = make_float2(M, L);
+    } else {
+        if (u.from > 0) {
+            const float2 ml = a.part_ml[to];
+            const float top = fmaxf(M, ml.x), f = part_factor(M, top), g = part_factor(ml.x, top);
+            v = v * f + *shared * g;
+            L = L * f + ml.y * g;
+        }
+        store4(static_cast<T*>(a.out) + (int64_t)(u.first + t) * a.ots + (int64_t)hq * a.ohs + lane * 4, v * (L == 0.f ? 0.f : 1.f / L));
     }
 }
 
@@ -1302,8 +1371,26 @@ hipError_t launch_tile(const AttnArgs& a, const Shares& sh, const Parts& p, unsi
     hipLaunchKernelGGL((attention_tile<T, DP, NW, MODE>), dim3(blocks), dim3(NW * 64), C::BYTES, st, a, sh, p);
     e = hipGetLastError();
     if (e != hipSuccess || sh.groups < 2) return e;
-    hipLaunchKernelGGL((attention_join<T, C::ROWS, 1, 4, MODE>), dim3(sh.groups - 1, C::ROWS / 16), dim3(256), 0, st, a, sh, p);
+    if constexpr (MODE == kAll)
+        hipLaunchKernelGGL((attention_join<T, C::ROWS, 1, 4>), dim3(sh.groups - 1, C::ROWS / 16), dim3(256), 0, st, a, sh, p);
+    else
+        hipLaunchKernelGGL((attention_join_parts<T, DP, C::ROWS, 1, MODE>), dim3(sh.groups - 1, C::ROWS / (1024 / DP)), dim3(256), 0, st, a, p);
     return hipGetLastError();
+}
+
+// From so many whole units on two waves take one, not four: more of them lie on the
+// chip at once, and what each waits for (its table, keys, values, its part of the
+// shared tokens) is waited for side by side.  Own tokens of 128 sequences and 8
+// heads, up to 500 each: a call 126 us, 138 with one wave; of 256 sequences 216,
+// 218 and with four 227.
+constexpr int64_t kShortUnits = 1024;
+
+template <typename T, int DP, int MODE, int WAVES>
+void launch_rows(const AttnArgs& a, const Shares& sh, const Parts& p, unsigned blocks, hipStream_t st) {
+    if (a.c.page_size % 16 == 0)
+        hipLaunchKernelGGL((attention_rows<T, DP, true, MODE, WAVES>), dim3(blocks), dim3(WAVES * 64), 0, st, a, sh, p);
+    else
+        hipLaunchKernelGGL((attention_rows<T, DP, false, MODE, WAVES>), dim3(blocks), dim3(WAVES * 64), 0, st, a, sh, p);
 }
 
 template <typename T, int DP, int MODE>
@@ -1318,13 +1405,17 @@ hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
     if (tile == 128) return launch_tile<T, DP, 4, MODE>(a, sh, p, blocks, st);
     if constexpr (DP <= 128)
         if (tile == 256) return launch_tile<T, DP, 8, MODE>(a, sh, p, blocks, st);
-    if (a.c.page_size % 16 == 0)
-        hipLaunchKernelGGL((attention_rows<T, DP, true, MODE>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
+    if (MODE == kOwn && sh.groups == 0 && units >= kShortUnits)
+        launch_rows<T, DP, MODE, MODE == kOwn ? 2 : kRowsWaves>(a, sh, p, blocks, st);
     else
-        hipLaunchKernelGGL((attention_rows<T, DP, false, MODE>), dim3(blocks), dim3(kRowsWaves * 64), 0, st, a, sh, p);
+        launch_rows<T, DP, MODE, kRowsWaves>(a, sh, p, blocks, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || sh.groups < 2) return e;
-    hipLaunchKernelGGL((attention_join<T, 16, 4, 1, MODE>), dim3(sh.groups - 1, std::min(16, a.max_chunk * G)), dim3(256), 0, st, a, sh, p);
+    const unsigned rows = std::min(16, a.max_chunk * G);
+    if constexpr (MODE == kAll)
+        hipLaunchKernelGGL((attention_join<T, 16, 4, 1>), dim3(sh.groups - 1, rows), dim3(256), 0, st, a, sh, p);
+    else  // (a workgroup a row)
+        hipLaunchKernelGGL((attention_join_parts<T, DP, 16, 1024 / DP, MODE>), dim3(sh.groups - 1, rows), dim3(256), 0, st, a, p);
     return hipGetLastError();
 }
 

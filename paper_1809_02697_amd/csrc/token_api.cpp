@@ -292,8 +292,8 @@ int neo_rotary(const void* x, int64_t x_token_stride, int64_t x_head_stride, int
     return guarded("neo_rotary", [&] {
         Check c{"neo_rotary"};
         c.type(dtype) && c.size(tokens, "tokens", 0) && c.size(heads, "heads", 1) && c.size(head_dim, "head_dim", 1);
-        if (c.rc == NEO_OK && (head_dim > 65536 || (int64_t)heads * head_dim > 1 << 28))
-            c.bad(NEO_ERR_UNSUPPORTED, "head_dim above 65,536, or heads * head_dim above 2^28");
+        if (c.rc == NEO_OK && (head_dim > 1024 || (int64_t)heads * head_dim > 1 << 28))
+            c.bad(NEO_ERR_UNSUPPORTED, "head_dim above 1024, or heads * head_dim above 2^28");
         check_rotary(c, x, x_token_stride, x_head_stride, tokens, heads, head_dim, rot_dim, layout, dtype, positions, freqs, amplitude, y,
                      y_token_stride, y_head_stride, "x", "y");
         if (c.rc != NEO_OK || tokens == 0) return c.rc;
@@ -409,15 +409,22 @@ int neo_attention_shared_int8(const neo_kv_cache* cache, const void* q, int64_t 
                      page_table, context_lens, q_starts, tokens, q_heads, seqs, std::min(max_chunk, tokens), max_context,
                      window, scale};
         own.group_starts = group_starts, own.prefix_lens = prefix_lens, own.all_seqs = seqs;
-        own.max_own = std::min(max_own, max_context);
+        own.max_own = max_own ? std::min(max_own, max_context) : max_context;
         AttnArgs shared = own;
         shared.seqs = groups, shared.max_chunk = std::max(1, std::min(max_group, tokens));
         if ((int64_t)own.max_chunk * q_heads > (1 << 28) / seqs || (int64_t)shared.max_chunk * q_heads > (1 << 28) / groups)
             return c.bad(NEO_ERR_UNSUPPORTED, "max_chunk * q_heads * seqs or max_group * q_heads * groups above 2^28"), c.rc;
+        Workspace ws;
+        if (!attention_worth_sharing(shared, own, max_context - std::min(max_own, max_context))) {
+            if (const size_t need = attention_workspace(own)) {
+                const int rc = stream_workspace(c.fn, (hipStream_t)stream, need, &ws);
+                if (rc != NEO_OK) return rc;
+            }
+            return c.launched(launch_attention(dtype, own, ws.ptr, (hipStream_t)stream));
+        }
         // the rows' parts of the shared tokens, how many each sequence shares, and behind them the shares' parts, of one launch
         // at a time
         const size_t rows = (size_t)tokens * q_heads, o = rows * cache->head_dim, lens = o + 2 * rows, parts = (lens + seqs + 3) / 4 * 4;
-        Workspace ws;
         const int rc = stream_workspace(c.fn, (hipStream_t)stream,
                                         (parts + std::max(attention_shared_floats(shared), attention_own_floats(own))) * sizeof(float), &ws);
         if (rc != NEO_OK) return rc;

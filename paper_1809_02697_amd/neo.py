@@ -880,12 +880,13 @@ def kv_compact(cache, page_table, bases, keep, keep_starts, max_keep, stream=Non
 
 
 def attention_shared_int8(cache, q, page_table, context_lens, q_starts, group_starts, prefix_lens, max_chunk, max_group,
-                          max_context, max_own=None, scale=None, window=0, out=None, stream=None):
+                          max_context, max_own=0, scale=None, window=0, out=None, stream=None):
     """attention_paged_int8 for sequences of which groups share their first tokens, which are then read
     once a group: sequences group_starts[g] .. group_starts[g + 1] - 1 (int32 [groups + 1]) share the
     first prefix_lens[g] (int32 [groups]), found in the first one's page table.  max_group: a group's
     new tokens at most (one with more is not taken together); max_own: a sequence's cached tokens behind
-    the shared ones at most (max_context unless given), which the work is laid out for."""
+    the shared ones at most (0: not known), which the work is laid out for.  Every sequence's
+    own table has the shared tokens too: calls that would save too little read them there."""
     t = q.dtype
     code = _dtype(t)
     i32 = _DTYPES["i32"]
@@ -905,7 +906,7 @@ def attention_shared_int8(cache, q, page_table, context_lens, q_starts, group_st
     _check(lib().neo_attention_shared_int8(ctypes.byref(c), qp, qt, qh, T, Hq, code, tp, ts,
                                            _vec(context_lens, B, i32, "context_lens"), _vec(q_starts, B + 1, i32, "q_starts"), B,
                                            _vec(group_starts, groups + 1, i32, "group_starts"), _vec(prefix_lens, groups, i32, "prefix_lens"),
-                                           groups, max_chunk, max_group, max_context, max_context if max_own is None else max_own,
+                                           groups, max_chunk, max_group, max_context, max_own,
                                            D ** -0.5 if scale is None else scale, window, op, ot, oh, _stream(stream)))
     return out
 

@@ -93,7 +93,7 @@ ROTARY_BAD = [(dict(rot=0), -2), (dict(rot=3), -2), (dict(rot=66), -2), (dict(la
 def test_rotary_refusals():
     def call(x=FAKE, xt=256, xh=64, T=3, H=4, D=64, rot=64, layout=0, dtype=F16, pos=FAKE, freqs=FAKE, amp=1.0, y=OTHER, yt=256, yh=64):
         return neo.lib().neo_rotary(x, xt, xh, T, H, D, rot, layout, dtype, pos, freqs, amp, y, yt, yh, None)
-    for over, code in ROTARY_BAD + [(dict(D=0), -1), (dict(D=65537, yh=65537, yt=1 << 20), -4), (dict(H=1 << 23), -4)]:
+    for over, code in ROTARY_BAD + [(dict(D=0), -1), (dict(D=1025, yh=1025, yt=1 << 20), -4), (dict(H=1 << 23), -4)]:
         assert call(**over) == code and "neo_rotary" in neo.last_error(), over
     assert call(y=FAKE, yt=512) == -2 and "in place" in neo.last_error()
     assert call(y=FAKE, xh=0) == -2 and "in place" in neo.last_error()     # heads read from one place, written in place
@@ -474,15 +474,31 @@ def _most(groups):
     return max(sum(n for n, _ in s) for _, s in groups)
 
 
-def _attend(torch, dtype, groups, Hq, H, D, page, window=0, seed=0, spread=1.0, max_group=None, max_own=None):
+def _wide(table, groups, H, D, page, max_own=0):
+    """A page table, and a bound of the contexts, so wide that sharing seems worth its launches
+    however short the tokens are (what it saves is told by the bounds)."""
+    more = len(table) - len(groups)
+    if more == 0:
+        return table, None
+    most = int(210e6 / (more * H * (2 * D + 8))) + max_own + page
+    out = np.full((len(table), max(-(-most // page), table.shape[1])), 1 << 30, np.int32)
+    out[:, :table.shape[1]] = table
+    return out, most
+
+
+def _attend(torch, dtype, groups, Hq, H, D, page, window=0, seed=0, spread=1.0, max_group=None, max_own=0, force=True):
     k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, H, D, page, seed)
     starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
     q = _rand(torch, (int(starts[-1]), Hq, D), dtype, seed + 1, spread)
     scale = D ** -0.5
     ref, A, B = _attention64(q.double().numpy(), k, v, ks, vs, table, contexts, starts, scale, window)
-    run = lambda: neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q.cuda(), cuda(table), cuda(np.array(contexts, np.int32)),  # noqa: E731
-                                            cuda(starts), cuda(first), cuda(prefix), max(chunks), _most(groups) if max_group is None else max_group,
-                                            max(contexts), max_own, scale=scale, window=window)
+    most = None
+    if force:
+        table, most = _wide(table, groups, H, D, page, max_own)
+    cache, tab, ctx = (cuda(k), cuda(v), cuda(ks), cuda(vs)), cuda(table), cuda(np.array(contexts, np.int32))
+    run = lambda: neo.attention_shared_int8(cache, q.cuda(), tab, ctx, cuda(starts), cuda(first), cuda(prefix), max(chunks),  # noqa: E731
+                                            _most(groups) if max_group is None else max_group, max(most or 0, *contexts), max_own,
+                                            scale=scale, window=window)
     got = run()
     err = np.abs(_np(got) - ref)
     bound = _attention_bound(ref, A, B, D, max(contexts), dtype) + 16 * u * A
@@ -518,6 +534,30 @@ def test_shared_attention(torch, case, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("case", range(len(SHARED)))
+def test_shared_attention_that_saves_little(torch, case):
+    """The same with the bounds as they are: too little to share."""
+    groups, Hq, H, D, page, window = SHARED[case]
+    _attend(torch, "bfloat16", groups, Hq, H, D, page, window, seed=case, force=False)
+
+
+WHOLE = [  # so many short sequences that neither launch cuts its work: groups, q heads, kv heads, head dim, page, max_own
+    ([(900, [(1, 20), (1, 1), (1, 60)])] * 25 + [(1, [(1, 5)] * 45)], 16, 8, 64, 16, 60),
+    ([(150, [(1, 50)] * 12)] * 9, 64, 16, 256, 10, 50),
+    ([(240, [(3, 9)] * 30)] * 4, 32, 16, 128, 16, 0),
+    ([(700, [(1, 40), (1, 300)] * 70)] * 1, 8, 8, 128, 16, 300),     # (a wave takes a sequence's head alone)
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(WHOLE)))
+def test_shared_attention_of_whole_units(torch, case, dtype):
+    groups, Hq, H, D, page, own = WHOLE[case]
+    _attend(torch, dtype, groups, Hq, H, D, page, seed=80 + case, max_own=own, force=case == 3)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("spread", [1e-4, 30.0])
 def test_shared_attention_flat_and_sharp(torch, dtype, spread):
@@ -532,7 +572,7 @@ def test_groups_beyond_the_bound_read_for_themselves(torch, max_group):
 
 
 @gpu
-@pytest.mark.parametrize("max_own", [0, 40, 1300])
+@pytest.mark.parametrize("max_own", [0, 1, 40, 1300])
 def test_the_layout_of_the_work_changes_no_more_than_rounding(torch, max_own):
     """max_own below what the sequences have, as tight as it may be, and above."""
     _attend(torch, "float16", [(150, [(1, 30), (5, 40)]), (0, [(4, 1200)]), (90, [(2, 7)])], 4, 2, 64, 16, seed=61, max_own=max_own)
@@ -556,8 +596,9 @@ def test_shared_rows_that_see_nothing(torch, new):
     starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
     q = _rand(torch, (int(starts[-1]), 4, 64), "float16", 65)
     q[new, 1, 5] = math.inf                 # (a query that sees nothing is zeros whatever it holds)
-    got = _np(neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q.cuda(), cuda(table), cuda(np.array(contexts, np.int32)),
-                                        cuda(starts), cuda(first), cuda(prefix), new, 2 * new, max(contexts), scale=0.125))
+    wide, most = _wide(table, groups, 2, 64, 4)
+    got = _np(neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q.cuda(), cuda(wide), cuda(np.array(contexts, np.int32)),
+                                        cuda(starts), cuda(first), cuda(prefix), new, 2 * new, most, scale=0.125))
     assert (got[new:new + 3] == 0).all() and (got[2 * new:2 * new + 2] == 0).all()
     q[new, 1, 5] = 0
     for b in range(3):
@@ -588,8 +629,9 @@ def test_shared_bad_entries_and_queries(torch, new):
     k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, 1, 64, 16, 66)
     starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
     q = _rand(torch, (int(starts[-1]), 2, 64), "bfloat16", 67).cuda()
-    run = lambda q: neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q, cuda(table), cuda(np.array(contexts, np.int32)),  # noqa: E731
-                                              cuda(starts), cuda(first), cuda(prefix), new, 2 * new, max(contexts))
+    wide, most = _wide(table, groups, 1, 64, 16)
+    run = lambda q: neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q, cuda(wide), cuda(np.array(contexts, np.int32)),  # noqa: E731
+                                              cuda(starts), cuda(first), cuda(prefix), new, 2 * new, most)
     good = run(q)
     at = table[1, 110 // 16], 0, 110 % 16
     for s in (ks, vs):
@@ -614,7 +656,8 @@ def test_shared_attention_strides(torch):
     groups = [(90, [(3, 30), (2, 40)])]
     k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, 2, 64, 16, 68)
     q = _rand(torch, (5, 9, 80), "float16", 69).cuda()
-    rest = (cuda(np.array(contexts, np.int32)), cuda(np.array([0, 3, 5], np.int32)), cuda(first), cuda(prefix), 3, 5, max(contexts))
+    table, most = _wide(table, groups, 2, 64, 16)
+    rest = (cuda(np.array(contexts, np.int32)), cuda(np.array([0, 3, 5], np.int32)), cuda(first), cuda(prefix), 3, 5, most)
     cache = cuda(k), cuda(v), cuda(ks), cuda(vs)
     want = neo.attention_shared_int8(cache, q[:, 3:7, 8:72].contiguous(), cuda(table), *rest)
     out = torch.full((5, 6, 70), 3.0, device="cuda", dtype=torch.float16)
@@ -666,8 +709,9 @@ def test_a_forked_prompt(torch):
     neo.kv_compact(mine, _i32(torch, pages), _i32(torch, [T] * 3), _i32(torch, kept * 3), _i32(torch, [0, 5, 10, 15]), 5)
     q = _rand(torch, (3, G * H, D), "bfloat16", 99).cuda()
     ctx, starts = _i32(torch, [T + 5] * 3), _i32(torch, [0, 1, 2, 3])
+    wide, most = _wide(np.array(pages, np.int32), [(T, [(1, 5)] * 3)], H, D, page, 5)
     for layer in range(L):
-        one = neo.attention_shared_int8(neo.kv_layer(mine, layer), q, _i32(torch, pages), ctx, starts, _i32(torch, [0, 3]), _i32(torch, [T]), 1, 3, T + 5, 5)
+        one = neo.attention_shared_int8(neo.kv_layer(mine, layer), q, cuda(wide), ctx, starts, _i32(torch, [0, 3]), _i32(torch, [T]), 1, 3, most, 5)
         two = neo.attention_paged_int8(neo.kv_layer(apart, layer), q, _i32(torch, alone), ctx, starts, 1, T + 5)
         # both round the output (2^-8) and the weights (2^-11, and less than 2^-12 for what float32 does, of values up to top)
         top = max(t.abs().max() for t in neo.kv_read_int8(neo.kv_layer(apart, layer), torch.arange(40 * page, device="cuda"), torch.float32)[1:])
@@ -689,17 +733,18 @@ def test_graph_of_all(torch):
     P, T = k.shape[0], 8
     qkv = _rand(torch, (T, 12, 128), "bfloat16", 72).cuda()
     q, kn, vn = qkv.split([8, 2, 2], 1)
+    table, most = _wide(table, groups, 2, 128, 16)
     tab, ctx, starts, fs, pl = (cuda(a) for a in (table, np.array(contexts, np.int32), np.arange(T + 1, dtype=np.int32), first, prefix))
     slots = torch.tensor([int(table[b, (c - 1) // 16]) * 16 + (c - 1) % 16 for b, c in enumerate(contexts)], device="cuda")
     pos, f = (ctx - 1).long(), neo.rotary_frequencies(128)
-    free = [p for p in range(P) if p not in set(table.flatten().tolist())][:2]
+    free = [p for p in range(P) if p not in set(table[table < P].tolist())][:2]
     src, dst = _i32(torch, [int(table[0, 0]), int(table[6, 0])]), _i32(torch, free)
     bases, keep, ksts = _i32(torch, [c - 3 for c in contexts]), _i32(torch, [x for c in contexts for x in (c - 2, c - 1)]), _i32(torch, list(range(0, 17, 2)))
     q_out, out = torch.empty(T, 8, 128, device="cuda", dtype=torch.bfloat16), torch.empty(T, 8, 128, device="cuda", dtype=torch.bfloat16)
 
     def step():
         neo.rotary_kv_write_int8(cache, q, kn, vn, slots, pos, f, q_out=q_out)
-        neo.attention_shared_int8(cache, q_out, tab, ctx, starts, fs, pl, 1, 6, max(contexts), out=out)
+        neo.attention_shared_int8(cache, q_out, tab, ctx, starts, fs, pl, 1, 6, most, out=out)
         neo.kv_copy_pages(cache, src, dst)
         neo.kv_compact(cache, tab, bases, keep, ksts, 2)
 
@@ -724,7 +769,7 @@ def test_graph_of_all(torch):
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip([*cache, out, q_out], want)), i
             if i == 1:                      # a larger call of the stream, and what it computes, between
-                neo.attention_shared_int8(cache, q_out.repeat(4, 1, 1), tab, ctx, starts * 4, fs, pl, 4, 24, max(contexts))
+                neo.attention_shared_int8(cache, q_out.repeat(4, 1, 1), tab, ctx, starts * 4, fs, pl, 4, 24, most)
                 torch.cuda.synchronize()
 
 
@@ -735,9 +780,10 @@ def test_two_streams(torch):
     for i, groups in enumerate(([(2000, [(1, 60)] * 9)], [(900, [(20, 90)] * 4)])):
         k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, 2, 128, 16, 73 + i)
         starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+        table, most = _wide(table, groups, 2, 128, 16)
         q = _rand(torch, (int(starts[-1]), 8, 128), "bfloat16", 75 + i).cuda()
         args = ((cuda(k), cuda(v), cuda(ks), cuda(vs)), q, cuda(table), cuda(np.array(contexts, np.int32)), cuda(starts), cuda(first), cuda(prefix),
-                max(chunks), _most(groups), max(contexts))
+                max(chunks), _most(groups), most)
         calls.append(lambda args=args, **kw: neo.attention_shared_int8(*args, **kw))
     want = [c() for c in calls]
     torch.cuda.synchronize()
