@@ -15,7 +15,13 @@ per token, keys and values int8 in a paged cache):
 
 ``Decoder.step`` takes any number of new tokens of each sequence: whole
 prompts, chunks of them, or one token each.  Positions enter through the causal
-order alone.
+order alone, or with ``freqs`` through rotary positions, queries and keys turned on
+their way to the attention and the cache (rotary_kv_write_int8).
+
+Sequences may share pages: ``fork`` gives copies of a sequence that hold its whole
+pages in common and a copy of the last one, and a step reads what neighbours
+share once for all of them (attention_shared_int8).  ``keep`` drops tokens of a
+sequence and closes up the others, ``drop`` gives its pages back.
 
     python -m paper_1809_02697_amd.decoder      # a small decoder: prompts, then tokens
 """
@@ -52,8 +58,15 @@ class Layer:
         h = x if h2 is None else h2
         qkv = self.qkv(q8, s, dtype).view(T, self.q_heads + 2 * self.kv_heads, D)
         q, k, v = qkv.split([self.q_heads, self.kv_heads, self.kv_heads], 1)
-        neo.kv_write_int8(cache, k, v, step.slots)
-        a = neo.attention_paged_int8(cache, q, step.table, step.contexts, step.starts, step.max_chunk, step.max_context)
+        if step.rotary is None:
+            neo.kv_write_int8(cache, k, v, step.slots)
+        else:
+            q = neo.rotary_kv_write_int8(cache, q, k, v, step.slots, step.positions, **step.rotary, q_out=q)
+        if step.prefix_lens is None:
+            a = neo.attention_paged_int8(cache, q, step.table, step.contexts, step.starts, step.max_chunk, step.max_context)
+        else:
+            a = neo.attention_shared_int8(cache, q, step.table, step.contexts, step.starts, step.group_starts, step.prefix_lens,
+                                          step.max_chunk, step.max_group, step.max_context, step.max_own)
         x = self.out(*neo.quantize_tokens_int8(a.view(T, self.q_heads * D)), dtype)
         q8, s, h = neo.rmsnorm_int8(x, self.norm2, residual=h)
         both = self.gate_up(q8, s, dtype)
@@ -62,9 +75,11 @@ class Layer:
 
 
 class Step:
-    """Where one call's tokens stand: cache slots of the new ones, page table, lengths."""
+    """Where one call's tokens stand: cache slots of the new ones, page table, lengths; with groups
+    (their starts and shared tokens, from ``shared_pages``) what neighbouring sequences have in common,
+    with rotary (freqs, layout, amplitude) the new tokens' positions."""
 
-    def __init__(self, pages, lengths, new, page_size, device):
+    def __init__(self, pages, lengths, new, page_size, device, groups=None, rotary=None, positions=None):
         slots, contexts = [], []
         for p, n, m in zip(pages, lengths, new):
             slots += [p[t // page_size] * page_size + t % page_size for t in range(n, n + m)]
@@ -77,27 +92,118 @@ class Step:
         ints = lambda v, t=torch.int32: torch.tensor(v, dtype=t, device=device)  # noqa: E731
         self.slots, self.table, self.contexts, self.starts = ints(slots, torch.int64), ints(table), ints(contexts), ints(starts)
         self.max_chunk, self.max_context = max(new), max(contexts)
-        self.last = ints([s - 1 for s, m in zip(starts[1:], new) if m], torch.int64)
+        self.ends = [s - 1 for s in starts[1:]]
+        self.last = ints([s for s, m in zip(self.ends, new) if m], torch.int64)
+        self.rotary = rotary
+        self.positions = None if rotary is None else ints(positions, torch.int64)
+        self.prefix_lens = None
+        if groups:
+            first, prefix = groups
+            self.group_starts, self.prefix_lens = ints(first), ints(prefix)
+            self.max_group = max(starts[b] - starts[a] for a, b in zip(first, first[1:]))
+            self.max_own = max(c - p for a, b, p in zip(first, first[1:], prefix) for c in contexts[a:b])
+
+
+def shared_pages(pages, page_size):
+    """Of sequences in the order of their pages: groups that begin with the same ones, as (starts of the groups
+    and the number of sequences, tokens that each group's sequences have in common); None if none do."""
+    first, prefix = [], []
+    for i, p in enumerate(pages):
+        if i and p and pages[i - 1] and p[0] == pages[i - 1][0]:
+            n = next((j for j, (a, b) in enumerate(zip(p, pages[first[-1]])) if a != b), min(len(p), len(pages[first[-1]])))
+            prefix[-1] = min(n * page_size, prefix[-1] or n * page_size)
+        else:
+            first.append(i)
+            prefix.append(0)
+    return (first + [len(pages)], prefix) if any(prefix) else None
 
 
 class Decoder:
     """weights: {"embed": [vocab][width], "norm": [width], "head": [vocab][width],
-    "layers": [{"norm1", "qkv", "out", "norm2", "gate_up", "down"}, ...]}, float32 on the device."""
+    "layers": [{"norm1", "qkv", "out", "norm2", "gate_up", "down"}, ...]}, float32 on the device.
+    freqs, layout, amplitude: rotary positions (neo.rotary), none without freqs."""
 
-    def __init__(self, weights, q_heads, kv_heads, head_dim, pages, page_size=64, dtype=torch.bfloat16):
+    def __init__(self, weights, q_heads, kv_heads, head_dim, pages, page_size=64, dtype=torch.bfloat16, freqs=None, layout="half",
+                 amplitude=1.0):
         self.embed, self.norm, self.head = weights["embed"].to(dtype), weights["norm"], Linear(weights["head"])
         self.layers = [Layer(w, q_heads, kv_heads, head_dim) for w in weights["layers"]]
         device = weights["embed"].device
-        self.caches = [neo.kv_cache(pages, kv_heads, page_size, head_dim, device) for _ in self.layers]
+        self.cache = neo.kv_cache(pages, kv_heads, page_size, head_dim, device, layers=len(self.layers))
+        self.caches = [neo.kv_layer(self.cache, i) for i in range(len(self.layers))]
+        self.rotary = None if freqs is None else dict(freqs=freqs, layout=layout, amplitude=amplitude)
         self.page_size, self.dtype, self.device = page_size, dtype, device
         self.free = list(range(pages))[::-1]
-        self.pages, self.lengths = [], []
+        self.users = [0] * pages                   # sequences that hold a page
+        self.pages, self.lengths, self.at = [], [], []  # of a sequence: pages, tokens, the tokens' positions
 
     def add(self):
         """A new, empty sequence; its number."""
         self.pages.append([])
         self.lengths.append(0)
+        self.at.append([])
         return len(self.pages) - 1
+
+    def _take(self):
+        page = self.free.pop()
+        self.users[page] = 1
+        return page
+
+    def _release(self, pages):
+        for page in pages:
+            self.users[page] -= 1
+            if self.users[page] == 0:
+                self.free.append(page)
+
+    def _copy(self, src, dst, entries=None):
+        if src:
+            ints = lambda v: torch.tensor(v, dtype=torch.int32, device=self.device)  # noqa: E731
+            neo.kv_copy_pages(self.cache, ints(src), ints(dst), None if entries is None else ints(entries))
+
+    def fork(self, sequence, copies=1):
+        """Sequences that go on from where this one is; their numbers.  Its whole pages are shared, what
+        is on the last one is copied."""
+        whole, rest = divmod(self.lengths[sequence], self.page_size)
+        if rest and copies > len(self.free):
+            raise RuntimeError("the cache has no page left")
+        new = [self._take() for _ in range(copies)] if rest else []
+        if rest:
+            self._copy([self.pages[sequence][whole]] * copies, new, [rest] * copies)
+        for i in range(copies):
+            for page in self.pages[sequence][:whole]:
+                self.users[page] += 1
+            self.pages.append(self.pages[sequence][:whole] + new[i:i + 1])
+            self.lengths.append(self.lengths[sequence])
+            self.at.append(list(self.at[sequence]))
+        return list(range(len(self.pages) - copies, len(self.pages)))
+
+    def drop(self, sequence):
+        """Gives a sequence's pages back; its number stays, for an empty one."""
+        self._release(self.pages[sequence])
+        self.pages[sequence], self.lengths[sequence], self.at[sequence] = [], 0, []
+
+    def keep(self, sequence, tokens):
+        """Drops a sequence's cached tokens but these (their places, ascending), which close up and stay as
+        they are, turned for the positions that they had; the next token's follows the last one's."""
+        tokens, pages, size = list(tokens), self.pages[sequence], self.page_size
+        if not all(a < b for a, b in zip([-1] + tokens, tokens + [self.lengths[sequence]])):
+            raise ValueError("tokens must be places of cached tokens, ascending")
+        base = next((i for i, t in enumerate(tokens) if i != t), len(tokens))
+        end = -(-len(tokens) // size)
+        # pages that others hold too are written in a copy
+        copied = [i for i in range(base // size, end) if self.users[pages[i]] > 1] if base < len(tokens) else []
+        if len(copied) > len(self.free):
+            raise RuntimeError("the cache has no page left")
+        new = [self._take() for _ in copied]
+        self._copy([pages[i] for i in copied], new)
+        self._release(pages[i] for i in copied)
+        for i, page in zip(copied, new):
+            pages[i] = page
+        if base < len(tokens):
+            ints = lambda v: torch.tensor(v, dtype=torch.int32, device=self.device)  # noqa: E731
+            neo.kv_compact(self.cache, ints([pages]), ints([base]), ints(tokens[base:]), ints([0, len(tokens) - base]), len(tokens) - base)
+        self._release(pages[end:])
+        self.pages[sequence], self.lengths[sequence] = pages[:end], len(tokens)
+        self.at[sequence] = [self.at[sequence][t] for t in tokens]
 
     def step(self, tokens):
         """tokens: for every sequence the list of its new tokens (maybe empty).  Returns the
@@ -108,18 +214,40 @@ class Decoder:
             raise ValueError("one list of tokens a sequence, and at least one token")
         if not all(0 <= t < len(self.embed) for s in tokens for t in s):  # (looked up on the device it ends the process)
             raise ValueError(f"a token outside the vocabulary of {len(self.embed)}")
-        need = [-(-(n + m) // self.page_size) - len(p) for p, n, m in zip(self.pages, self.lengths, new)]
-        if sum(need) > len(self.free):
+        size = self.page_size
+        need = [-(-(n + m) // size) - len(p) for p, n, m in zip(self.pages, self.lengths, new)]
+        # a page that is not full is written in a copy if others hold it too
+        copied = [i for i, (p, n, m) in enumerate(zip(self.pages, self.lengths, new)) if m and n % size and self.users[p[n // size]] > 1]
+        if sum(need) + len(copied) > len(self.free):
             raise RuntimeError("the cache has no page left")
+        shared = [self.pages[i][self.lengths[i] // size] for i in copied]
+        for i in copied:
+            self.pages[i][self.lengths[i] // size] = self._take()
+        self._copy(shared, [self.pages[i][self.lengths[i] // size] for i in copied])
+        self._release(shared)
         for p, n in zip(self.pages, need):
-            p += [self.free.pop() for _ in range(n)]
-        step = Step(self.pages, self.lengths, new, self.page_size, self.device)
-        x = self.embed[torch.tensor([t for s in tokens for t in s], device=self.device)]
+            p += [self._take() for _ in range(n)]
+        # sequences that begin with the same pages side by side
+        order = list(range(len(new)))
+        groups = None
+        if any(n > 1 for n in self.users):
+            order.sort(key=self.pages.__getitem__)
+            groups = shared_pages([self.pages[i] for i in order], size)
+        places = [range(a[-1] + 1 if a else 0, (a[-1] + 1 if a else 0) + m) for a, m in zip(self.at, new)]
+        step = Step([self.pages[i] for i in order], [self.lengths[i] for i in order], [new[i] for i in order], size, self.device,
+                    groups, self.rotary, [t for i in order for t in places[i]])
+        x = self.embed[torch.tensor([t for i in order for t in tokens[i]], device=self.device)]
         h = None
         for layer, cache in zip(self.layers, self.caches):
             x, h = layer(x, h, cache, step)
         self.lengths = [n + m for n, m in zip(self.lengths, new)]
-        q8, s, _ = neo.rmsnorm_int8(x[step.last], self.norm, residual=h[step.last], h=False)
+        for a, p in zip(self.at, places):
+            a += p
+        last = step.last
+        if groups:
+            ends = dict(zip(order, step.ends))
+            last = torch.tensor([ends[i] for i, m in enumerate(new) if m], device=self.device)
+        q8, s, _ = neo.rmsnorm_int8(x[last], self.norm, residual=h[last], h=False)
         return self.head(q8, s, torch.float32)
 
 
@@ -136,7 +264,7 @@ def random_weights(layers, vocab, width, q_heads, kv_heads, head_dim, inner, see
 def main():
     import time
     shape = dict(q_heads=16, kv_heads=4, head_dim=128)
-    d = Decoder(random_weights(4, 8192, 2048, inner=8192, **shape), pages=256, **shape)
+    d = Decoder(random_weights(4, 8192, 2048, inner=8192, **shape), pages=256, freqs=neo.rotary_frequencies(128), **shape)
     g = torch.Generator().manual_seed(1)
     prompts = [torch.randint(8192, (n,), generator=g).tolist() for n in (700, 33, 1, 256)]
     for _ in prompts:
@@ -154,6 +282,14 @@ def main():
     print(f"32 tokens of each of 4 sequences in {(time.perf_counter() - t0) * 1e3:.1f} ms")
     for i, o in enumerate(out):
         print(f"sequence {i} ({len(prompts[i])} tokens of prompt):", *o[:12], "...")
+    forks = d.fork(0, 3)                                   # four ways on from the long prompt
+    logits = d.step([[tokens[0]], [], [], []] + [[t] for t in (1, 2, 3)])
+    for i, t in zip([0] + forks, logits.argmax(1).tolist()):
+        print(f"sequence {i} goes on with", t)
+    d.keep(forks[0], range(d.lengths[forks[0]] - 5))       # one goes back five tokens
+    for i in forks[1:]:
+        d.drop(i)
+    print("and from five tokens before:", d.step([[]] * 4 + [[5], [], []]).argmax(1).item())
 
 
 if __name__ == "__main__":
