@@ -413,7 +413,7 @@ struct Walk {
         if (threadIdx.x == 0) {
             int count = 0;
             const int64_t x0 = x - c.skip;  // of the unit
-            if (MODE != kAll && c.skip > 0 && x0 >= share_start(W, used, share - 1))
+            if (c.skip > 0 && x0 >= share_start(W, used, share - 1))
                 count = (int)(((x0 + c.blocks) * used + W - 1) / W) - share + 1;  // (share i starts before y if i < y used / W)
             ws.starts[share] = Start{W, c.b, c.h, c.tile, c.skip, c.blocks, count};
         }
@@ -470,8 +470,8 @@ __device__ inline void write_shared(const AttnArgs& a) {
 // the whole wave; other pages are looked up key by key.
 //
 // The cache, read once, bounds it: one token each of 32 sequences, 32 query
-// heads on 8 of 128, contexts up to 32,000 (650 MB) 124 us, 5.2 TB/s, and 8 us
-// to join.
+// heads on 8 of 128, contexts up to 32,000 (650 MB) 127 us with the join of the
+// shares' parts, 5.1 TB/s.
 constexpr int kRowsWaves = 4;
 
 template <int DP>
@@ -560,6 +560,7 @@ template <typename T, int DP, bool TILED, int MODE, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void attention_rows(AttnArgs a, Shares sp, Parts ws) {
     typedef Weights<T> W;
     constexpr int KB = DP / 4, STEPS = DP / 32, VB = DP / 16;
+    constexpr bool AHEAD = WAVES == kRowsWaves;  // the next block is on its way while one is used
     constexpr int kRowsBlock = WAVES * 32;  // keys the workgroup takes at a time
     __shared__ float red_m[WAVES][16], red_l[WAVES][16], red_o[WAVES][16][DP + 4];
     __shared__ typename Cursor<16, kRowsBlock, MODE>::Scratch scratch;
@@ -580,8 +581,10 @@ __global__ __launch_bounds__(WAVES * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void 
         KeyPages<TILED> pages;
         if (hi > 0) {
             look_up<TILED>(sp, table, kb, hi, li, g, pages);
-            load_block<DP, TILED>(a, sp, pages, h, kb, hi, li, g, kv);
-            look_up<TILED>(sp, table, kb + kRowsBlock, hi, li, g, pages);
+            if constexpr (AHEAD) {
+                load_block<DP, TILED>(a, sp, pages, h, kb, hi, li, g, kv);
+                look_up<TILED>(sp, table, kb + kRowsBlock, hi, li, g, pages);
+            }
         }
 
         // this lane's row of queries: values d = g * KB + ...
@@ -632,8 +635,13 @@ __global__ __launch_bounds__(WAVES * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void 
         while (kb < last) {
             const int kn = kb + kRowsBlock;
             KeyBlock<DP> next;
-            load_block<DP, TILED>(a, sp, pages, h, kn, hi, li, g, next);
-            look_up<TILED>(sp, table, kn + kRowsBlock, hi, li, g, pages);
+            if constexpr (AHEAD) {
+                load_block<DP, TILED>(a, sp, pages, h, kn, hi, li, g, next);
+                look_up<TILED>(sp, table, kn + kRowsBlock, hi, li, g, pages);
+            } else {
+                load_block<DP, TILED>(a, sp, pages, h, kb, hi, li, g, kv);
+                look_up<TILED>(sp, table, kn, hi, li, g, pages);
+            }
 
             v4f s[2];
 #pragma unroll
@@ -741,7 +749,7 @@ __global__ __launch_bounds__(WAVES * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void 
 #pragma unroll
                 for (int i = 0; i < W::TERMS; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i], o[t], 0, 0, 0);
             }
-            kv = next;
+            if constexpr (AHEAD) kv = next;
             kb = kn;
         }
         l += __shfl_xor(l, 16, 64);
@@ -1185,78 +1193,11 @@ __global__ __launch_bounds__(NW * 64) void attention_tile(AttnArgs a, Shares sp,
 }
 
 // The parts of the unit in which share j starts, if it is the first to start in
-// it: workgroup (j - 1, y) joins ROUNDS times four rows of the tile, a wave a
-// row, or with WAVES = 4 row y, its waves taking the parts in turn.
-template <typename T, int ROWS, int WAVES, int ROUNDS>
-__global__ __launch_bounds__(256) void attention_join(AttnArgs a, Shares sh, Parts ws) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turn = wave % WAVES;
-    const int G = a.q_heads / a.c.kv_heads, D = a.c.head_dim, j = blockIdx.x + 1;
-    const Start at = ws.starts[j];
-    if (at.W == 0 || at.skip == 0) return;
-    const int64_t W = at.W;
-    const int used = sh.used(W);
-    const int64_t x0 = share_start(W, used, j) - at.skip;
-    if (x0 < share_start(W, used, j - 1)) return;
-    // parts: the end of share j - 1, the starts of shares j .. j + count - 2
-    int count = 2;
-    while (j + count - 1 < used && share_start(W, used, j + count - 1) < x0 + at.blocks) ++count;
-    const Unit u = unit_of<kAll>(a, at.b);
-    static_assert(WAVES == 1 || ROUNDS == 1, "");
-#pragma unroll 1
-    for (int round = 0; round < ROUNDS; ++round) {
-        const int rr = (blockIdx.y * ROUNDS + round) * (4 / WAVES) + wave / WAVES, row = at.tile * ROWS + rr;
-        if (row >= u.n * G) return;  // (with four waves a row: all of them)
-        auto part = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0)) * ROWS + rr; };
-        float M = kMinusInf, L = 0.f;
-        for (int i = lane; i < count; i += 64) M = fmaxf(M, ws.ml[part(i)].x);
-#pragma unroll
-        for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
-        auto factor = [&](float m) { return part_factor(m, M); };
-        for (int i = lane; i < count; i += 64) L += ws.ml[part(i)].y * factor(ws.ml[part(i)].x);
-        L = lanes_sum(L);
-        float v[4] = {0, 0, 0, 0};
-        for (int i0 = 0; i0 < count; i0 += 64 * WAVES) {
-            const int mine = i0 + lane * WAVES + turn;  // this lane's part
-            const float f = mine < count ? factor(ws.ml[part(mine)].x) : 0.f;
-            const int parts = min(64, (count - i0 - turn + WAVES - 1) / WAVES);
-            for (int i = 0; i < parts; i += 4) {  // (past the last: the last, not added)
-                float w[4][4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        w[y][x] = ws.o[part(i0 + min(i + y, parts - 1) * WAVES + turn) * D + min(lane + 64 * x, D - 1)];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const float fi = __shfl(f, min(i + y, 63), 64);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) v[x] += i + y < parts ? w[y][x] * fi : 0.f;
-                }
-            }
-        }
-        if constexpr (WAVES > 1) {
-            __shared__ float red[WAVES][256];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) red[turn][lane + 64 * x] = v[x];
-            __syncthreads();
-            if (turn) return;
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) v[x] += red[w][lane + 64 * x];
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-            if (lane + 64 * x < D) finish<T, kAll>(a, u, at.h, G, row, lane + 64 * x, v[x], M, L);
-    }
-}
-
-// The same for the other modes: DP / 4 lanes take a row, four columns each, and
-// SPLIT such groups its parts in turn.  What attention_join works out from the
-// shares' starts (64-bit divisions, which bound it where units have few parts)
-// stands in them.
+// the middle of it: DP / 4 lanes take a row of the tile, four columns each, and SPLIT
+// such groups its parts in turn.  256 shares of tiles of 256 rows, 34 MB of parts: 10
+// us (in units of eight parts) to 14 (of two).
 template <typename T, int DP, int ROWS, int SPLIT, int MODE>
-__global__ __launch_bounds__(256) void attention_join_parts(AttnArgs a, Parts ws) {
+__global__ __launch_bounds__(256) void attention_join(AttnArgs a, Parts ws) {
     constexpr int LW = DP / 4, GROUPS = 256 / LW, EACH = GROUPS / SPLIT;
     const int lane = threadIdx.x % LW, group = threadIdx.x / LW, turn = group % SPLIT;
     const int G = a.q_heads / a.c.kv_heads, D = a.c.head_dim, j = blockIdx.x + 1;
@@ -1298,19 +1239,20 @@ __global__ __launch_bounds__(256) void attention_join_parts(AttnArgs a, Parts ws
     if (lane * 4 >= D) return;
     const int t = row / G, hq = at.h * G + row - t * G;
     const int64_t to = (int64_t)(u.first + t) * a.q_heads + hq;
-    v4f* shared = reinterpret_cast<v4f*>(a.part_o + to * D + lane * 4);
     if constexpr (MODE == kShared) {
-        *shared = v;
+        *reinterpret_cast<v4f*>(a.part_o + to * D + lane * 4) = v;
         if (lane == 0) a.part_ml[to] = make_float2(M, L);
-    } else {
+        return;
+    }
+    if constexpr (MODE == kOwn)
         if (u.from > 0) {
             const float2 ml = a.part_ml[to];
             const float top = fmaxf(M, ml.x), f = part_factor(M, top), g = part_factor(ml.x, top);
-            v = v * f + *shared * g;
+            v = v * f + *reinterpret_cast<const v4f*>(a.part_o + to * D + lane * 4) * g;
             L = L * f + ml.y * g;
         }
-        store4(static_cast<T*>(a.out) + (int64_t)(u.first + t) * a.ots + (int64_t)hq * a.ohs + lane * 4, v * (L == 0.f ? 0.f : 1.f / L));
-    }
+    store4(static_cast<T*>(a.out) + (int64_t)(u.first + t) * a.ots + (int64_t)hq * a.ohs + lane * 4,
+           L == 0.f ? v4f{0, 0, 0, 0} : v4f{v[0] / L, v[1] / L, v[2] / L, v[3] / L});
 }
 
 // Rows a workgroup takes.  Up to two tiles of 16 go to the kernel for few rows
@@ -1371,18 +1313,15 @@ hipError_t launch_tile(const AttnArgs& a, const Shares& sh, const Parts& p, unsi
     hipLaunchKernelGGL((attention_tile<T, DP, NW, MODE>), dim3(blocks), dim3(NW * 64), C::BYTES, st, a, sh, p);
     e = hipGetLastError();
     if (e != hipSuccess || sh.groups < 2) return e;
-    if constexpr (MODE == kAll)
-        hipLaunchKernelGGL((attention_join<T, C::ROWS, 1, 4>), dim3(sh.groups - 1, C::ROWS / 16), dim3(256), 0, st, a, sh, p);
-    else
-        hipLaunchKernelGGL((attention_join_parts<T, DP, C::ROWS, 1, MODE>), dim3(sh.groups - 1, C::ROWS / (1024 / DP)), dim3(256), 0, st, a, p);
+    hipLaunchKernelGGL((attention_join<T, DP, C::ROWS, 1, MODE>), dim3(sh.groups - 1, C::ROWS / (1024 / DP)), dim3(256), 0, st, a, p);
     return hipGetLastError();
 }
 
-// From so many whole units on two waves take one, not four: more of them lie on the
-// chip at once, and what each waits for (its table, keys, values, its part of the
-// shared tokens) is waited for side by side.  Own tokens of 128 sequences and 8
-// heads, up to 500 each: a call 126 us, 138 with one wave; of 256 sequences 216,
-// 218 and with four 227.
+// From so many whole units on two waves take one, not four, and each loads a block
+// when it needs it: more units lie on the chip at once, and what each waits for (its
+// table, keys, values, its part of the shared tokens) is waited for side by side.
+// Own tokens of 256 sequences and 8 heads, up to 500 each: the call 216 us, 221 with
+// the next block on its way, 227 with four waves; of 128 sequences 127, 131, 138.
 constexpr int64_t kShortUnits = 1024;
 
 template <typename T, int DP, int MODE, int WAVES>
@@ -1411,11 +1350,8 @@ hipError_t launch_d(const AttnArgs& a, float* ws, hipStream_t st) {
         launch_rows<T, DP, MODE, kRowsWaves>(a, sh, p, blocks, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || sh.groups < 2) return e;
-    const unsigned rows = std::min(16, a.max_chunk * G);
-    if constexpr (MODE == kAll)
-        hipLaunchKernelGGL((attention_join<T, 16, 4, 1>), dim3(sh.groups - 1, rows), dim3(256), 0, st, a, sh, p);
-    else  // (a workgroup a row)
-        hipLaunchKernelGGL((attention_join_parts<T, DP, 16, 1024 / DP, MODE>), dim3(sh.groups - 1, rows), dim3(256), 0, st, a, p);
+    // (a workgroup a row)
+    hipLaunchKernelGGL((attention_join<T, DP, 16, 1024 / DP, MODE>), dim3(sh.groups - 1, std::min(16, a.max_chunk * G)), dim3(256), 0, st, a, p);
     return hipGetLastError();
 }
 

@@ -480,7 +480,7 @@ def _wide(table, groups, H, D, page, max_own=0):
     more = len(table) - len(groups)
     if more == 0:
         return table, None
-    most = int(210e6 / (more * H * (2 * D + 8))) + max_own + page
+    most = int(260e6 / (more * H * (2 * D + 8))) + max_own + page
     out = np.full((len(table), max(-(-most // page), table.shape[1])), 1 << 30, np.int32)
     out[:, :table.shape[1]] = table
     return out, most
@@ -542,10 +542,10 @@ def test_shared_attention_that_saves_little(torch, case):
 
 
 WHOLE = [  # so many short sequences that neither launch cuts its work: groups, q heads, kv heads, head dim, page, max_own
-    ([(900, [(1, 20), (1, 1), (1, 60)])] * 25 + [(1, [(1, 5)] * 45)], 16, 8, 64, 16, 60),
-    ([(150, [(1, 50)] * 12)] * 9, 64, 16, 256, 10, 50),
-    ([(240, [(3, 9)] * 30)] * 4, 32, 16, 128, 16, 0),
-    ([(700, [(1, 40), (1, 300)] * 70)] * 1, 8, 8, 128, 16, 300),     # (a wave takes a sequence's head alone)
+    ([(900, [(1, 20), (1, 1), (1, 60)])] * 42 + [(1, [(1, 5)] * 45)], 32, 16, 64, 16, 60),
+    ([(190, [(1, 50)] * 12)] * 17, 64, 16, 256, 10, 50),
+    ([(240, [(3, 9)] * 32)] * 4, 64, 32, 128, 16, 0),
+    ([(700, [(1, 40), (1, 300)] * 70)] * 1, 8, 8, 128, 16, 300),     # (two waves take a sequence's head)
 ]
 
 
