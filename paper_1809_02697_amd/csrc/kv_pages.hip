@@ -10,42 +10,60 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 // ---- copies -----------------------------------------------------------------------------
 // A page's keys (or values) in one layer are kv_heads stretches of page_size
-// entries, of which the first `n` are copied: pieces of 16 bytes, an entry's
-// scale with its first piece.  A workgroup takes kChunk pieces, four a thread,
-// all loaded before the first is stored.
+// entries, of which the first `n` are copied; whole pages are one stretch.  Pieces of
+// 16 bytes, four a thread, all loaded before the first is stored.  Nothing is read
+// again soon, so the stores (and where whole pages move, the loads) pass the caches
+// by: 256 pages of 64 tokens, 8 heads of 128, 16 layers (1.1 GB) 211 us (5.2 TB/s; 222
+// without); 256 tails of up to 64 tokens of one page 74 (83 without, and 136 with loads
+// that do so too).
 constexpr int kDepth = 4, kChunk = 256 * kDepth;
 
+template <bool WHOLE>
 __global__ __launch_bounds__(256) void kv_copy(CopyArgs a, int chunks, int64_t work) {
     const neo_kv_cache& c = a.c;
     const uint32_t each = (uint32_t)c.head_dim / 16, page = (uint32_t)(c.kv_heads * c.page_size);
     for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
         const int64_t q = w / chunks;
         const int chunk = (int)(w - q * chunks), of = (int)(q % (2 * a.layers)), pair = (int)(q / (2 * a.layers));
-        const int src = a.src[pair], dst = a.dst[pair], n = a.entries ? min(max(a.entries[pair], 0), c.page_size) : c.page_size;
+        const int src = a.src[pair], dst = a.dst[pair];
         if ((uint32_t)src >= (uint32_t)c.pages || (uint32_t)dst >= (uint32_t)c.pages || src == dst) continue;
-        const int64_t layer = (of >> 1) * a.layer_stride;
-        int8_t* data = (of & 1 ? c.v : c.k) + layer * c.head_dim;
-        float* scales = (of & 1 ? c.v_scale : c.k_scale) + layer;
-        const uint32_t row = (uint32_t)n * each, pieces = row * (uint32_t)c.kv_heads;
-        const int64_t from = (int64_t)src * page, to = (int64_t)dst * page;
+        const int64_t layer = (of >> 1) * a.layer_stride, from = layer + (int64_t)src * page, to = layer + (int64_t)dst * page;
+        int8_t* data = of & 1 ? c.v : c.k;
+        float* scales = of & 1 ? c.v_scale : c.k_scale;
+        const uint32_t start = (uint32_t)chunk * kChunk;
         u4 v[kDepth];
-        float s[kDepth];
-        uint32_t entry[kDepth], piece[kDepth];
+        if constexpr (WHOLE) {
+            const uint32_t pieces = page * each, end = min(start + kChunk, pieces);
+            const u4* x = reinterpret_cast<const u4*>(data + from * c.head_dim);
+            u4* y = reinterpret_cast<u4*>(data + to * c.head_dim);
 #pragma unroll
-        for (int i = 0; i < kDepth; ++i) {
-            const uint32_t x = (uint32_t)chunk * kChunk + i * 256 + threadIdx.x, h = n == c.page_size ? 0 : x / max(row, 1u), y = x - h * row;
-            const uint32_t o = y / each;
-            entry[i] = x < pieces ? h * (uint32_t)c.page_size + o : 0xffffffffu;
-            piece[i] = y - o * each;
-            if (x >= pieces) continue;
-            v[i] = *reinterpret_cast<const u4*>(data + (from + entry[i]) * c.head_dim + piece[i] * 16);
-            if (piece[i] == 0) s[i] = scales[from + entry[i]];
-        }
+            for (int i = 0; i < kDepth; ++i)
+                if (start + i * 256 + threadIdx.x < end) v[i] = __builtin_nontemporal_load(x + start + i * 256 + threadIdx.x);
+            // (the scales of the entries that start in the chunk)
+            for (uint32_t e = (start + each - 1) / each + threadIdx.x; e < (end + each - 1) / each; e += 256) scales[to + e] = scales[from + e];
 #pragma unroll
-        for (int i = 0; i < kDepth; ++i) {
-            if (entry[i] == 0xffffffffu) continue;
-            *reinterpret_cast<u4*>(data + (to + entry[i]) * c.head_dim + piece[i] * 16) = v[i];
-            if (piece[i] == 0) scales[to + entry[i]] = s[i];
+            for (int i = 0; i < kDepth; ++i)
+                if (start + i * 256 + threadIdx.x < end) __builtin_nontemporal_store(v[i], y + start + i * 256 + threadIdx.x);
+        } else {
+            const uint32_t row = (uint32_t)min(max(a.entries[pair], 0), c.page_size) * each, pieces = row * (uint32_t)c.kv_heads;
+            if (start >= pieces) continue;
+            float s[kDepth];
+            uint32_t entry[kDepth], piece[kDepth];
+#pragma unroll
+            for (int i = 0; i < kDepth; ++i) {
+                const uint32_t x = start + i * 256 + threadIdx.x, h = x / row, y = x - h * row, o = y / each;
+                entry[i] = x < pieces ? h * (uint32_t)c.page_size + o : 0xffffffffu;
+                piece[i] = y - o * each;
+                if (x >= pieces) continue;
+                v[i] = *reinterpret_cast<const u4*>(data + (from + entry[i]) * c.head_dim + piece[i] * 16);
+                if (piece[i] == 0) s[i] = scales[from + entry[i]];
+            }
+#pragma unroll
+            for (int i = 0; i < kDepth; ++i) {
+                if (entry[i] == 0xffffffffu) continue;
+                __builtin_nontemporal_store(v[i], reinterpret_cast<u4*>(data + (to + entry[i]) * c.head_dim + piece[i] * 16));
+                if (piece[i] == 0) scales[to + entry[i]] = s[i];
+            }
         }
     }
 }
@@ -58,8 +76,9 @@ __global__ __launch_bounds__(256) void kv_copy(CopyArgs a, int chunks, int64_t w
 // back, in every wave, before the first of its stores.  Four waves move bytes, the
 // next chunk's on their way while one is stored; a fifth looks up where the
 // tokens of the chunk after that lie.
-// (4 sequences of 6000 kept tokens of up to 12,064, 8 layers of 8 heads of 128: 166
-// us, 4.9 TB/s; with a chunk's loads waited for before the next one's 370.)
+// (4 sequences of 6000 kept tokens of up to 12,064, 8 layers of 8 heads of 128: 158
+// us, 5.1 TB/s; 178 with stores that stay in the caches, 370 with a chunk's loads waited
+// for before the next one's.)
 constexpr int kMovers = 256, kTokensMax = 256;
 
 struct Lines {  // entries of head 0, of a chunk's tokens; to < 0: nothing moves
@@ -185,7 +204,7 @@ __global__ __launch_bounds__(kMovers + 64) void kv_close_up(CompactArgs a, int t
 #pragma unroll
             for (int x = 0; x < kDepth; ++x) {
                 if (m.to[x] < 0) continue;
-                *reinterpret_cast<u4*>(data + m.to[x] * c.head_dim + byte[x]) = m.v[x];
+                __builtin_nontemporal_store(m.v[x], reinterpret_cast<u4*>(data + m.to[x] * c.head_dim + byte[x]));
                 if (byte[x] == 0) scales[m.to[x]] = m.s[x];
             }
         };
@@ -222,7 +241,11 @@ hipError_t launch_kv_copy(const CopyArgs& a, hipStream_t st) {
     const int64_t pieces = (int64_t)a.c.kv_heads * a.c.page_size * (a.c.head_dim / 16);
     const int chunks = (int)((pieces + kChunk - 1) / kChunk);
     const int64_t work = (int64_t)a.pairs * 2 * a.layers * chunks;
-    hipLaunchKernelGGL(kv_copy, dim3((unsigned)std::min(work, kBlocksMax)), dim3(256), 0, st, a, chunks, work);
+    const dim3 blocks((unsigned)std::min(work, kBlocksMax));
+    if (a.entries)
+        hipLaunchKernelGGL(kv_copy<false>, blocks, dim3(256), 0, st, a, chunks, work);
+    else
+        hipLaunchKernelGGL(kv_copy<true>, blocks, dim3(256), 0, st, a, chunks, work);
     return hipGetLastError();
 }
 

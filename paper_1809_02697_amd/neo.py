@@ -73,7 +73,7 @@ class KvCacheStruct(ctypes.Structure):
 
 
 _lib = None
-_RAW_STREAM = False  # set by lib(): torch hands out the current stream's raw handle
+_RAW_STREAM = None  # set by lib(): torch's calls for the current stream's raw handle and the current device
 
 
 def lib():
@@ -160,7 +160,8 @@ def lib():
     L.neo_tune_db_clear.restype = None
     L.neo_last_error.restype = ctypes.c_char_p
     global _RAW_STREAM
-    _RAW_STREAM = hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice")
+    if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice"):
+        _RAW_STREAM = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     _lib = L
     return L
 
@@ -183,13 +184,13 @@ def _check(rc):
 
 
 def _stream(stream=None):
-    import torch
     if stream is not None:
         return stream.cuda_stream
     # the current stream's handle without a torch.cuda.Stream object around it
     # (2.6 us a call, a fifth of a small layer's)
     if _RAW_STREAM:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return _RAW_STREAM[0](_RAW_STREAM[1]())
+    import torch
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -229,6 +230,21 @@ def _dptr_typed(t, dtype, name="tensor"):
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+def _current_device():
+    import torch
+    return torch.cuda.current_device()
+
+
+def _here(stream, *tensors):
+    """The tensors of a call lie on the device that it runs on (elsewhere a kernel's access may fault)."""
+    dev = None if stream is None else getattr(stream, "device_index", None)
+    if dev is None:  # the current stream, or a handle that does not say
+        dev = _RAW_STREAM[1]() if _RAW_STREAM else _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor on {t.device} in a call on device {dev}")
 
 
 def _pair(v):
@@ -688,11 +704,17 @@ def _cache(cache):
     """A KVCache (or a tuple of its four tensors) as the C struct."""
     k, v, ks, vs = cache
     shape = k.shape
-    if len(shape) != 4 or v.shape != shape or ks.shape != shape[:3] or vs.shape != shape[:3]:
+    if len(shape) != 4 or v.shape != shape or ks.shape != shape[:3] or vs.shape != ks.shape:
         raise ValueError("a cache is k and v [pages][kv_heads][page_size][head_dim] and their scales [pages][kv_heads][page_size]")
+    return KvCacheStruct(*_cache_ptrs(k, v, ks, vs), *shape)
+
+
+def _cache_ptrs(k, v, ks, vs):
     i8, f32 = _DTYPES["i8"], _DTYPES["f32"]
-    return KvCacheStruct(_vec(k, 0, i8, "k"), _vec(v, 0, i8, "v"), _vec(ks, 0, f32, "k_scale"), _vec(vs, 0, f32, "v_scale"),
-                         *shape)
+    if (k.dtype is i8 and v.dtype is i8 and ks.dtype is f32 and vs.dtype is f32 and k.is_cuda and v.is_cuda and ks.is_cuda and vs.is_cuda
+            and k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
+        return k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()
+    return _vec(k, 0, i8, "k"), _vec(v, 0, i8, "v"), _vec(ks, 0, f32, "k_scale"), _vec(vs, 0, f32, "v_scale")  # (says which)
 
 
 def _heads(t, heads, dim, name):
@@ -719,15 +741,14 @@ def _layers(cache):
     if not _DTYPES:
         _fill_dtypes()
     k, v, ks, vs = cache
-    if k.dim() == 4:
-        return _cache(cache), 1, 0
     shape = k.shape
-    if len(shape) != 5 or v.shape != shape or ks.shape != shape[:4] or vs.shape != shape[:4]:
+    if len(shape) == 4:
+        return _cache(cache), 1, 0
+    if len(shape) != 5 or v.shape != shape or ks.shape != shape[:4] or vs.shape != ks.shape:
         raise ValueError("the caches of several layers are k and v [layers][pages][kv_heads][page_size][head_dim] and their scales "
                          "[layers][pages][kv_heads][page_size]")
-    i8, f32 = _DTYPES["i8"], _DTYPES["f32"]
-    c = KvCacheStruct(_vec(k, 0, i8, "k"), _vec(v, 0, i8, "v"), _vec(ks, 0, f32, "k_scale"), _vec(vs, 0, f32, "v_scale"), *shape[1:])
-    return c, shape[0], shape[1] * shape[2] * shape[3]
+    layers, pages, heads, size, dim = shape
+    return KvCacheStruct(*_cache_ptrs(k, v, ks, vs), pages, heads, size, dim), layers, pages * heads * size
 
 
 def kv_write_int8(cache, k, v, slots, stream=None):
@@ -813,16 +834,18 @@ def rotary(x, positions, freqs, layout="half", amplitude=1.0, out=None, stream=N
     "half", neighbours in "interleaved", times amplitude.  out=x works in place."""
     t = x.dtype
     code = _dtype(t)
-    if x.dim() != 3:
-        raise ValueError(f"x must be [tokens][heads][dim], is {tuple(x.shape)}")
-    T, H, D = x.shape
-    xp, xt, xh = _heads(x, H, D, "x")
+    shape = x.shape
+    if len(shape) != 3:
+        raise ValueError(f"x must be [tokens][heads][dim], is {tuple(shape)}")
+    T, H, D = shape
+    xp, xt, xh = _heads(x, None, D, "x")
     if out is None:
         out = x.new_empty((T, H, D)) if stream is None else _new(x, (T, H, D), t, stream)
         op, ot, oh = out.data_ptr(), H * D, D
     else:
         op, ot, oh = _heads_like(out, x, "out")
     rot = 2 * freqs.numel()
+    _here(stream, x, positions, freqs, out)
     _check(lib().neo_rotary(xp, xt, xh, T, H, D, rot, ROTARY_LAYOUT[layout], code, _vec(positions, T, _DTYPES["i64"], "positions"),
                             _vec(freqs, 0, _DTYPES["f64"], "freqs"), amplitude, op, ot, oh, _stream(stream)))
     return out
@@ -845,6 +868,7 @@ def rotary_kv_write_int8(cache, q, k, v, slots, positions, freqs, layout="half",
     else:
         op, ot, oh = _heads_like(q_out, q, "q_out")
     i64 = _DTYPES["i64"]
+    _here(stream, cache[0], q, k, v, slots, positions, freqs, q_out)
     _check(lib().neo_rotary_kv_write_int8(ctypes.byref(c), qp, qt, qh, Hq, *_heads(k, c.kv_heads, D, "k"),
                                           *_heads(v, c.kv_heads, D, "v"), T, 2 * freqs.numel(), ROTARY_LAYOUT[layout], code,
                                           _vec(positions, T, i64, "positions"), _vec(freqs, 0, _DTYPES["f64"], "freqs"), amplitude,
@@ -861,6 +885,7 @@ def kv_copy_pages(cache, src, dst, entries=None, stream=None):
     n = src.numel()
     if dst.numel() != n or (entries is not None and entries.numel() != n):
         raise ValueError("src, dst and entries differ in length")
+    _here(stream, cache[0], src, dst, entries)
     _check(lib().neo_kv_copy_pages(ctypes.byref(c), layers, stride, _vec(src, n, i32, "src"), _vec(dst, n, i32, "dst"),
                                    _vec(entries, n, i32, "entries"), n, _stream(stream)))
 
@@ -875,6 +900,7 @@ def kv_compact(cache, page_table, bases, keep, keep_starts, max_keep, stream=Non
     B, most = _shape2(page_table, "page_table")
     tp, ts = _rows(page_table, B, most, i32, "page_table")
     n = keep.numel()
+    _here(stream, cache[0], page_table, bases, keep, keep_starts)
     _check(lib().neo_kv_compact(ctypes.byref(c), layers, stride, tp, ts, _vec(bases, B, i32, "bases"), _vec(keep, n, i32, "keep"),
                                 _vec(keep_starts, B + 1, i32, "keep_starts"), n, B, max_keep, _stream(stream)))
 
@@ -903,6 +929,7 @@ def attention_shared_int8(cache, q, page_table, context_lens, q_starts, group_st
         op, ot, oh = out.data_ptr(), Hq * D, D
     else:
         op, ot, oh = _heads_like(out, q, "out")
+    _here(stream, cache[0], q, page_table, context_lens, q_starts, group_starts, prefix_lens, out)
     _check(lib().neo_attention_shared_int8(ctypes.byref(c), qp, qt, qh, T, Hq, code, tp, ts,
                                            _vec(context_lens, B, i32, "context_lens"), _vec(q_starts, B + 1, i32, "q_starts"), B,
                                            _vec(group_starts, groups + 1, i32, "group_starts"), _vec(prefix_lens, groups, i32, "prefix_lens"),

@@ -794,6 +794,65 @@ def test_two_streams(torch):
 
 
 @gpu
+def test_calls_on_a_given_stream(torch):
+    """Every call on a stream of its own, while the current one is busy: the bits of the current one's calls."""
+    x = _rand(torch, (300, 6, 64), "bfloat16", 90).cuda()
+    q, k, v = x.split([2, 2, 2], 1)
+    pos, slots, f = torch.arange(300, device="cuda") * 7, torch.randperm(320, device="cuda")[:300], neo.rotary_frequencies(64)
+    caches = [neo.kv_cache(40, 2, 16, 64, layers=1) for _ in range(2)]
+    src, dst = _i32(torch, [0, 1, 2]), _i32(torch, [30, 31, 32])
+    table, bases = _i32(torch, [list(range(20))]), _i32(torch, [3])
+    keep = torch.arange(10, 290, 2, dtype=torch.int32, device="cuda")
+    starts = _i32(torch, [0, 140])
+
+    def calls(cache, **kw):
+        one = neo.kv_layer(cache, 0)
+        a = neo.rotary(x, pos, f, layout="interleaved", **kw)
+        b = neo.rotary_kv_write_int8(one, q, k, v, slots, pos, f, **kw)
+        neo.kv_copy_pages(cache, src, dst, **kw)
+        neo.kv_compact(cache, table, bases, keep, starts, 140, **kw)
+        return [a, b, *cache]
+    want = calls(caches[0])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    busy = torch.randn(4000, 4000, device="cuda")
+    for _ in range(20):
+        busy = busy @ busy * 1e-3
+    got = calls(caches[1], stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@gpu
+def test_a_rotation_of_more_items_than_a_launch_has(torch):
+    """2^30 threads and more are taken in slices of tokens."""
+    T, H = 1030, 1 << 20
+    x = torch.randn(T, 1, 2, device="cuda").bfloat16().expand(T, H, 2)
+    pos, f = torch.arange(T, device="cuda"), torch.tensor([0.3], dtype=torch.float64, device="cuda")
+    got = neo.rotary(x, pos, f)
+    want = neo.rotary(x[:, :3], pos, f)
+    assert torch.equal(got[:, ::H // 2 - 1], want) and torch.equal(got[-1], want[-1, :1].expand(H, 2))
+
+
+def test_a_tensor_of_another_device_is_refused():
+    """(On the host: which device a tensor says it lies on.)"""
+    class On:
+        def __init__(self, d):
+            self.device = d
+
+        def get_device(self):
+            return self.device
+
+    class Stream:
+        device_index = 1
+    neo._here(Stream, On(1), None, On(1))
+    for bad in ((On(0),), (On(1), On(2)), (On(1), None, On(-1))):
+        with pytest.raises(ValueError):
+            neo._here(Stream, *bad)
+
+
+@gpu
 def test_no_work(torch):
     """No tokens, no pairs, nothing kept: nothing happens."""
     cache = neo.kv_cache(2, 1, 4, 16, layers=2)
