@@ -868,7 +868,7 @@ def rotary_kv_write_int8(cache, q, k, v, slots, positions, freqs, layout="half",
     else:
         op, ot, oh = _heads_like(q_out, q, "q_out")
     i64 = _DTYPES["i64"]
-    _here(stream, cache[0], q, k, v, slots, positions, freqs, q_out)
+    _here(stream, *cache, q, k, v, slots, positions, freqs, q_out)
     _check(lib().neo_rotary_kv_write_int8(ctypes.byref(c), qp, qt, qh, Hq, *_heads(k, c.kv_heads, D, "k"),
                                           *_heads(v, c.kv_heads, D, "v"), T, 2 * freqs.numel(), ROTARY_LAYOUT[layout], code,
                                           _vec(positions, T, i64, "positions"), _vec(freqs, 0, _DTYPES["f64"], "freqs"), amplitude,
@@ -885,7 +885,7 @@ def kv_copy_pages(cache, src, dst, entries=None, stream=None):
     n = src.numel()
     if dst.numel() != n or (entries is not None and entries.numel() != n):
         raise ValueError("src, dst and entries differ in length")
-    _here(stream, cache[0], src, dst, entries)
+    _here(stream, *cache, src, dst, entries)
     _check(lib().neo_kv_copy_pages(ctypes.byref(c), layers, stride, _vec(src, n, i32, "src"), _vec(dst, n, i32, "dst"),
                                    _vec(entries, n, i32, "entries"), n, _stream(stream)))
 
@@ -900,7 +900,7 @@ def kv_compact(cache, page_table, bases, keep, keep_starts, max_keep, stream=Non
     B, most = _shape2(page_table, "page_table")
     tp, ts = _rows(page_table, B, most, i32, "page_table")
     n = keep.numel()
-    _here(stream, cache[0], page_table, bases, keep, keep_starts)
+    _here(stream, *cache, page_table, bases, keep, keep_starts)
     _check(lib().neo_kv_compact(ctypes.byref(c), layers, stride, tp, ts, _vec(bases, B, i32, "bases"), _vec(keep, n, i32, "keep"),
                                 _vec(keep_starts, B + 1, i32, "keep_starts"), n, B, max_keep, _stream(stream)))
 
@@ -929,7 +929,7 @@ def attention_shared_int8(cache, q, page_table, context_lens, q_starts, group_st
         op, ot, oh = out.data_ptr(), Hq * D, D
     else:
         op, ot, oh = _heads_like(out, q, "out")
-    _here(stream, cache[0], q, page_table, context_lens, q_starts, group_starts, prefix_lens, out)
+    _here(stream, *cache, q, page_table, context_lens, q_starts, group_starts, prefix_lens, out)
     _check(lib().neo_attention_shared_int8(ctypes.byref(c), qp, qt, qh, T, Hq, code, tp, ts,
                                            _vec(context_lens, B, i32, "context_lens"), _vec(q_starts, B + 1, i32, "q_starts"), B,
                                            _vec(group_starts, groups + 1, i32, "group_starts"), _vec(prefix_lens, groups, i32, "prefix_lens"),

@@ -852,6 +852,37 @@ def test_a_tensor_of_another_device_is_refused():
             neo._here(Stream, *bad)
 
 
+def test_every_tensor_of_a_call_is_looked_at(monkeypatch):
+    """Keys, values and both scales of the cache, and all the others, before any address is used."""
+    import torch
+    seen = []
+
+    class Enough(Exception):
+        pass
+
+    def here(stream, *tensors):
+        seen.extend(t for t in tensors if t is not None)
+        raise Enough
+    monkeypatch.setattr(neo, "_here", here)
+    monkeypatch.setattr(neo, "_cache_ptrs", lambda *t: (0, 0, 0, 0))
+    monkeypatch.setattr(neo, "_heads", lambda t, heads, dim, name: (0, 0, 0))
+    monkeypatch.setattr(neo, "_rows", lambda *a: (0, 0))
+    cache = neo.kv_cache(4, 2, 16, 64, device="cpu")
+    q, kv = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64)
+    i32, i64 = (lambda n: torch.zeros(n, dtype=torch.int32)), torch.zeros(3, dtype=torch.int64)
+    pos, freqs, table = i64.clone(), torch.zeros(32, dtype=torch.float64), torch.zeros((2, 4), dtype=torch.int32)
+    calls = [(neo.rotary, [q, pos, freqs], {}), (neo.rotary_kv_write_int8, [cache, q, kv, kv.clone(), i64, pos, freqs], {}),
+             (neo.kv_copy_pages, [cache, i32(2), i32(2), i32(2)], {}), (neo.kv_compact, [cache, table, i32(2), i32(5), i32(3), 4], {}),
+             (neo.attention_shared_int8, [cache, q, table, i32(2), i32(3), i32(2), i32(1), 2, 3, 60], {})]
+    for call, args, kw in calls:
+        seen.clear()
+        with pytest.raises(Enough):
+            call(*args, **kw)
+        want = [t for a in args for t in (a if isinstance(a, tuple) else (a,)) if isinstance(t, torch.Tensor)]
+        missed = [tuple(t.shape) for t in want if not any(t is s for s in seen)]
+        assert not missed, (call.__name__, missed)
+
+
 @gpu
 def test_no_work(torch):
     """No tokens, no pairs, nothing kept: nothing happens."""
