@@ -808,9 +808,9 @@ __global__ __launch_bounds__(WAVES * 64, DP == 256 ? 1 : DP == 64 ? 3 : 2) void 
 // The softmax's arithmetic and the products bound it, one after the other more
 // than side by side: of the cycles the vector unit works 58 %, the matrix unit
 // 37 % and LDS 38 %.  2048 tokens at 32,768, 32 query heads on 8 of 128 in
-// bfloat16 take 1.29 ms, 823 TFLOP/s (float16, whose weights are two terms, 28 %
-// more; float32, whose queries are too, 57 %).  Scores ten times as far apart, so
-// that most tiles hold small weights, take 2.24 ms.  32 rows a wave rather than
+// bfloat16 take 1.24 ms, 860 TFLOP/s (float16, whose weights are two terms, 29 %
+// more; float32, whose queries are too, 56 %).  Scores ten times as far apart, so
+// that most tiles hold small weights, take 2.18 ms.  32 rows a wave rather than
 // 16 halve the reads of keys and values (16 rows: 1.63 ms); eight waves share a
 // tile because each then converts an eighth of it (two workgroups of four
 // waves a CU: 1.54 ms).
@@ -1259,7 +1259,7 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs a, Parts ws) {
 // (8 tokens of 4 heads a unit, 8 sequences of 8192: 61 us against 79 in tiles of
 // 64); the tiles grow with the rows that the longest chunk has.  (A sequence of one
 // token beside a chunk takes a whole such tile: 512 tokens and 31 single ones over
-// 8192 take 407 us in one call, 125 and 112 in two.)
+// 8192 take 398 us in one call; 125 and 112 in two, with the slower join of then.)
 inline int tile_rows(const AttnArgs& a) {
     const int64_t rows = (int64_t)a.max_chunk * (a.q_heads / a.c.kv_heads);
     if (rows <= 32) return 16;

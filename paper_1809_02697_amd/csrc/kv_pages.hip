@@ -14,8 +14,8 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 // 16 bytes, four a thread, all loaded before the first is stored.  Nothing is read
 // again soon, so the stores (and where whole pages move, the loads) pass the caches
 // by: 256 pages of 64 tokens, 8 heads of 128, 16 layers (1.1 GB) 211 us (5.2 TB/s; 222
-// without); 256 tails of up to 64 tokens of one page 74 (83 without, and 136 with loads
-// that do so too).
+// without); 256 pairs' first entries of pages of 64 79 (84 without, and 136 with
+// loads that do so too).
 constexpr int kDepth = 4, kChunk = 256 * kDepth;
 
 template <bool WHOLE>
