@@ -885,11 +885,15 @@ int neo_rotary_kv_write_int8(const neo_kv_cache* cache, const void* q, int64_t q
  * neo_kv_compact: of sequence b, token bases[b] + i becomes what token
  *   keep[keep_starts[b] + i] was before the call (tokens are dropped, and those
  *   that are kept close up).  keep device int32 [kept], keep_starts device int32
- *   [seqs + 1], ascending from 0 to kept, bases device int32 [seqs]; page_table as
- *   in neo_attention_paged_int8.  An entry keep < bases[b] + i, or a token past
- *   the table's end or in a page outside the cache, moves nothing; entries need not
- *   ascend, and may repeat.  max_keep (host) bounds a sequence's entries: those past
- *   it move nothing.  A page that a token moves to must belong to one sequence.
+ *   [seqs + 1], ascending from 0 to kept, bases device int32 [seqs]; page_table
+ *   device int32, the pages of sequence b from b * table_stride on.  An entry
+ *   keep < bases[b] + i, or a token past the table's end or in a page outside the
+ *   cache, moves nothing; entries need not ascend, and may repeat.  max_keep (host)
+ *   bounds a sequence's entries: those past it move nothing.  A page that a token
+ *   moves to must belong to one sequence.  A row of the table has table_stride pages.
+ * neo_kv_compact_columns: the same where a row has table_pages pages (some columns of
+ *   a wider table), at most table_stride unless there is one row only; nothing behind
+ *   them is looked at.
  */
 int neo_kv_copy_pages(const neo_kv_cache* cache, int layers, int64_t layer_stride, const int32_t* src,
                       const int32_t* dst, const int32_t* entries, int pairs, neo_stream_t stream);
@@ -897,6 +901,10 @@ int neo_kv_compact(const neo_kv_cache* cache, int layers, int64_t layer_stride,
                    const int32_t* page_table, int64_t table_stride, const int32_t* bases,
                    const int32_t* keep, const int32_t* keep_starts, int kept, int seqs, int max_keep,
                    neo_stream_t stream);
+int neo_kv_compact_columns(const neo_kv_cache* cache, int layers, int64_t layer_stride,
+                           const int32_t* page_table, int64_t table_stride, int64_t table_pages,
+                           const int32_t* bases, const int32_t* keep, const int32_t* keep_starts,
+                           int kept, int seqs, int max_keep, neo_stream_t stream);
 
 /*
  * neo_attention_paged_int8 for sequences of which groups share their first

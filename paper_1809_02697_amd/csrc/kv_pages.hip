@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kMovers) void kv_close_up_few(CompactArgs a, int he
     const neo_kv_cache& c = a.c;
     const int parts = (c.kv_heads + heads - 1) / heads;
     const uint32_t each = (uint32_t)c.head_dim / 16;
-    const int64_t limit = a.table_stride * c.page_size;
+    const int64_t limit = a.table_pages * c.page_size;
     for (int64_t at = blockIdx.x; at < work; at += gridDim.x) {
         const int64_t q = at / parts;
         const int part = (int)(at - q * parts), of = (int)(q % (2 * a.layers)), b = (int)(q / (2 * a.layers));
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kMovers + 64) void kv_close_up(CompactArgs a, int t
     const neo_kv_cache& c = a.c;
     const int parts = c.kv_heads * splits;
     const uint32_t each = (uint32_t)c.head_dim / 16 / (uint32_t)splits;
-    const int64_t limit = a.table_stride * c.page_size;  // tokens that a sequence's table has
+    const int64_t limit = a.table_pages * c.page_size;  // tokens that a sequence's table has
     const bool mover = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < kMovers / 64;
     for (int64_t at = blockIdx.x; at < work; at += gridDim.x) {
         const int64_t q = at / parts;

@@ -139,6 +139,26 @@ bool check_layers(Check& c, const neo_kv_cache* k, int layers, int64_t layer_str
     return c.rc == NEO_OK;
 }
 
+int compact(const char* fn, const neo_kv_cache* cache, int layers, int64_t layer_stride, const int32_t* page_table, int64_t table_stride,
+            int64_t table_pages, const int32_t* bases, const int32_t* keep, const int32_t* keep_starts, int kept, int seqs, int max_keep,
+            neo_stream_t stream) {
+    Check c{fn};
+    check_layers(c, cache, layers, layer_stride) && c.size(kept, "kept", 0) && c.size(seqs, "seqs", 0) && c.size(max_keep, "max_keep", 0);
+    if (c.rc == NEO_OK && (table_pages < 0 || table_stride < 0 || (seqs > 1 && table_stride < table_pages)))
+        c.bad(NEO_ERR_SHAPE, "table_stride is less than a row");
+    if (c.rc == NEO_OK && (table_stride > 0x7fffffff || table_pages > 0x7fffffff))
+        c.bad(NEO_ERR_UNSUPPORTED, "table_stride or table_pages above 2^31 - 1");
+    if (c.rc != NEO_OK || layers == 0 || kept == 0 || seqs == 0 || max_keep == 0 || table_pages == 0) return c.rc;
+    c.ptr(page_table, "page_table") && c.aligned(page_table, "page_table", 4);
+    c.ptr(bases, "bases") && c.aligned(bases, "bases", 4);
+    c.ptr(keep, "keep") && c.aligned(keep, "keep", 4);
+    c.ptr(keep_starts, "keep_starts") && c.aligned(keep_starts, "keep_starts", 4);
+    if (c.rc != NEO_OK) return c.rc;
+    CompactArgs a{*cache, layers > 1 ? layer_stride : 0, layers, page_table, bases, keep, keep_starts, table_stride, table_pages, kept, seqs,
+                  std::min(max_keep, kept)};
+    return c.launched(launch_kv_compact(a, (hipStream_t)stream));
+}
+
 }  // namespace
 
 int neo_rmsnorm_int8(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
@@ -349,19 +369,17 @@ int neo_kv_compact(const neo_kv_cache* cache, int layers, int64_t layer_stride, 
                    const int32_t* bases, const int32_t* keep, const int32_t* keep_starts, int kept, int seqs, int max_keep,
                    neo_stream_t stream) {
     return guarded("neo_kv_compact", [&] {
-        Check c{"neo_kv_compact"};
-        check_layers(c, cache, layers, layer_stride) && c.size(kept, "kept", 0) && c.size(seqs, "seqs", 0) && c.size(max_keep, "max_keep", 0);
-        if (c.rc == NEO_OK && table_stride < 0) c.bad(NEO_ERR_SHAPE, "table_stride is less than a row");
-        if (c.rc == NEO_OK && table_stride > 0x7fffffff) c.bad(NEO_ERR_UNSUPPORTED, "table_stride above 2^31 - 1");
-        if (c.rc != NEO_OK || layers == 0 || kept == 0 || seqs == 0 || max_keep == 0 || table_stride == 0) return c.rc;
-        c.ptr(page_table, "page_table") && c.aligned(page_table, "page_table", 4);
-        c.ptr(bases, "bases") && c.aligned(bases, "bases", 4);
-        c.ptr(keep, "keep") && c.aligned(keep, "keep", 4);
-        c.ptr(keep_starts, "keep_starts") && c.aligned(keep_starts, "keep_starts", 4);
-        if (c.rc != NEO_OK) return c.rc;
-        CompactArgs a{*cache, layers > 1 ? layer_stride : 0, layers, page_table, bases, keep, keep_starts, table_stride, kept, seqs,
-                      std::min(max_keep, kept)};
-        return c.launched(launch_kv_compact(a, (hipStream_t)stream));
+        return compact("neo_kv_compact", cache, layers, layer_stride, page_table, table_stride, table_stride, bases, keep, keep_starts,
+                       kept, seqs, max_keep, stream);
+    });
+}
+
+int neo_kv_compact_columns(const neo_kv_cache* cache, int layers, int64_t layer_stride, const int32_t* page_table, int64_t table_stride,
+                           int64_t table_pages, const int32_t* bases, const int32_t* keep, const int32_t* keep_starts, int kept,
+                           int seqs, int max_keep, neo_stream_t stream) {
+    return guarded("neo_kv_compact_columns", [&] {
+        return compact("neo_kv_compact_columns", cache, layers, layer_stride, page_table, table_stride, table_pages, bases, keep,
+                       keep_starts, kept, seqs, max_keep, stream);
     });
 }
 

@@ -231,7 +231,7 @@ struct CompactArgs {
     int64_t layer_stride;
     int layers;
     const int32_t *table, *bases, *keep, *starts;
-    int64_t table_stride;
+    int64_t table_stride, table_pages;
     int kept, seqs, max_keep;
 };
 hipError_t launch_kv_compact(const CompactArgs& a, hipStream_t st);

@@ -144,6 +144,7 @@ def lib():
         "neo_rotary_kv_write_int8": [KV, P, L64, L64, I, P, L64, L64, P, L64, L64, I, I, I, I, P, P, F, P, P, L64, L64, P],
         "neo_kv_copy_pages": [KV, I, L64, P, P, P, I, P],
         "neo_kv_compact": [KV, I, L64, P, L64, P, P, P, I, I, I, P],
+        "neo_kv_compact_columns": [KV, I, L64, P, L64, L64, P, P, P, I, I, I, P],
         "neo_attention_shared_int8": [KV, P, L64, L64, I, I, I, P, L64, P, P, I, P, P, I, I, I, I, I, F, I, P, L64, L64, P],
         "neo_tune_db_save": [ctypes.c_char_p],
         "neo_tune_db_load": [ctypes.c_char_p],
@@ -893,16 +894,18 @@ def kv_copy_pages(cache, src, dst, entries=None, stream=None):
 def kv_compact(cache, page_table, bases, keep, keep_starts, max_keep, stream=None):
     """Tokens close up in every layer of the cache: token bases[b] + i of sequence b becomes what
     its token keep[keep_starts[b] + i] >= bases[b] + i was.  page_table int32 [seqs][pages of a
-    sequence], bases int32 [seqs], keep int32, keep_starts int32 [seqs + 1]; max_keep bounds a
-    sequence's entries.  A page that a token moves to must belong to one sequence."""
+    sequence] (of columns of a wider table those alone are looked at), bases int32 [seqs], keep int32,
+    keep_starts int32 [seqs + 1]; max_keep bounds a sequence's entries.  A page that a token moves to
+    must belong to one sequence."""
     c, layers, stride = _layers(cache)
     i32 = _DTYPES["i32"]
     B, most = _shape2(page_table, "page_table")
     tp, ts = _rows(page_table, B, most, i32, "page_table")
     n = keep.numel()
     _here(stream, *cache, page_table, bases, keep, keep_starts)
-    _check(lib().neo_kv_compact(ctypes.byref(c), layers, stride, tp, ts, _vec(bases, B, i32, "bases"), _vec(keep, n, i32, "keep"),
-                                _vec(keep_starts, B + 1, i32, "keep_starts"), n, B, max_keep, _stream(stream)))
+    _check(lib().neo_kv_compact_columns(ctypes.byref(c), layers, stride, tp, ts, most, _vec(bases, B, i32, "bases"),
+                                        _vec(keep, n, i32, "keep"), _vec(keep_starts, B + 1, i32, "keep_starts"), n, B, max_keep,
+                                        _stream(stream)))
 
 
 def attention_shared_int8(cache, q, page_table, context_lens, q_starts, group_starts, prefix_lens, max_chunk, max_group,
