@@ -819,8 +819,9 @@ int neo_attention_paged_int8(const neo_kv_cache* cache, const void* q, int64_t q
  * values is (x[i], x[i + rot_dim / 2]) in the layout HALF, (x[2 i], x[2 i + 1])
  * in INTERLEAVED; at position p it becomes
  *   amplitude * (a cos t - b sin t, b cos t + a sin t),  t = p * freqs[i]
- * the product and the angle in 64 bits (right for |t| up to 2^45), sine and
- * cosine rounded to float32, the rest in float32, rounded once to `dtype`.
+ * the product, the angle, its sine and cosine and those times `amplitude` in 64 bits
+ * (right for |t| up to 2^45), rounded once to float32, the rest in float32, rounded
+ * once to `dtype`.
  * Values from rot_dim on stay as they are.
  */
 enum neo_rotary_layout { NEO_ROTARY_HALF = 0, NEO_ROTARY_INTERLEAVED = 1 };
@@ -855,18 +856,18 @@ int neo_rotary_frequencies(int rot_dim, double base, int scaling, double factor,
  *   and the keys, turned in float32 and not rounded between, and values quantized
  *   into the entries slots[t] as neo_kv_write_int8 does.  Tokens whose slot lies
  *   outside the cache have their queries turned all the same.
- * amplitude finite.
+ * amplitude finite in float32.
  */
 int neo_rotary(const void* x, int64_t x_token_stride, int64_t x_head_stride, int tokens, int heads,
                int head_dim, int rot_dim, int layout, int dtype, const int64_t* positions,
-               const double* freqs, float amplitude, void* y, int64_t y_token_stride,
+               const double* freqs, double amplitude, void* y, int64_t y_token_stride,
                int64_t y_head_stride, neo_stream_t stream);
 int neo_rotary_kv_write_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride,
                              int64_t q_head_stride, int q_heads, const void* k,
                              int64_t k_token_stride, int64_t k_head_stride, const void* v,
                              int64_t v_token_stride, int64_t v_head_stride, int tokens, int rot_dim,
                              int layout, int dtype, const int64_t* positions, const double* freqs,
-                             float amplitude, const int64_t* slots, void* q_out,
+                             double amplitude, const int64_t* slots, void* q_out,
                              int64_t out_token_stride, int64_t out_head_stride, neo_stream_t stream);
 
 /*

@@ -9,25 +9,25 @@
 //
 // t is one product in 64 bits, taken to the quarter turn next to it in two parts
 // of pi / 2, so that positions of 2^30 keep their angle; sine and cosine are
-// polynomials in 64 bits, rounded once.  A workgroup works its tokens' angles out
-// once, into LDS, while the values are on their way; a lane takes two vectors of
-// 16 bytes, neighbouring lanes neighbouring ones.
+// polynomials in 64 bits, rounded once, with the amplitude in them.  A workgroup
+// works its tokens' angles out once, into LDS, while the values are on their way; a
+// lane takes two vectors of 16 bytes, neighbouring lanes neighbouring ones.
 #include "token_types.h"
 
 namespace neo {
 namespace {
 
-// A cos t and A sin t.  |x| <= pi / 4: the series end at x^13 / 13! < 7e-12 and
-// x^12 / 12! < 2e-10.
-__device__ inline void angle(double t, float amplitude, float& c, float& s) {
+// A cos t and A sin t, each rounded once.  |x| <= pi / 4: the series end at
+// x^13 / 13! < 7e-12 and x^12 / 12! < 2e-10.
+__device__ inline void angle(double t, double amplitude, float& c, float& s) {
     const double n = rint(t * 0.6366197723675814);
     const double x = fma(-n, 6.123233995736766e-17, fma(-n, 1.5707963267948966, t)), z = x * x;
     const double sine = fma(x * z, fma(z, fma(z, fma(z, fma(z, -1. / 39916800, 1. / 362880), -1. / 5040), 1. / 120), -1. / 6), x);
     const double cosine = fma(z, fma(z, fma(z, fma(z, fma(z, -1. / 3628800, 1. / 40320), -1. / 720), 1. / 24), -0.5), 1.);
     const int quarter = (int)(n - 4. * floor(n * 0.25));  // 0 .. 3
     const double cc = quarter & 1 ? sine : cosine, ss = quarter & 1 ? cosine : sine;
-    c = (float)((quarter + 1) & 2 ? -cc : cc) * amplitude;
-    s = (float)(quarter & 2 ? -ss : ss) * amplitude;
+    c = (float)(((quarter + 1) & 2 ? -cc : cc) * amplitude);
+    s = (float)((quarter & 2 ? -ss : ss) * amplitude);
 }
 
 // ---- vectors of a row ----------------------------------------------------------------

@@ -1,5 +1,6 @@
 // C-ABI entry points of the token operators: argument validation, then the
 // launchers.
+#include <cfloat>
 #include <cmath>
 #include <exception>
 #include <string>
@@ -90,11 +91,11 @@ bool check_out(Check& c, const void* p, int64_t ts, int64_t hs, int tokens, int 
 
 // What both rotary calls take; in place, the strides are the input's.
 bool check_rotary(Check& c, const void* x, int64_t xts, int64_t xhs, int tokens, int heads, int dim, int rot_dim, int layout, int dtype,
-                  const int64_t* positions, const double* freqs, float amplitude, const void* y, int64_t yts, int64_t yhs,
+                  const int64_t* positions, const double* freqs, double amplitude, const void* y, int64_t yts, int64_t yhs,
                   const char* in, const char* out) {
     if (c.rc == NEO_OK && (rot_dim < 2 || rot_dim % 2 || rot_dim > dim)) c.bad(NEO_ERR_SHAPE, "rot_dim must be even, 2 .. head_dim");
     if (c.rc == NEO_OK && layout != NEO_ROTARY_HALF && layout != NEO_ROTARY_INTERLEAVED) c.bad(NEO_ERR_INVALID_ARG, "layout");
-    if (c.rc == NEO_OK && !std::isfinite(amplitude)) c.bad(NEO_ERR_INVALID_ARG, "amplitude must be finite");
+    if (c.rc == NEO_OK && !(std::fabs(amplitude) <= FLT_MAX)) c.bad(NEO_ERR_INVALID_ARG, "amplitude must be finite in float32");
     if (c.rc != NEO_OK || tokens == 0) return c.rc == NEO_OK;
     c.ptr(x, in) && c.aligned(x, in, dtype_size(dtype));
     if (c.rc == NEO_OK && (xts < 0 || xhs < 0)) c.bad(NEO_ERR_INVALID_ARG, "negative stride");
@@ -307,7 +308,7 @@ int neo_rotary_frequencies(int rot_dim, double base, int scaling, double factor,
 }
 
 int neo_rotary(const void* x, int64_t x_token_stride, int64_t x_head_stride, int tokens, int heads, int head_dim, int rot_dim,
-               int layout, int dtype, const int64_t* positions, const double* freqs, float amplitude, void* y,
+               int layout, int dtype, const int64_t* positions, const double* freqs, double amplitude, void* y,
                int64_t y_token_stride, int64_t y_head_stride, neo_stream_t stream) {
     return guarded("neo_rotary", [&] {
         Check c{"neo_rotary"};
@@ -326,7 +327,7 @@ int neo_rotary(const void* x, int64_t x_token_stride, int64_t x_head_stride, int
 int neo_rotary_kv_write_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
                              const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
                              int64_t v_head_stride, int tokens, int rot_dim, int layout, int dtype, const int64_t* positions,
-                             const double* freqs, float amplitude, const int64_t* slots, void* q_out, int64_t out_token_stride,
+                             const double* freqs, double amplitude, const int64_t* slots, void* q_out, int64_t out_token_stride,
                              int64_t out_head_stride, neo_stream_t stream) {
     return guarded("neo_rotary_kv_write_int8", [&] {
         Check c{"neo_rotary_kv_write_int8"};

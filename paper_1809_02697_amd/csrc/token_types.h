@@ -212,7 +212,7 @@ struct RotaryArgs {
     int heads;
     const int64_t* positions;
     const double* freqs;
-    float amplitude;
+    double amplitude;
     int tokens, dim, rot, layout;
     KvArgs kv;  // with the cache's write: keys (turned too) and values
 };

@@ -140,8 +140,8 @@ def lib():
         "neo_attention_paged_int8": [KV, P, L64, L64, I, I, I, P, L64, P, P, I, I, I, F, I, P, L64,
                                      L64, P],
         "neo_rotary_frequencies": [I, D, I, D, D, D, D, P],
-        "neo_rotary": [P, L64, L64, I, I, I, I, I, I, P, P, F, P, L64, L64, P],
-        "neo_rotary_kv_write_int8": [KV, P, L64, L64, I, P, L64, L64, P, L64, L64, I, I, I, I, P, P, F, P, P, L64, L64, P],
+        "neo_rotary": [P, L64, L64, I, I, I, I, I, I, P, P, D, P, L64, L64, P],
+        "neo_rotary_kv_write_int8": [KV, P, L64, L64, I, P, L64, L64, P, L64, L64, I, I, I, I, P, P, D, P, P, L64, L64, P],
         "neo_kv_copy_pages": [KV, I, L64, P, P, P, I, P],
         "neo_kv_compact": [KV, I, L64, P, L64, P, P, P, I, I, I, P],
         "neo_kv_compact_columns": [KV, I, L64, P, L64, L64, P, P, P, I, I, I, P],

@@ -1,5 +1,6 @@
 """Calls of the operators of requests that share a prompt which the tests beside the
-operators (test_shared_prompt) do not make: page tables that are columns of wider ones."""
+operators (test_shared_prompt) do not make: page tables that are columns of wider ones,
+amplitudes of a rotation that float32 does not hold."""
 import ctypes
 
 import numpy as np
@@ -9,9 +10,10 @@ from paper_1809_02697_amd import neo
 
 from gpu_util import torch_cuda
 from test_shared_prompt import _bits, _compacted, _layers, _tables, cuda
-from test_token_ops import BAD_CACHES, FAKE, ODD, _struct
+from test_token_ops import BAD_CACHES, F32, FAKE, ODD, U, _struct
 
 gpu = pytest.mark.gpu
+u = U["float32"]
 
 
 @pytest.fixture(scope="module")
@@ -62,6 +64,38 @@ def test_closing_up_within_columns_refusals():
     assert call(ts=-1) == -2 and call(pages=-1) == -2 and call(pages=9) == -2 and call(ts=1 << 31, pages=1) == -4
     assert call(seqs=1, ts=0, pages=1 << 31) == -4
     assert call(pages=0, table=None) == 0 and call(kept=0, keep=None) == 0 and call(seqs=0, table=None) == 0
+
+
+def test_an_amplitude_past_float32_is_refused():
+    def call(amp):
+        return neo.lib().neo_rotary(FAKE, 256, 64, 0, 4, 64, 64, 0, F32, FAKE, FAKE, amp, FAKE, 256, 64, None)
+    assert call(3.4028234663852886e38) == 0 and call(-3.4028234663852886e38) == 0
+    for amp in (3.5e38, -1e300, float("inf"), float("nan")):
+        assert call(amp) == -1 and "amplitude" in neo.last_error(), amp
+
+
+# ---- rotation --------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("amp", [1.2, 1.3465, 0.1, -7.3])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_sine_and_cosine_are_rounded_once(torch, layout, amp):
+    """A pair (1, 0) becomes (A cos t, A sin t): in 64 bits within 2^-31 A (the series end below 7e-12
+    and 2e-10, the angle's rounding below 2^-50 of an angle up to 2^20), rounded to float32 once (u)."""
+    T, H, half = 700, 2, 24
+    rng = np.random.default_rng(5)
+    pos, f = rng.integers(0, 1 << 20, T), rng.uniform(0, 1, half)
+    x = torch.zeros(T, H, 2 * half, device="cuda")
+    a, b = (slice(0, half), slice(half, None)) if layout == "half" else (slice(0, None, 2), slice(1, None, 2))
+    x[..., a] = 1
+    t = pos.astype(np.float64)[:, None, None] * f
+    got = [neo.rotary(x, cuda(pos), cuda(f), layout=layout, amplitude=amp)]
+    cache = neo.kv_cache(T, 1, 1, 2 * half)
+    got.append(neo.rotary_kv_write_int8(cache, x, x[:, :1], x[:, :1], torch.arange(T, device="cuda"), cuda(pos), cuda(f), layout=layout, amplitude=amp))
+    for y in got:
+        for part, want in ((a, amp * np.cos(t)), (b, amp * np.sin(t))):
+            err = np.abs(y[..., part].double().cpu().numpy() - want)
+            assert (err <= u * np.abs(want) * (1 + 2.0 ** -20) + 2.0 ** -30 * abs(amp)).all(), (err / np.abs(want)).max() / u
 
 
 # ---- closing up ------------------------------------------------------------------------
