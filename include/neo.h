@@ -923,10 +923,17 @@ int neo_kv_compact_columns(const neo_kv_cache* cache, int layers, int64_t layer_
  *   max_own       host: how many cached tokens a sequence has behind its prefix at
  *                 most (0: not known).  The work is laid out for it; where one has
  *                 more, its tokens take longer and are the same
- * and the rest as there.  A window hides shared tokens too, but they are read: for
- * windows much shorter than the prefix the other call reads less.  The parts of
- * the shared tokens are kept in the workspace of the stream,
- * tokens * q_heads * (head_dim + 2) floats beside those of the shares.
+ * and the rest as there.  A window hides shared tokens too, but they are read where
+ * they are read together.  The parts of the shared tokens are kept in the workspace of
+ * the stream, tokens * q_heads * (head_dim + 2) floats beside those of the shares.
+ * What reading them once saves is judged by max_context - max_own, as if all sequences
+ * shared so much: a sequence that shares nothing and is as long as the others makes
+ * that little.  neo_attention_shared_saving_int8 is told instead:
+ *   saved         host: how many cached tokens fewer are read, the sum over groups of
+ *                 (its sequences - 1) * prefix.  Under a window, of
+ *                   its sequences * seen - prefix - its rows * (prefix - seen) / 32,
+ *                 seen = min(prefix, window + max_chunk - 1), a group's rows its new
+ *                 tokens * q_heads / kv_heads
  */
 int neo_attention_shared_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride,
                               int64_t q_head_stride, int tokens, int q_heads, int dtype,
@@ -936,6 +943,15 @@ int neo_attention_shared_int8(const neo_kv_cache* cache, const void* q, int64_t 
                               int max_chunk, int max_group, int max_context, int max_own, float scale,
                               int window, void* out, int64_t out_token_stride,
                               int64_t out_head_stride, neo_stream_t stream);
+int neo_attention_shared_saving_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride,
+                                     int64_t q_head_stride, int tokens, int q_heads, int dtype,
+                                     const int32_t* page_table, int64_t table_stride,
+                                     const int32_t* context_lens, const int32_t* q_starts, int seqs,
+                                     const int32_t* group_starts, const int32_t* prefix_lens, int groups,
+                                     int max_chunk, int max_group, int max_context, int max_own,
+                                     int64_t saved, float scale, int window, void* out,
+                                     int64_t out_token_stride, int64_t out_head_stride,
+                                     neo_stream_t stream);
 
 #ifdef __cplusplus
 }

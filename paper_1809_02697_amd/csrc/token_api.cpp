@@ -5,6 +5,7 @@
 #include <exception>
 #include <string>
 
+#include "attention_share.h"
 #include "token_types.h"
 
 using namespace neo;
@@ -158,6 +159,57 @@ int compact(const char* fn, const neo_kv_cache* cache, int layers, int64_t layer
     CompactArgs a{*cache, layers > 1 ? layer_stride : 0, layers, page_table, bases, keep, keep_starts, table_stride, table_pages, kept, seqs,
                   std::min(max_keep, kept)};
     return c.launched(launch_kv_compact(a, (hipStream_t)stream));
+}
+
+// Both calls over shared prefixes; `saved` null: by the bounds.
+int shared_attention(const char* fn, const neo_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int tokens,
+                     int q_heads, int dtype, const int32_t* page_table, int64_t table_stride, const int32_t* context_lens,
+                     const int32_t* q_starts, int seqs, const int32_t* group_starts, const int32_t* prefix_lens, int groups,
+                     int max_chunk, int max_group, int max_context, int max_own, const int64_t* saved, float scale, int window, void* out,
+                     int64_t out_token_stride, int64_t out_head_stride, neo_stream_t stream) {
+    Check c{fn};
+    c.size(groups, "groups", 0) && c.size(max_group, "max_group", 0) && c.size(max_own, "max_own", 0);
+    if (c.rc != NEO_OK || !check_attention(c, cache, q, q_token_stride, q_head_stride, tokens, q_heads, dtype, page_table, table_stride,
+                                           context_lens, q_starts, seqs, max_chunk, max_context, scale, window, out,
+                                           out_token_stride, out_head_stride))
+        return c.rc;
+    if (groups == 0 || groups > seqs) c.bad(NEO_ERR_SHAPE, "groups must be 1 .. seqs");
+    c.ptr(group_starts, "group_starts") && c.aligned(group_starts, "group_starts", 4);
+    c.ptr(prefix_lens, "prefix_lens") && c.aligned(prefix_lens, "prefix_lens", 4);
+    if (c.rc != NEO_OK) return c.rc;
+    AttnArgs own{*cache, q, out, q_token_stride, q_head_stride, out_token_stride, out_head_stride, table_stride,
+                 page_table, context_lens, q_starts, tokens, q_heads, seqs, std::min(max_chunk, tokens), max_context,
+                 window, scale};
+    own.group_starts = group_starts, own.prefix_lens = prefix_lens, own.all_seqs = seqs;
+    own.max_own = max_own ? std::min(max_own, max_context) : max_context;
+    AttnArgs shared = own;
+    shared.seqs = groups, shared.max_chunk = std::max(1, std::min(max_group, tokens));
+    if ((int64_t)own.max_chunk * q_heads > (1 << 28) / seqs || (int64_t)shared.max_chunk * q_heads > (1 << 28) / groups)
+        return c.bad(NEO_ERR_UNSUPPORTED, "max_chunk * q_heads * seqs or max_group * q_heads * groups above 2^28"), c.rc;
+    Workspace ws;
+    const double less = saved ? (double)*saved
+                              : saved_by_bounds(seqs, groups, (int64_t)tokens * (q_heads / cache->kv_heads), own.max_chunk, max_context,
+                                                max_own, window);
+    if (!worth_sharing(less, cache->kv_heads, cache->head_dim)) {
+        if (const size_t need = attention_workspace(own)) {
+            const int rc = stream_workspace(c.fn, (hipStream_t)stream, need, &ws);
+            if (rc != NEO_OK) return rc;
+        }
+        return c.launched(launch_attention(dtype, own, ws.ptr, (hipStream_t)stream));
+    }
+    // the rows' parts of the shared tokens, how many each sequence shares, and behind them the shares' parts, of one launch
+    // at a time
+    const size_t rows = (size_t)tokens * q_heads, o = rows * cache->head_dim, lens = o + 2 * rows, parts = (lens + seqs + 3) / 4 * 4;
+    const int rc = stream_workspace(c.fn, (hipStream_t)stream,
+                                    (parts + std::max(attention_shared_floats(shared), attention_own_floats(own))) * sizeof(float), &ws);
+    if (rc != NEO_OK) return rc;
+    for (AttnArgs* a : {&shared, &own}) {
+        a->part_o = ws.ptr;
+        a->part_ml = reinterpret_cast<float2*>(ws.ptr + o);
+        a->shared = reinterpret_cast<int32_t*>(ws.ptr + lens);
+    }
+    if (const int failed = c.launched(launch_attention_shared(dtype, shared, ws.ptr + parts, (hipStream_t)stream))) return failed;
+    return c.launched(launch_attention_own(dtype, own, ws.ptr + parts, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -414,45 +466,21 @@ int neo_attention_shared_int8(const neo_kv_cache* cache, const void* q, int64_t 
                               int max_chunk, int max_group, int max_context, int max_own, float scale, int window, void* out,
                               int64_t out_token_stride, int64_t out_head_stride, neo_stream_t stream) {
     return guarded("neo_attention_shared_int8", [&] {
-        Check c{"neo_attention_shared_int8"};
-        c.size(groups, "groups", 0) && c.size(max_group, "max_group", 0) && c.size(max_own, "max_own", 0);
-        if (c.rc != NEO_OK || !check_attention(c, cache, q, q_token_stride, q_head_stride, tokens, q_heads, dtype, page_table, table_stride,
-                                               context_lens, q_starts, seqs, max_chunk, max_context, scale, window, out,
-                                               out_token_stride, out_head_stride))
-            return c.rc;
-        if (groups == 0 || groups > seqs) c.bad(NEO_ERR_SHAPE, "groups must be 1 .. seqs");
-        c.ptr(group_starts, "group_starts") && c.aligned(group_starts, "group_starts", 4);
-        c.ptr(prefix_lens, "prefix_lens") && c.aligned(prefix_lens, "prefix_lens", 4);
-        if (c.rc != NEO_OK) return c.rc;
-        AttnArgs own{*cache, q, out, q_token_stride, q_head_stride, out_token_stride, out_head_stride, table_stride,
-                     page_table, context_lens, q_starts, tokens, q_heads, seqs, std::min(max_chunk, tokens), max_context,
-                     window, scale};
-        own.group_starts = group_starts, own.prefix_lens = prefix_lens, own.all_seqs = seqs;
-        own.max_own = max_own ? std::min(max_own, max_context) : max_context;
-        AttnArgs shared = own;
-        shared.seqs = groups, shared.max_chunk = std::max(1, std::min(max_group, tokens));
-        if ((int64_t)own.max_chunk * q_heads > (1 << 28) / seqs || (int64_t)shared.max_chunk * q_heads > (1 << 28) / groups)
-            return c.bad(NEO_ERR_UNSUPPORTED, "max_chunk * q_heads * seqs or max_group * q_heads * groups above 2^28"), c.rc;
-        Workspace ws;
-        if (!attention_worth_sharing(shared, own, max_context - std::min(max_own, max_context))) {
-            if (const size_t need = attention_workspace(own)) {
-                const int rc = stream_workspace(c.fn, (hipStream_t)stream, need, &ws);
-                if (rc != NEO_OK) return rc;
-            }
-            return c.launched(launch_attention(dtype, own, ws.ptr, (hipStream_t)stream));
-        }
-        // the rows' parts of the shared tokens, how many each sequence shares, and behind them the shares' parts, of one launch
-        // at a time
-        const size_t rows = (size_t)tokens * q_heads, o = rows * cache->head_dim, lens = o + 2 * rows, parts = (lens + seqs + 3) / 4 * 4;
-        const int rc = stream_workspace(c.fn, (hipStream_t)stream,
-                                        (parts + std::max(attention_shared_floats(shared), attention_own_floats(own))) * sizeof(float), &ws);
-        if (rc != NEO_OK) return rc;
-        for (AttnArgs* a : {&shared, &own}) {
-            a->part_o = ws.ptr;
-            a->part_ml = reinterpret_cast<float2*>(ws.ptr + o);
-            a->shared = reinterpret_cast<int32_t*>(ws.ptr + lens);
-        }
-        if (const int failed = c.launched(launch_attention_shared(dtype, shared, ws.ptr + parts, (hipStream_t)stream))) return failed;
-        return c.launched(launch_attention_own(dtype, own, ws.ptr + parts, (hipStream_t)stream));
+        return shared_attention("neo_attention_shared_int8", cache, q, q_token_stride, q_head_stride, tokens, q_heads, dtype, page_table,
+                                table_stride, context_lens, q_starts, seqs, group_starts, prefix_lens, groups, max_chunk, max_group,
+                                max_context, max_own, nullptr, scale, window, out, out_token_stride, out_head_stride, stream);
+    });
+}
+
+int neo_attention_shared_saving_int8(const neo_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                                     int tokens, int q_heads, int dtype, const int32_t* page_table, int64_t table_stride,
+                                     const int32_t* context_lens, const int32_t* q_starts, int seqs, const int32_t* group_starts,
+                                     const int32_t* prefix_lens, int groups, int max_chunk, int max_group, int max_context,
+                                     int max_own, int64_t saved, float scale, int window, void* out, int64_t out_token_stride,
+                                     int64_t out_head_stride, neo_stream_t stream) {
+    return guarded("neo_attention_shared_saving_int8", [&] {
+        return shared_attention("neo_attention_shared_saving_int8", cache, q, q_token_stride, q_head_stride, tokens, q_heads, dtype,
+                                page_table, table_stride, context_lens, q_starts, seqs, group_starts, prefix_lens, groups, max_chunk,
+                                max_group, max_context, max_own, &saved, scale, window, out, out_token_stride, out_head_stride, stream);
     });
 }

@@ -196,9 +196,6 @@ struct AttnArgs {
 };
 size_t attention_workspace(const AttnArgs& a);
 hipError_t launch_attention(int dtype, const AttnArgs& a, float* ws, hipStream_t st);
-// Whether to read the shared tokens once, `prefix` of them at most; else launch_attention
-// does without the groups.
-bool attention_worth_sharing(const AttnArgs& shared, const AttnArgs& own, int prefix);
 // Floats of the parts, and the launches: over the shared tokens, then over the others.
 size_t attention_shared_floats(const AttnArgs& a);
 size_t attention_own_floats(const AttnArgs& a);

@@ -66,7 +66,7 @@ class Layer:
             a = neo.attention_paged_int8(cache, q, step.table, step.contexts, step.starts, step.max_chunk, step.max_context)
         else:
             a = neo.attention_shared_int8(cache, q, step.table, step.contexts, step.starts, step.group_starts, step.prefix_lens,
-                                          step.max_chunk, step.max_group, step.max_context, step.max_own)
+                                          step.max_chunk, step.max_group, step.max_context, step.max_own, **step.saved)
         x = self.out(*neo.quantize_tokens_int8(a.view(T, self.q_heads * D)), dtype)
         q8, s, h = neo.rmsnorm_int8(x, self.norm2, residual=h)
         both = self.gate_up(q8, s, dtype)
@@ -102,6 +102,8 @@ class Step:
             self.group_starts, self.prefix_lens = ints(first), ints(prefix)
             self.max_group = max(starts[b] - starts[a] for a, b in zip(first, first[1:]))
             self.max_own = max(c - p for a, b, p in zip(first, first[1:], prefix) for c in contexts[a:b])
+            # (a single group's prefix is max_context - max_own)
+            self.saved = {} if len(prefix) == 1 else {"saved": neo.shared_saving(first, prefix)}
 
 
 def shared_pages(pages, page_size):

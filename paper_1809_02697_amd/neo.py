@@ -146,6 +146,7 @@ def lib():
         "neo_kv_compact": [KV, I, L64, P, L64, P, P, P, I, I, I, P],
         "neo_kv_compact_columns": [KV, I, L64, P, L64, L64, P, P, P, I, I, I, P],
         "neo_attention_shared_int8": [KV, P, L64, L64, I, I, I, P, L64, P, P, I, P, P, I, I, I, I, I, F, I, P, L64, L64, P],
+        "neo_attention_shared_saving_int8": [KV, P, L64, L64, I, I, I, P, L64, P, P, I, P, P, I, I, I, I, I, L64, F, I, P, L64, L64, P],
         "neo_tune_db_save": [ctypes.c_char_p],
         "neo_tune_db_load": [ctypes.c_char_p],
         "neo_tune_db_clear": [],
@@ -909,13 +910,15 @@ def kv_compact(cache, page_table, bases, keep, keep_starts, max_keep, stream=Non
 
 
 def attention_shared_int8(cache, q, page_table, context_lens, q_starts, group_starts, prefix_lens, max_chunk, max_group,
-                          max_context, max_own=0, scale=None, window=0, out=None, stream=None):
+                          max_context, max_own=0, scale=None, window=0, out=None, stream=None, saved=None):
     """attention_paged_int8 for sequences of which groups share their first tokens, which are then read
     once a group: sequences group_starts[g] .. group_starts[g + 1] - 1 (int32 [groups + 1]) share the
     first prefix_lens[g] (int32 [groups]), found in the first one's page table.  max_group: a group's
     new tokens at most (one with more is not taken together); max_own: a sequence's cached tokens behind
     the shared ones at most (0: not known), which the work is laid out for.  Every sequence's
-    own table has the shared tokens too: calls that would save too little read them there."""
+    own table has the shared tokens too: calls that would save too little read them there.  How much that
+    is, is judged by max_context - max_own, as if all sequences shared so much, or told by saved
+    (shared_saving): for sequences that share nothing beside others that do, or groups that differ."""
     t = q.dtype
     code = _dtype(t)
     i32 = _DTYPES["i32"]
@@ -933,12 +936,23 @@ def attention_shared_int8(cache, q, page_table, context_lens, q_starts, group_st
     else:
         op, ot, oh = _heads_like(out, q, "out")
     _here(stream, *cache, q, page_table, context_lens, q_starts, group_starts, prefix_lens, out)
-    _check(lib().neo_attention_shared_int8(ctypes.byref(c), qp, qt, qh, T, Hq, code, tp, ts,
-                                           _vec(context_lens, B, i32, "context_lens"), _vec(q_starts, B + 1, i32, "q_starts"), B,
-                                           _vec(group_starts, groups + 1, i32, "group_starts"), _vec(prefix_lens, groups, i32, "prefix_lens"),
-                                           groups, max_chunk, max_group, max_context, max_own,
-                                           D ** -0.5 if scale is None else scale, window, op, ot, oh, _stream(stream)))
+    args = (ctypes.byref(c), qp, qt, qh, T, Hq, code, tp, ts, _vec(context_lens, B, i32, "context_lens"),
+            _vec(q_starts, B + 1, i32, "q_starts"), B, _vec(group_starts, groups + 1, i32, "group_starts"),
+            _vec(prefix_lens, groups, i32, "prefix_lens"), groups, max_chunk, max_group, max_context, max_own)
+    rest = D ** -0.5 if scale is None else scale, window, op, ot, oh, _stream(stream)
+    _check(lib().neo_attention_shared_int8(*args, *rest) if saved is None else lib().neo_attention_shared_saving_int8(*args, saved, *rest))
     return out
+
+
+def shared_saving(group_starts, prefix_lens, window=0, max_chunk=1, heads=1):
+    """How many cached tokens fewer attention_shared_int8 reads where it reads those that a group shares
+    once (its `saved`), from its groups in host numbers.  Under a window, less what the products with hidden
+    ones cost there: with max_chunk new tokens a sequence, heads query heads a key head."""
+    saved = 0
+    for a, b, prefix in zip(group_starts, group_starts[1:], prefix_lens):
+        seen = min(prefix, window + max_chunk - 1) if window else prefix
+        saved += (b - a) * seen - prefix - (b - a) * max_chunk * heads * (prefix - seen) // 32
+    return saved
 
 
 def _int8_args(xq, C, w_packed, K, R, S, stride, pad):

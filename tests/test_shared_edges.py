@@ -1,16 +1,26 @@
 """Calls of the operators of requests that share a prompt which the tests beside the
 operators (test_shared_prompt) do not make: page tables that are columns of wider ones,
-amplitudes of a rotation that float32 does not hold."""
+amplitudes of a rotation that float32 does not hold, groups beside sequences that share
+nothing and under windows.
+
+Which table attention read is seen by a second one, in which all sequences of a group but
+the first have pages outside the cache in place of the whole shared ones: it gives the
+same bits where the shared tokens are read once, through the first one's, and others
+where every sequence reads its own.  Tolerances are those of test_shared_prompt."""
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
 
-from paper_1809_02697_amd import neo
+from paper_1809_02697_amd import decoder, neo
 
 from gpu_util import torch_cuda
-from test_shared_prompt import _bits, _compacted, _layers, _tables, cuda
-from test_token_ops import BAD_CACHES, F32, FAKE, ODD, U, _struct
+from test_shared_prompt import SHARED, _bits, _compacted, _layers, _most, _shared, cuda
+from test_token_ops import BAD_CACHES, F16, F32, FAKE, ODD, TYPES, U, _attention64, _attention_bound, _np, _rand, _struct
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1809_02697_amd", "csrc")
 
 gpu = pytest.mark.gpu
 u = U["float32"]
@@ -74,6 +84,77 @@ def test_an_amplitude_past_float32_is_refused():
         assert call(amp) == -1 and "amplitude" in neo.last_error(), amp
 
 
+RULE = r"""
+#include "attention_share.h"
+extern "C" double saved(int64_t seqs, int64_t groups, int64_t rows, int64_t chunk, int64_t context, int64_t own, int64_t window) {
+    return neo::saved_by_bounds(seqs, groups, rows, chunk, context, own, window);
+}
+extern "C" int worth(double saved, int heads, int dim) { return neo::worth_sharing(saved, heads, dim); }
+"""
+
+
+@pytest.fixture(scope="module")
+def rule(tmp_path_factory):
+    at = tmp_path_factory.mktemp("rule")
+    (at / "rule.cpp").write_text(RULE)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, "-o", str(at / "rule.so"), str(at / "rule.cpp")], check=True)
+    so = ctypes.CDLL(str(at / "rule.so"))
+    so.saved.restype, so.saved.argtypes, so.worth.argtypes = ctypes.c_double, [ctypes.c_int64] * 7, [ctypes.c_double, ctypes.c_int, ctypes.c_int]
+    return so
+
+
+def test_whether_to_share(rule):
+    """8 key/value heads of 128.  By the bounds where all sequences share alike, or told where they do not."""
+    share = lambda saved: bool(rule.worth(saved, 8, 128))  # noqa: E731
+    assert rule.saved(256, 1, 1024, 1, 32500, 500, 0) == 255 * 32000 == neo.shared_saving([0, 256], [32000])
+    assert share(255 * 32000) and not share(0) and not share(-5)
+    # one sequence that shares nothing, as long as the longest: the bounds say nothing of the others' prefix
+    assert rule.saved(256, 2, 1024, 1, 32500, 32500, 0) == 0
+    told = neo.shared_saving([0, 255, 256], [32000, 0])
+    assert told == 254 * 32000 and share(told)
+    # groups that differ; one of one sequence saves nothing whatever its prefix
+    assert neo.shared_saving([0, 3, 4, 9], [1000, 700, 20]) == 2 * 1000 + 4 * 20
+    # a window far shorter than the prefix: apart each sequence reads that much, together all of the prefix is multiplied
+    for seqs, window, together in ((16, 1000, False), (256, 1000, False), (16, 8000, False), (256, 8000, True), (16, 16000, True), (256, 16000, True)):
+        by_bounds = rule.saved(seqs, 1, seqs * 4, 1, 32500, 500, window)
+        told = neo.shared_saving([0, seqs], [32000], window=window, heads=4)
+        assert abs(by_bounds - told) <= 1 and share(told) == share(by_bounds) == together, (seqs, window)
+    # one that is as long as the prefix or longer hides nothing of it
+    assert rule.saved(7, 2, 28, 5, 500, 100, 396) == rule.saved(7, 2, 28, 5, 500, 100, 0) == 5 * 400
+    assert neo.shared_saving([0, 7], [400], window=396, max_chunk=5) == neo.shared_saving([0, 7], [400]) == 6 * 400
+    # sizes whose products leave 32 bits
+    assert rule.saved(1 << 20, 1, 1 << 25, 1, 0x7fff0000, 0, 0) == ((1 << 20) - 1) * 0x7fff0000
+
+
+def test_a_step_says_what_sharing_saves(rule):
+    """255 sequences on 32,000 tokens beside an unrelated one of 32,500: as much as without it."""
+    lone = list(range(1000, 1509))
+    pages = [list(range(500)) + [2000 + 10 * b + i for i in range(8)] for b in range(255)]
+    lengths = [32000 + b for b in range(255)]
+    step = decoder.Step(pages + [lone], lengths + [32500], [1] * 256, 64, "cpu", decoder.shared_pages(pages + [lone], 64))
+    assert step.saved == {"saved": 254 * 32000} and rule.worth(step.saved["saved"], 8, 128)
+    one = decoder.Step(pages, lengths, [1] * 255, 64, "cpu", decoder.shared_pages(pages, 64))
+    assert one.saved == {}
+    # (one group: by the bounds)
+    assert rule.saved(255, 1, 4 * 255, 1, one.max_context, one.max_own, 0) == 254 * 32000
+
+
+def test_shared_attention_that_is_told_refusals():
+    def call(c=None, q=FAKE, qt=256, T=3, Hq=4, dtype=F16, table=FAKE, ts=8, ctx=FAKE, st=FAKE, B=2, gs=FAKE, pl=FAKE, groups=1,
+             n=2, group=3, most=100, own=50, saved=1 << 40, scale=0.125, window=0, out=FAKE, ot=256, oh=64):
+        return neo.lib().neo_attention_shared_saving_int8(_struct() if c is None else c, q, qt, 64, T, Hq, dtype, table, ts, ctx, st, B, gs, pl,
+                                                          groups, n, group, most, own, saved, scale, window, out, ot, oh, None)
+    for over, code in BAD_CACHES:
+        assert call(_struct(**over)) == code and "neo_attention_shared_saving_int8: cache" in neo.last_error(), over
+    for name in ("q", "table", "ctx", "st", "out", "gs", "pl"):
+        assert call(**{name: None}) == -1 and call(**{name: ODD}) == -3, name
+    for name in ("T", "B", "n", "most", "window", "groups", "group", "own"):
+        assert call(**{name: -1}) == -1 and call(**{name: -1}, saved=-1) == -1, name
+    assert call(Hq=3) == -2 and call(qt=-1) == -1 and call(oh=63) == -2 and call(most=129) == -2 and call(groups=0) == -2 and call(groups=3) == -2
+    assert call(scale=0.0) == -1 and call(T=1 << 29, n=1 << 29) == -4 and call(T=1 << 27, group=1 << 27) == -4
+    assert call(T=0, q=None) == 0 and call(B=0, q=None) == 0 and call(n=0, q=None) == 0
+
+
 # ---- rotation --------------------------------------------------------------------------
 
 @gpu
@@ -128,3 +209,65 @@ def test_closing_up_looks_at_no_other_columns(torch, layers, H, page, D, tokens,
     assert neo.lib().neo_kv_compact(ctypes.byref(struct), layers, P * H * page, C(args[0].data_ptr()), width, *(C(a.data_ptr()) for a in args[1:]),
                                     len(flat), len(bases), max(len(k) for k in keep), neo._stream()) == 0
     assert all((_bits(a) == _bits(b)).all() for a, b in zip(dev, want))
+
+
+# ---- attention ---------------------------------------------------------------------------
+
+MUCH = 1 << 40      # saved: enough to share whatever the sizes
+
+
+def _blank(table, first, prefix, page):
+    """The table in which sequences of a group but its first have no pages of the whole shared ones."""
+    out = table.copy()
+    for a, b, p in zip(first, first[1:], prefix):
+        out[a + 1:b, :p // page] = -1
+    return out
+
+
+def _read(torch, dtype, groups, Hq, H, D, page, window=0, seed=0, **kw):
+    """The call over the shared tables, held against 64 bits, and whether it read the first sequences' pages for all."""
+    k, v, ks, vs, table, chunks, contexts, first, prefix = _shared(groups, H, D, page, seed)
+    starts = np.concatenate([[0], np.cumsum(chunks)]).astype(np.int32)
+    q = _rand(torch, (int(starts[-1]), Hq, D), dtype, seed + 1)
+    ref, A, B = _attention64(q.double().numpy(), k, v, ks, vs, table, contexts, starts, D ** -0.5, window)
+    args = [cuda(a) for a in (np.array(contexts, np.int32), starts, first, prefix)]
+    run = lambda t: neo.attention_shared_int8((cuda(k), cuda(v), cuda(ks), cuda(vs)), q.cuda(), cuda(t), *args, max(chunks), _most(groups),  # noqa: E731
+                                              max(contexts), window=window, **kw)
+    got = run(table)
+    bound = _attention_bound(ref, A, B, D, max(contexts), dtype) + 16 * u * A
+    assert (np.abs(_np(got) - ref) <= bound).all()
+    other = _blank(table, first, prefix, page)
+    assert (other != table).any()
+    return torch.equal(run(other), got)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", [i for i, (g, _, _, _, page, _) in enumerate(SHARED) if any(p >= page and len(s) > 1 for p, s in g)])
+def test_sharing_goes_by_what_is_told(torch, case, dtype):
+    """Windows among the cases."""
+    groups, Hq, H, D, page, window = SHARED[case]
+    assert _read(torch, dtype, groups, Hq, H, D, page, window, seed=case, saved=MUCH)
+    assert not _read(torch, dtype, groups, Hq, H, D, page, window, seed=case, saved=0)
+    assert not _read(torch, dtype, groups, Hq, H, D, page, window, seed=case, saved=-MUCH)
+
+
+@gpu
+@pytest.mark.parametrize("lone", [1, 800, 4100, 9000])
+def test_a_group_beside_a_sequence_that_shares_nothing(torch, lone):
+    """34 MB a prefix read once: told, the group's are, whatever the other's length; by the bounds not
+    where that one is the longest."""
+    groups = [(4000, [(1, 1 + b % 40) for b in range(40)]), (0, [(1, lone)])]
+    own = max(lone, 40)
+    told = neo.shared_saving([0, 40, 41], [4000, 0])
+    assert _read(torch, "bfloat16", groups, 8, 8, 128, 16, seed=30, max_own=own, saved=told)
+    if lone > 4000:
+        assert not _read(torch, "bfloat16", groups, 8, 8, 128, 16, seed=30, max_own=own)
+
+
+@gpu
+@pytest.mark.parametrize("window,together", [(0, True), (200, False), (3000, True)])
+def test_a_window_shorter_than_the_prefix_is_reckoned_with(torch, window, together):
+    """By the bounds: 40 sequences that see 200 of 4000 shared tokens read less apart."""
+    groups = [(4000, [(1, 1 + b % 40) for b in range(60)])]
+    assert _read(torch, "float16", groups, 8, 8, 128, 16, window, seed=31, max_own=40) == together
