@@ -106,18 +106,41 @@ class Step:
             self.saved = {} if len(prefix) == 1 else {"saved": neo.shared_saving(first, prefix)}
 
 
+def _alike(a, b):
+    """How many pages two lists begin with in common."""
+    same, differ = 0, min(len(a), len(b)) + 1  # so many are alike, so many are not (or not there)
+    step = differ - 1
+    while differ - same > 1:
+        if a[same:same + step] == b[same:same + step]:
+            same += step
+        else:
+            differ = same + step
+        step = (differ - same) // 2
+    return same
+
+
 def shared_pages(pages, page_size):
     """Of sequences in the order of their pages: groups that begin with the same ones, as (starts of the groups
-    and the number of sequences, tokens that each group's sequences have in common); None if none do."""
-    first, prefix = [], []
+    and the number of sequences, tokens that each group's sequences have in common); None if none do.  Sequences
+    that have more in common than their neighbours have with them are a group of their own where that saves more
+    reading: those on one long prompt, say, beside one that left it early."""
+    part = None    # the last closed stretch: its first sequence, the pages that it saves, its groups (first sequence, pages)
+    around = []    # stretches that go on: pages in common, and the same three of their closed parts
     for i, p in enumerate(pages):
-        if i and p and pages[i - 1] and p[0] == pages[i - 1][0]:
-            n = next((j for j, (a, b) in enumerate(zip(p, pages[first[-1]])) if a != b), min(len(p), len(pages[first[-1]])))
-            prefix[-1] = min(n * page_size, prefix[-1] or n * page_size)
-        else:
-            first.append(i)
-            prefix.append(0)
-    return (first + [len(pages)], prefix) if any(prefix) else None
+        part = i, 0, [(i, 0)]
+        alike = _alike(p, pages[i + 1]) if i + 1 < len(pages) else -1
+        while around and around[-1][0] > alike:
+            n, first, saved, groups = around.pop()
+            saved, groups, whole = saved + part[1], groups + part[2], (i - first) * n
+            part = (first, whole, [(first, n)]) if n and whole >= saved else (first, saved, groups)
+        if around and around[-1][0] == alike:
+            around[-1][2] += part[1]
+            around[-1][3] += part[2]
+        elif alike >= 0:
+            around.append([alike, *part])
+    if part is None or part[1] == 0:
+        return None
+    return [first for first, _ in part[2]] + [len(pages)], [n * page_size for _, n in part[2]]
 
 
 class Decoder:
@@ -229,12 +252,12 @@ class Decoder:
         self._release(shared)
         for p, n in zip(self.pages, need):
             p += [self._take() for _ in range(n)]
-        # sequences that begin with the same pages side by side
-        order = list(range(len(new)))
-        groups = None
+        # sequences that begin with the same pages side by side, those without new tokens left out
+        order, groups = list(range(len(new))), None
         if any(n > 1 for n in self.users):
-            order.sort(key=self.pages.__getitem__)
-            groups = shared_pages([self.pages[i] for i in order], size)
+            alike = sorted((i for i in order if new[i]), key=self.pages.__getitem__)
+            groups = shared_pages([self.pages[i] for i in alike], size)
+            order = alike if groups else order
         places = [range(a[-1] + 1 if a else 0, (a[-1] + 1 if a else 0) + m) for a, m in zip(self.at, new)]
         step = Step([self.pages[i] for i in order], [self.lengths[i] for i in order], [new[i] for i in order], size, self.device,
                     groups, self.rotary, [t for i in order for t in places[i]])

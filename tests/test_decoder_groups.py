@@ -1,0 +1,105 @@
+"""Which sequences a decoder's step puts into a group, on the host."""
+import random
+
+import pytest
+
+from paper_1809_02697_amd import decoder
+
+from test_decoder_shared import _Host
+
+
+class _Seen(Exception):
+    pass
+
+
+def _step(monkeypatch, d, tokens):
+    """What a step of the decoder hands to the device: pages, lengths and groups of its sequences."""
+    def step(pages, lengths, new, size, device, groups, rotary, positions):
+        raise _Seen([list(p) for p in pages], lengths, new, groups)
+    d.rotary = None
+    monkeypatch.setattr(decoder, "Step", step)
+    with pytest.raises(_Seen) as seen:
+        d.step(tokens)
+    return seen.value.args
+
+
+def _saved(groups):
+    first, prefix = groups
+    return sum((b - a - 1) * p for a, b, p in zip(first, first[1:], prefix))
+
+
+def test_one_that_left_early_does_not_part_the_others():
+    """255 sequences on 500 pages and one that shares the first of them alone: before and behind them in order."""
+    many = [list(range(500)) + [2000 + b] for b in range(255)]
+    for early in (-1, 5000):
+        pages = sorted(many + [[0, early, early + 1]])
+        first, prefix = decoder.shared_pages(pages, 64)
+        assert (first, prefix) == (([0, 1, 256], [0, 32000]) if early < 0 else ([0, 255, 256], [32000, 0]))
+    # two prompts behind one system prompt; three that share that one alone stay beside them
+    pages = sorted([[0, 1, 2, 3, 100 + b] for b in range(4)] + [[0, 10, 11, 12, 200 + b] for b in range(5)])
+    assert decoder.shared_pages(pages, 1) == ([0, 4, 9], [4, 4])
+    # where all save as much together, they stay together
+    assert decoder.shared_pages([[0, 1, 2], [0, 1, 3], [0, 4]], 10) == ([0, 3], [10])
+    assert decoder.shared_pages([[0, 1, 2, 5], [0, 1, 2, 6], [0, 4]], 10) == ([0, 2, 3], [30, 0])
+    assert decoder.shared_pages([], 10) is None and decoder.shared_pages([[]], 10) is None and decoder.shared_pages([[1], [1]], 10) == ([0, 2], [10])
+    # as deep as sequences are many
+    deep = [list(range(k)) + [9000 + k] for k in range(1, 3000, 2)][::-1]
+    assert _saved(decoder.shared_pages(deep, 1)) >= 1499 * 1
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_groups_hold_what_they_say_and_save_no_less_than_one_a_first_page(seed):
+    r = random.Random(seed)
+    pages, fresh = [[]], 1000
+    for _ in range(r.randrange(1, 40)):
+        old = r.choice(pages)
+        p = old[:r.randrange(len(old) + 1)] if r.random() < 0.8 else []
+        p = p + list(range(fresh, fresh + r.randrange(6)))
+        fresh += 6
+        pages.append(p)
+    pages.sort()
+    got = decoder.shared_pages(pages, 3)
+    firsts = {}
+    for p in pages:
+        firsts.setdefault(p[0] if p else None, []).append(p)
+    least = 0
+    for k, ps in firsts.items():
+        if k is not None:
+            n = next((j for j, c in enumerate(zip(*ps)) if len(set(c)) > 1), min(map(len, ps)))
+            least += (len(ps) - 1) * n * 3
+    if got is None:
+        assert least == 0
+        return
+    first, prefix = got
+    assert first[0] == 0 and first[-1] == len(pages) and all(a < b for a, b in zip(first, first[1:])) and len(prefix) == len(first) - 1
+    for a, b, n in zip(first, first[1:], prefix):
+        assert n % 3 == 0 and all(p[:n // 3] == pages[a][:n // 3] and len(p) >= n // 3 for p in pages[a:b])
+        assert n == 0 or b - a > 1
+    assert _saved(got) >= least > 0 or least == 0
+
+
+def test_a_sequence_without_new_tokens_lowers_nothing(monkeypatch):
+    """A fork that went back to the first page and waits: the others' prefix is their own."""
+    d = _Host(60, 4)
+    d.fill(d.add(), 40)
+    d.fork(0, 3)
+    d.keep(2, range(6))
+    pages, lengths, new, groups = _step(monkeypatch, d, [[1], [1, 1], [], [1]])
+    assert groups == ([0, 3], [40]) and new == [1, 2, 1] and lengths == [40, 40, 40]
+    assert all(p[:10] == list(range(10)) for p in pages)
+    # all but one wait: nothing is shared, and no sequence is left out
+    pages, lengths, new, groups = _step(monkeypatch, d, [[], [], [1], []])
+    assert groups is None and new == [0, 0, 1, 0]
+
+
+def test_dropping_an_early_token_leaves_the_others_their_prefix(monkeypatch):
+    """(The pages behind it are copies then.)"""
+    monkeypatch.setattr(decoder.neo, "kv_compact", lambda *a: None)
+    d = _Host(100, 4)
+    d.cache = None
+    d.fill(d.add(), 80)
+    d.fork(0, 5)
+    d.keep(3, [t for t in range(80) if t != 6])
+    assert d.pages[3][0] == 0 and d.pages[3][1] != 1
+    pages, lengths, new, groups = _step(monkeypatch, d, [[1]] * 6)
+    assert sorted(groups[1]) == [0, 80] and len(groups[0]) == 3
