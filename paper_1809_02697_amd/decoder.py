@@ -241,8 +241,14 @@ class Decoder:
             raise ValueError(f"a token outside the vocabulary of {len(self.embed)}")
         size = self.page_size
         need = [-(-(n + m) // size) - len(p) for p, n, m in zip(self.pages, self.lengths, new)]
-        # a page that is not full is written in a copy if others hold it too
-        copied = [i for i, (p, n, m) in enumerate(zip(self.pages, self.lengths, new)) if m and n % size and self.users[p[n // size]] > 1]
+        # a page that is not full is written in a copy while others hold it too (the last of them writes the page itself)
+        copied, holders = [], {}
+        for i, (p, n, m) in enumerate(zip(self.pages, self.lengths, new)):
+            if m and n % size:
+                page = p[n // size]
+                if holders.setdefault(page, self.users[page]) > 1:
+                    copied.append(i)
+                    holders[page] -= 1
         if sum(need) + len(copied) > len(self.free):
             raise RuntimeError("the cache has no page left")
         shared = [self.pages[i][self.lengths[i] // size] for i in copied]

@@ -1,11 +1,16 @@
-"""Which sequences a decoder's step puts into a group, on the host."""
+"""Which sequences a decoder's step puts into a group, and which pages it takes, on the host;
+on the GPU that sequences which part in the middle of a page are what sequences apart are."""
 import random
 
 import pytest
 
 from paper_1809_02697_amd import decoder
 
+from gpu_util import torch_cuda
+from test_decoder import SHAPE
 from test_decoder_shared import _Host
+
+gpu = pytest.mark.gpu
 
 
 class _Seen(Exception):
@@ -103,3 +108,57 @@ def test_dropping_an_early_token_leaves_the_others_their_prefix(monkeypatch):
     assert d.pages[3][0] == 0 and d.pages[3][1] != 1
     pages, lengths, new, groups = _step(monkeypatch, d, [[1]] * 6)
     assert sorted(groups[1]) == [0, 80] and len(groups[0]) == 3
+
+
+def test_the_last_holder_of_a_page_writes_the_page_itself(monkeypatch):
+    """Two that share a page which is not full, one page free: one copy is enough."""
+    d = _Host(3, 4)
+    d.fill(d.add(), 8)
+    d.fork(0)
+    for i in range(2):
+        d.keep(i, range(6))
+    assert d.pages == [[0, 1], [0, 1]] and d.free == [2]
+    _step(monkeypatch, d, [[1], [1]])
+    assert d.copies == [([1], [2], None)] and d.pages == [[0, 2], [0, 1]] and d.users == [2, 1, 1] and d.free == []
+    # with a third one that waits, both writers need a copy
+    d = _Host(4, 4)
+    d.fill(d.add(), 8)
+    d.fork(0, 2)
+    for i in range(3):
+        d.keep(i, range(6))
+    _step(monkeypatch, d, [[1], [], [1]])
+    assert d.copies == [([1, 1], [2, 3], None)] and d.pages == [[0, 2], [0, 1], [0, 3]] and d.users == [3, 1, 1, 1]
+    d = _Host(3, 4)
+    d.fill(d.add(), 8)
+    d.fork(0, 2)
+    for i in range(3):
+        d.keep(i, range(6))
+    with pytest.raises(RuntimeError):
+        d.step([[1], [], [1]])
+    assert d.pages == [[0, 1]] * 3 and d.users == [3, 3, 0] and d.free == [2] and d.copies == []
+
+
+@gpu
+@pytest.mark.parametrize("layers", [1, 3])
+def test_sequences_that_part_in_the_middle_of_a_page(layers):
+    """Three that share a page which is not full write into it in one step, in two copies and the page itself:
+    the bits of sequences that shared nothing."""
+    torch = torch_cuda()
+    w = decoder.random_weights(layers, 300, 96, inner=160, **SHAPE)
+    r = random.Random(5)
+    prompt = [r.randrange(300) for _ in range(24)]
+    make = lambda pages: decoder.Decoder(w, pages=pages, page_size=8, dtype=torch.float32, freqs=decoder.neo.rotary_frequencies(32), **SHAPE)  # noqa: E731
+    d, apart = make(7), make(12)  # (two whole pages in common, three parted, two behind those)
+    d.add()
+    d.step([prompt])
+    d.fork(0, 2)
+    for _ in range(3):
+        apart.add()
+    apart.step([prompt] * 3)
+    for x in (d, apart):
+        for i in range(3):
+            x.keep(i, range(21))
+    for new in ([1, 2, 1], [2, 1, 2], [0, 3, 1]):
+        tokens = [[r.randrange(300) for _ in range(n)] for n in new]
+        assert torch.equal(d.step(tokens), apart.step(tokens))
+    assert len({p[2] for p in d.pages}) == 3 and [p[:2] for p in d.pages] == [d.pages[0][:2]] * 3
