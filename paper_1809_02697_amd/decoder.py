@@ -216,8 +216,12 @@ class Decoder:
         end = -(-len(tokens) // size)
         # pages that others hold too are written in a copy
         copied = [i for i in range(base // size, end) if self.users[pages[i]] > 1] if base < len(tokens) else []
-        if len(copied) > len(self.free):
+        # (pages behind the last one that nothing kept lies on, and that no other holds, may serve)
+        short, kept = len(copied) - len(self.free), {t // size for t in tokens}
+        spare = [i for i in range(end, len(pages)) if i not in kept and self.users[pages[i]] == 1][:max(short, 0)]
+        if short > len(spare):
             raise RuntimeError("the cache has no page left")
+        self._release(pages[i] for i in spare)
         new = [self._take() for _ in copied]
         self._copy([pages[i] for i in copied], new)
         self._release(pages[i] for i in copied)
@@ -226,7 +230,7 @@ class Decoder:
         if base < len(tokens):
             ints = lambda v: torch.tensor(v, dtype=torch.int32, device=self.device)  # noqa: E731
             neo.kv_compact(self.cache, ints([pages]), ints([base]), ints(tokens[base:]), ints([0, len(tokens) - base]), len(tokens) - base)
-        self._release(pages[end:])
+        self._release(pages[i] for i in range(end, len(pages)) if i not in spare)
         self.pages[sequence], self.lengths[sequence] = pages[:end], len(tokens)
         self.at[sequence] = [self.at[sequence][t] for t in tokens]
 

@@ -138,6 +138,37 @@ def test_the_last_holder_of_a_page_writes_the_page_itself(monkeypatch):
     assert d.pages == [[0, 1]] * 3 and d.users == [3, 3, 0] and d.free == [2] and d.copies == []
 
 
+def _closing(monkeypatch, d):
+    """The tables and kept tokens of the decoder's calls that close up."""
+    calls = []
+    d.cache = None
+    monkeypatch.setattr(decoder.neo, "kv_compact", lambda c, table, bases, keep, starts, most: calls.append((table.tolist(), bases.tolist(), keep.tolist())))
+    return calls
+
+
+def test_pages_that_a_sequence_gives_up_serve_its_copies(monkeypatch):
+    """No page is free, the first is shared, and the last holds nothing that is kept."""
+    d = _Host(4, 4)
+    d.fill(d.add(), 4)
+    d.fork(0)
+    d.fill(0, 16)
+    assert d.pages == [[0, 1, 2, 3], [0]] and d.free == []
+    calls = _closing(monkeypatch, d)
+    d.keep(0, [1, 2, 5, 6, 7])
+    assert d.copies == [([0], [2], None)] and calls == [([[2, 1, 2, 3]], [0], [1, 2, 5, 6, 7])]
+    assert d.pages == [[2, 1], [0]] and d.users == [1, 1, 1, 0] and d.free == [3] and d.at[0] == [1, 2, 5, 6, 7]
+    # a page that something kept lies on is read when the tokens close up; one that others hold too is not free
+    for first, second, kept in ((4, 16, [1, 5, 9, 12, 13]), (8, 8, [1, 2])):
+        d = _Host(second // 4, 4)
+        d.fill(d.add(), first)
+        d.fork(0)
+        d.fill(0, second)
+        before = [list(p) for p in d.pages], list(d.users), list(d.free), list(d.lengths)
+        with pytest.raises(RuntimeError):
+            d.keep(0, kept)
+        assert before == (d.pages, d.users, d.free, d.lengths) and d.copies == []
+
+
 @gpu
 @pytest.mark.parametrize("layers", [1, 3])
 def test_sequences_that_part_in_the_middle_of_a_page(layers):
@@ -162,3 +193,30 @@ def test_sequences_that_part_in_the_middle_of_a_page(layers):
         tokens = [[r.randrange(300) for _ in range(n)] for n in new]
         assert torch.equal(d.step(tokens), apart.step(tokens))
     assert len({p[2] for p in d.pages}) == 3 and [p[:2] for p in d.pages] == [d.pages[0][:2]] * 3
+
+
+@gpu
+def test_a_full_cache_closes_up_into_pages_it_gives_up():
+    torch = torch_cuda()
+    w = decoder.random_weights(2, 300, 96, inner=160, **SHAPE)
+    r = random.Random(6)
+    head, tail = [r.randrange(300) for _ in range(8)], [r.randrange(300) for _ in range(24)]
+    make = lambda pages: decoder.Decoder(w, pages=pages, page_size=8, dtype=torch.float32, freqs=decoder.neo.rotary_frequencies(32), **SHAPE)  # noqa: E731
+    d, apart = make(4), make(6)
+    d.add()
+    d.step([head])
+    d.fork(0)
+    d.step([tail, []])
+    assert d.free == []
+    for _ in range(2):
+        apart.add()
+    apart.step([head, head])
+    apart.step([tail, []])
+    for x in (d, apart):
+        x.keep(0, [0, 3, 4, 7, 9, 10, 15, 16, 18])
+    assert len(d.free) == 1 and d.pages[1] != d.pages[0][:1]
+    for tokens in ([[1, 2], []], [[3], []]):
+        assert torch.equal(d.step(tokens), apart.step(tokens))
+    d.drop(0)
+    apart.drop(0)
+    assert torch.equal(d.step([[], [4]]), apart.step([[], [4]]))       # what the fork reads is as it was
