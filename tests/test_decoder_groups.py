@@ -1,7 +1,9 @@
 """Which sequences a decoder's step puts into a group, and which pages it takes, on the host;
-on the GPU that sequences which part in the middle of a page are what sequences apart are."""
+on the GPU that sequences which part in the middle of a page are what sequences apart are, and
+that what a group has in common is read once, within the bound of attention (test_shared_prompt)."""
 import random
 
+import numpy as np
 import pytest
 
 from paper_1809_02697_amd import decoder
@@ -9,6 +11,7 @@ from paper_1809_02697_amd import decoder
 from gpu_util import torch_cuda
 from test_decoder import SHAPE
 from test_decoder_shared import _Host
+from test_token_ops import U, _attention64, _attention_bound, _np
 
 gpu = pytest.mark.gpu
 
@@ -220,3 +223,47 @@ def test_a_full_cache_closes_up_into_pages_it_gives_up():
     d.drop(0)
     apart.drop(0)
     assert torch.equal(d.step([[], [4]]), apart.step([[], [4]]))       # what the fork reads is as it was
+
+
+@gpu
+@pytest.mark.parametrize("beside", [[], [4300], [1, 5000]])
+def test_a_step_reads_a_long_prompt_once(monkeypatch, beside):
+    """33 sequences on a prompt of 4000 tokens, of which one left it early and one waits, and others that share
+    nothing, beside them: the pages of the first serve all of the group, and every output is within
+    the bound of attention against 64 bits."""
+    torch = torch_cuda()
+    shape = dict(q_heads=16, kv_heads=8, head_dim=128)
+    d = decoder.Decoder(decoder.random_weights(1, 300, 256, inner=256, **shape), pages=1500, page_size=16, dtype=torch.float32,
+                        freqs=decoder.neo.rotary_frequencies(128), **shape)
+    r = random.Random(8)
+    text = lambda n: [r.randrange(300) for _ in range(n)]  # noqa: E731
+    d.add()
+    d.step([text(4000)])
+    for n in beside:
+        d.add()
+        d.step([[]] * (len(d.pages) - 1) + [text(n)])
+    forks = d.fork(0, 33)
+    d.keep(forks[4], range(70))
+    d.step([[]] * forks[4] + [text(40)] + [[]] * (len(d.pages) - forks[4] - 1))
+    d.keep(forks[9], range(30))             # (it waits)
+    was, seen = decoder.neo.attention_shared_int8, []
+
+    def call(cache, q, table, contexts, starts, first, prefix, *rest, **kw):
+        out = was(cache, q, table, contexts, starts, first, prefix, *rest, **kw)
+        f, p, other = first.tolist(), prefix.tolist(), table.clone()
+        for a, b, n in zip(f, f[1:], p):
+            other[a + 1:b, :n // 16] = -1
+        same = torch.equal(was(cache, q, other, contexts, starts, first, prefix, *rest, **kw), out)
+        k, v, ks, vs = (t.cpu().numpy() for t in cache)
+        ctx = contexts.tolist()
+        ref, A, B = _attention64(q.double().cpu().numpy(), k, v, ks, vs, table.cpu().numpy(), ctx, starts.tolist(), 128 ** -0.5, 0)
+        within = np.abs(_np(out) - ref) <= _attention_bound(ref, A, B, 128, max(ctx), "float32") + 16 * U["float32"] * A
+        seen.append((same, within.all(), sorted(zip(p, (b - a for a, b in zip(f, f[1:]))))))
+        return out
+    monkeypatch.setattr(decoder.neo, "attention_shared_int8", call)
+    for i in range(3):
+        tokens = [text(1) for _ in d.pages]
+        tokens[forks[9]] = []
+        d.step(tokens)
+        same, within, groups = seen[i]
+        assert same and within and groups == sorted([(4000, 32), (0, 1)] + [(0, 1)] * len(beside))

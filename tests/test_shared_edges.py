@@ -17,7 +17,7 @@ import pytest
 from paper_1809_02697_amd import decoder, neo
 
 from gpu_util import torch_cuda
-from test_shared_prompt import SHARED, _bits, _compacted, _layers, _most, _shared, cuda
+from test_shared_prompt import SHARED, WHOLE, _attend, _bits, _compacted, _layers, _most, _shared, cuda
 from test_token_ops import BAD_CACHES, F16, F32, FAKE, ODD, TYPES, U, _attention64, _attention_bound, _np, _rand, _struct
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1809_02697_amd", "csrc")
@@ -271,3 +271,41 @@ def test_a_window_shorter_than_the_prefix_is_reckoned_with(torch, window, togeth
     """By the bounds: 40 sequences that see 200 of 4000 shared tokens read less apart."""
     groups = [(4000, [(1, 1 + b % 40) for b in range(60)])]
     assert _read(torch, "float16", groups, 8, 8, 128, 16, window, seed=31, max_own=40) == together
+
+
+@pytest.fixture
+def watched(monkeypatch):
+    """Of every call of attention over groups, whether it read the first sequences' pages for all."""
+    was, seen = neo.attention_shared_int8, []
+
+    def call(cache, q, table, contexts, starts, first, prefix, *rest, **kw):
+        out = was(cache, q, table, contexts, starts, first, prefix, *rest, **kw)
+        other = _blank(table.cpu().numpy(), first.tolist(), prefix.tolist(), cache[0].shape[-2])
+        seen.append((was(cache, q, cuda(other), contexts, starts, first, prefix, *rest, **kw) == out).all().item())
+        return out
+    monkeypatch.setattr(neo, "attention_shared_int8", call)
+    return seen
+
+
+def _whole_pages(groups, page):
+    return any(p >= page and sum(n > 0 for n, _ in s[1:]) for p, s in groups)
+
+
+@gpu
+@pytest.mark.parametrize("case", [i for i, (g, _, _, _, page, _) in enumerate(SHARED) if _whole_pages(g, page)])
+def test_the_cases_of_shared_prompts_share(torch, watched, case):
+    """Those of test_shared_prompt, whose bounds make sharing seem worth it; under a window the bounds
+    do not (those share above, where they are told to)."""
+    groups, Hq, H, D, page, window = SHARED[case]
+    _attend(torch, "bfloat16", groups, Hq, H, D, page, window, seed=case)
+    assert watched == [window == 0] * 2
+    _attend(torch, "bfloat16", groups, Hq, H, D, page, window, seed=case, force=False)
+    assert watched[2:] == [False] * 2
+
+
+@gpu
+@pytest.mark.parametrize("case", range(len(WHOLE)))
+def test_the_cases_of_whole_units_share(torch, watched, case):
+    groups, Hq, H, D, page, own = WHOLE[case]
+    _attend(torch, "bfloat16", groups, Hq, H, D, page, seed=80 + case, max_own=own, force=case == 3)
+    assert watched == [True] * 2
