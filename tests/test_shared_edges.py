@@ -17,7 +17,7 @@ import pytest
 from paper_1809_02697_amd import decoder, neo
 
 from gpu_util import torch_cuda
-from test_shared_prompt import SHARED, WHOLE, _attend, _bits, _compacted, _layers, _most, _shared, cuda
+from test_shared_prompt import SHARED, WHOLE, _attend, _bits, _compacted, _layers, _most, _shared, _tables, cuda
 from test_token_ops import BAD_CACHES, F16, F32, FAKE, ODD, TYPES, U, _attention64, _attention_bound, _np, _rand, _struct
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1809_02697_amd", "csrc")
@@ -209,6 +209,50 @@ def test_closing_up_looks_at_no_other_columns(torch, layers, H, page, D, tokens,
     assert neo.lib().neo_kv_compact(ctypes.byref(struct), layers, P * H * page, C(args[0].data_ptr()), width, *(C(a.data_ptr()) for a in args[1:]),
                                     len(flat), len(bases), max(len(k) for k in keep), neo._stream()) == 0
     assert all((_bits(a) == _bits(b)).all() for a, b in zip(dev, want))
+
+
+KINDS = [  # layers, heads, page size, dim, sequences, entries of each, bound
+    (1, 1, 16, 64, 2, 700, 700),       # chunks of 256 tokens
+    (3, 90, 7, 32, 2, 600, 550),       # so many heads that none is split
+    (1, 2, 16, 256, 3, 420, 333),      # an entry's bytes in four parts
+    (2, 1, 10, 128, 1, 1100, 1099),    # in two
+    (1, 3, 64, 240, 2, 300, 299),      # fifteen pieces, which are not split
+]
+
+
+@gpu
+@pytest.mark.parametrize("case", range(len(KINDS)))
+def test_closing_up_in_chunks_entries_of_any_kind(torch, case):
+    """More entries than a chunk holds, which repeat, descend, lie at or below their place, past the table or in
+    pages that do not exist, across the edges of chunks; a bound that ends inside a chunk, a base that is negative."""
+    layers, H, page, D, B, n, most = KINDS[case]
+    assert min(n, most) * D // 16 > 1024        # (the kernel that goes through them in chunks)
+    rng = np.random.default_rng(case)
+    need = -(-(2 * n) // page)
+    P = B * need + 1
+    table = _tables(rng, [need] * B, P)
+    for row in table:                           # a tenth of the pages are nowhere
+        row[rng.choice(need, need // 10, replace=False)] = rng.choice([-1, P, 2 ** 31 - 1])
+    have = _layers(torch, layers, P, H, page, D, case)
+    bases = [int(b) for b in rng.integers(0, 40, B)]
+    if B > 2:
+        bases[1] = -1
+    keep = []
+    for base in bases:
+        i = np.arange(n)
+        k = np.sort(rng.choice(2 * n, n, replace=False))                # most: from anywhere, in order
+        k = np.where(rng.random(n) < 0.2, rng.integers(-50, 3 * n, n), k)
+        k = np.where(rng.random(n) < 0.1, base + i, k)                  # where it is
+        k[100:140] = 2 * n - 1                                          # one token many times
+        k[200:290] = np.arange(200, 290)[::-1] + base + 95              # (descends past its own places)
+        k[250:260] = 2 ** 31 - 1
+        keep.append(k.tolist())
+    want = _compacted(have, table, bases, [k[:most] for k in keep])
+    starts = np.arange(B + 1, dtype=np.int32) * n
+    for _ in range(2):
+        dev = tuple(cuda(a) for a in have)
+        neo.kv_compact(dev, cuda(table), cuda(np.array(bases, np.int32)), cuda(np.array(keep, np.int64).astype(np.int32).ravel()), cuda(starts), most)
+        assert all((_bits(a) == _bits(b)).all() for a, b in zip(dev, want))
 
 
 # ---- attention ---------------------------------------------------------------------------
