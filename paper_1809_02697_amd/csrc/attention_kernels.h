@@ -78,7 +78,8 @@ __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // How many fp16 terms a type's queries and weights are taken as.  float16 queries
 // are exact in one, but one rounding of the weights would be as large as the
 // output's own (error against 64 bits 1.4 times as much); bfloat16's is eight
-// times larger.
+// times larger: with one term 256 tokens on a shared 32,000 are off by 1.668e-3 of
+// their norm, with two by 1.655e-3, what rounding them once leaves, in 258 us for 214.
 //
 // A term holds 11 bits from fp16's least normal number 2^-14 up, two terms 22
 // from 2^-3 up (and at least 11 from 2^-14).  Smaller weights (of keys whose

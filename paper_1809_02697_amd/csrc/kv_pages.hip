@@ -76,9 +76,9 @@ __global__ __launch_bounds__(256) void kv_copy(CopyArgs a, int chunks, int64_t w
 // back, in every wave, before the first of its stores.  Four waves move bytes, the
 // next chunk's on their way while one is stored; a fifth looks up where the
 // tokens of the chunk after that lie.
-// (4 sequences of 6000 kept tokens of up to 12,064, 8 layers of 8 heads of 128: 158
-// us, 5.1 TB/s; 178 with stores that stay in the caches, 370 with a chunk's loads waited
-// for before the next one's.)
+// (4 sequences of 6000 kept tokens of up to 12,064, 8 layers of 8 heads of 128: the
+// call 157 to 172 us, the kernel 159 under the profiler, 5.1 TB/s; the call 178 with stores
+// that stay in the caches, 370 with a chunk's loads waited for before the next one's.)
 constexpr int kMovers = 256, kTokensMax = 256;
 
 struct Lines {  // entries of head 0, of a chunk's tokens; to < 0: nothing moves
